@@ -354,6 +354,94 @@ qta_status qta_finest_attn(const void* q0, const void* k0, const void* v0,
                            int levels, const float* const* coarser_msg, const float* w,
                            void* out, void* stream);
 
+/* ---- positions and dense attention ---- */
+
+/*
+ * qta_rotary - rotary positions: pairs of channels of each head turned by an angle linear in the token's position,
+ * y1 = scale * (x1 cos t - x2 sin t), y2 = scale * (x2 cos t + x1 sin t), t = position * freqs[pair], for one or two
+ * tensors of the same tokens (queries and keys) in one launch.
+ *   tensors     `count` (1 or 2) of them: x, y are [B][N][heads][d] by strides in elements, the channels of a head
+ *               contiguous, aligned to their type (16-byte aligned tensors whose strides are multiples of 16 bytes, with
+ *               every half of an axis (half layout) or all turned channels (interleaved), and the rest, multiples of 16
+ *               bytes, take 16-byte accesses, others single elements). y may be x itself (in place, same strides);
+ *               otherwise they must not overlap. Strides of y must place no two elements together.
+ *   rot, axes   the first rot <= d channels turn, the others are copied. axes = 1: by the token's position; axes = 2:
+ *               the first rot/2 of them by its first position (row), the others by its second (column). rot is a multiple
+ *               of 2 axes; d <= QTA_MAX_ROTARY_D.
+ *   interleaved within an axis of S channels pair j is (2j, 2j+1); 0: (j, j + S/2).
+ *   freqs       device fp64 [rot/2], radians a position step, axis by axis. Angles are taken in fp64.
+ *   pos         device int32 [B][N][axes], pos_batch elements between batch elements (0: the same for all); or NULL:
+ *               start + n for axes = 1, and (n / width, n % width) for axes = 2, N a multiple of width.
+ *   inverse     nonzero: angles negated. scale is kept, so this is the gradient: dx from dy with the same arguments.
+ */
+#define QTA_MAX_ROTARY_D 4096
+typedef struct {
+    const void* x;
+    void* y;
+    int heads;
+    int64_t x_batch, x_token, x_head;
+    int64_t y_batch, y_token, y_head;
+} qta_rotary_tensor;
+
+qta_status qta_rotary(const qta_rotary_tensor* tensors, int count, int B, int N, int d, int rot, int axes, int width,
+                      int interleaved, int inverse, qta_dtype dtype, const double* freqs, const int32_t* pos,
+                      int64_t pos_batch, int start, float scale, void* stream);
+
+/*
+ * Differential attention: the difference of two softmax maps, the second with a learned weight,
+ *   O = P_0 V - lambda P_1 V,   P_m = softmax over the visible keys of scale * Q_m K_m^T,   m = 0, 1.
+ * Head i has the query maps 2i and 2i + 1 and, with g = i / (heads / kv_heads), the key maps 2g and 2g + 1 and the values g.
+ *   q           [B][Nq][2 heads][d], k [B][Nk][2 kv_heads][d], v [B][Nk][kv_heads][2d] dtype, by strides in elements;
+ *               channels contiguous, pointers 16-byte aligned, strides multiples of 16 bytes (0: broadcast).
+ *   lam         lambda by strides: 0 for the batch and the token where a head has one weight. fp32, or bf16 with bf16 inputs.
+ *   d           32 or 64; heads a multiple of kv_heads.
+ *   scale       of the logits; <= 0: 1/sqrt(d).
+ *   lens        device int32 [B] or NULL: element b's keys are [0, lens[b]) (clamped to [0, Nk]). What lies behind them is
+ *               never used, whatever it holds.
+ *   causal      nonzero: query i of element b sees the keys up to q_pos[b] + i (device int32 [B]); q_pos NULL: Nk - Nq + i.
+ * A row that sees no key gives 0, and has and gives no gradient.
+ * Sums, maxima and the softmax are fp32. With bf16 inputs the weights are rounded to bf16 for the products with V, and
+ * results once at the end.
+ */
+typedef struct {
+    const void* q;
+    const void* k;
+    const void* v;
+    const void* lam;
+    int B, heads, kv_heads, Nq, Nk, d;
+    qta_dtype dtype, lam_dtype;
+    int64_t q_batch, q_token, q_head;
+    int64_t k_batch, k_token, k_head;
+    int64_t v_batch, v_token, v_head;
+    int64_t lam_batch, lam_token, lam_head;
+    const int32_t* lens;
+    const int32_t* q_pos;
+    int causal;
+    float scale;
+} qta_diff_attn_args;
+
+/*
+ * qta_diff_attn - the forward.
+ *   out         [B][Nq][heads][2d] dtype, 16-byte aligned.
+ *   out1, lse   for qta_diff_attn_backward: P_1 V as out, and fp32 [B][heads][2][Nq], the base-2 logarithm of each row's
+ *               sum of weights (-inf for an empty row). Both NULL for inference.
+ */
+qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, void* out1, float* lse, void* stream);
+
+/*
+ * qta_diff_attn_backward - gradients for dout = dLoss/dout, the arguments and out, out1, lse being the forward's.
+ *   dout        [B][Nq][heads][2d] dtype, contiguous.
+ *   dq, dk, dv  dtype, contiguous in the shapes of q, k and v, overwritten (also where no row sees a key: zeros).
+ *   dlam        lambda's type, overwritten: [B][Nq][heads], or with dlam_heads nonzero [heads], summed over batch and tokens.
+ *   workspace   qta_diff_attn_backward_workspace_bytes bytes, 256-byte aligned; need not be preserved or cleared.
+ * dout, dq, dk, dv 16-byte aligned. Every gradient is summed in fp32 in a fixed order: runs are identical. For inputs
+ * broadcast by a zero stride the gradient comes in the full shape.
+ */
+size_t qta_diff_attn_backward_workspace_bytes(const qta_diff_attn_args* args);
+qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const void* out, const void* out1, const float* lse,
+                                  const void* dout, void* dq, void* dk, void* dv, void* dlam, int dlam_heads, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

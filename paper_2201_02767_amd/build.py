@@ -28,7 +28,8 @@ FLAGS = [
 # The attention kernels (forward and backward) never see a NaN (finite inputs; masked logits are
 # -inf and are selected away before use), so their max reductions may skip the NaN-quieting the
 # IEEE mode asks for, which lets each butterfly step fuse into one DPP max.
-NO_NAN_SOURCES = {"fine.hip", "coarse.hip", "backward.hip", "backward_bf16.hip", "coarse_bwd.hip"}
+NO_NAN_SOURCES = {"fine.hip", "coarse.hip", "backward.hip", "backward_bf16.hip", "coarse_bwd.hip",
+                  "diff_attn.hip", "diff_attn_bwd.hip"}
 
 # The fine kernels and the backward query pass keep one accumulator per 16-slot tile; with the MFMA
 # results in VGPRs instead of AGPRs (the compiler's default) they hold the same values in fewer

@@ -1,0 +1,273 @@
+// Differential attention: argument blocks, and the tiles and matrix fragments its kernels share.
+//
+//   O = P_0 V - lambda P_1 V,   P_m = softmax(scale Q_m K_m^T) over the visible keys,   m = 0, 1
+//
+// All products run on the 32x32 MFMA, contracted 16 elements at a time. A fragment is one lane's 8 elements of such a
+// step: lane l holds row l & 31, elements 8 (l >> 5) .. + 7 (bf16: one 32x32x16 instruction; fp32: eight 32x32x2 ones,
+// which take the elements in another order, the same on both sides). A result lane holds column l & 31 and rows
+// 8 (r >> 2) + 4 (l >> 5) + (r & 3) for r = 0 .. 15: eight of them, packed, are a fragment of the next product whose
+// contraction runs over those rows, in the order 4h .. 4h+3, 8+4h .. 8+4h+3 (h = l >> 5). The other operand of that
+// product is read from LDS in the same order (col_frag), so scores never leave their lanes.
+#ifndef QTA_DIFF_ATTN_H
+#define QTA_DIFF_ATTN_H
+
+#include "bf16_tiles.h"
+#include "qta_internal.h"
+
+namespace qta {
+
+struct DiffArgs {
+    const void* q;              // [B][Nq][2 heads][d], by strides; head i's maps are 2i and 2i + 1
+    const void* k;              // [B][Nk][2 kv_heads][d]
+    const void* v;              // [B][Nk][kv_heads][2d]
+    const void* lam;            // fp32, or bf16 with lam_bf16
+    bool lam_bf16, causal;
+    int B, heads, kv_heads, Nq, Nk;
+    int R;                      // Nq * (heads / kv_heads) rows of one key head: row r is query r / G of its head r % G
+    FastDiv div_G;
+    long long qb, qn, qh, kb, kn, kh, vb, vn, vh, lb, ln, lh;   // strides in elements
+    const int32_t* lens;        // [B] keys of each batch element, or NULL
+    const int32_t* q_pos;       // [B] key position of query 0 (causal), or NULL: Nk - Nq
+    float scale;                // of the logits, times log2(e): weights are powers of two
+    void* out;                  // [B][Nq][heads][2d]
+    // kept for the backward (NULL in inference): P_1 V, [B][Nq][heads][2d], and log2 of the weights' sums
+    // [B][heads][2][Nq] (-inf where a row sees nothing)
+    void* out1;
+    float* lse;
+};
+
+// The visible range of one batch element: keys [0, len), and for query i of a causal call those up to pos + i.
+struct DiffRange {
+    int len, pos;
+    bool causal;
+    __device__ __forceinline__ int limit(int i) const { return causal ? max(0, min(len, pos + i + 1)) : len; }
+};
+__device__ __forceinline__ DiffRange diff_range(const DiffArgs& a, int b)
+{
+    DiffRange r;
+    r.len = a.lens ? min(max(a.lens[b], 0), a.Nk) : a.Nk;
+    // (clamped so that pos + i + 1 cannot overflow; nothing changes in what is visible)
+    r.pos = a.causal ? (a.q_pos ? min(max(a.q_pos[b], -a.Nq - 1), a.Nk) : a.Nk - a.Nq) : 0;
+    r.causal = a.causal;
+    return r;
+}
+
+__device__ __forceinline__ float diff_lambda(const DiffArgs& a, int b, int i, int h)
+{
+    const long long at = b * a.lb + i * a.ln + h * a.lh;
+    return a.lam_bf16 ? bf16_bits_to_f32(static_cast<const uint16_t*>(a.lam)[at]) : static_cast<const float*>(a.lam)[at];
+}
+
+namespace diff {
+
+using tiles::bf16x8_t;
+using tiles::lds_byte;
+using tiles::lds_ptr;
+using tiles::pack2;
+using tiles::short4_t;
+using tiles::u32x4_t;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> struct Frag;
+template <> struct Frag<bf16> {
+    bf16x8_t v;
+};
+template <> struct Frag<float> {
+    float v[8];
+};
+
+__device__ __forceinline__ f32x16 mma(const Frag<bf16>& a, const Frag<bf16>& b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(const Frag<float>& a, const Frag<float>& b, f32x16 c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], c, 0, 0, 0);
+    return c;
+}
+
+// 16 bytes at p as part of a fragment; a fragment of 8 elements in memory.
+__device__ __forceinline__ void frag_from(Frag<bf16>& f, const u32x4_t& x, int) { f.v = __builtin_bit_cast(bf16x8_t, x); }
+__device__ __forceinline__ void frag_from(Frag<float>& f, const u32x4_t& x, int part)
+{
+    const f32x4 y = __builtin_bit_cast(f32x4, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[4 * part + i] = y[i];
+}
+template <typename T>
+__device__ __forceinline__ Frag<T> global_frag(const void* base, long long elem)
+{
+    constexpr int parts = sizeof(T) / 2;
+    const u32x4_t* p = reinterpret_cast<const u32x4_t*>(static_cast<const unsigned char*>(base) + elem * static_cast<long long>(sizeof(T)));
+    Frag<T> f;
+#pragma unroll
+    for (int i = 0; i < parts; ++i) frag_from(f, p[i], i);
+    return f;
+}
+
+// Result rows 8s .. 8s + 7 (in the order above) as a fragment. bf16: rounded to nearest, 2^-9 of each value at
+// most, once, as the matrix product asks; sums of weights are taken from the fp32 values.
+template <typename T>
+__device__ __forceinline__ Frag<T> pack_frag(const float* x)
+{
+    Frag<T> f;
+    if constexpr (sizeof(T) == 2) {
+        u32x4_t w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = pack2(x[2 * i], x[2 * i + 1]);
+        f.v = __builtin_bit_cast(bf16x8_t, w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f.v[i] = x[i];
+    }
+    return f;
+}
+
+// A tile of rows of W elements in LDS, in 16-byte chunks: chunk c of row r lies at place c ^ swz(r) of its row. The
+// swizzle spreads both ways of reading over all banks: 16 lanes on one chunk of 16 rows (row_frag), and for bf16 four
+// rows times 64 bytes (col_frag, transposed by the read). fp32 column reads meet two to a bank where a row is 128 bytes,
+// which an fp32 product (64 cycles for 2 of the 16 elements) hides.
+template <typename T, int W>
+struct Tile {
+    static constexpr int kRow = W * static_cast<int>(sizeof(T));
+    static constexpr int kChunks = kRow / 16;              // 4, 8, 16 or 32
+    static constexpr int bytes(int rows) { return rows * kRow; }
+
+    __device__ static __forceinline__ int swz(int r)
+    {
+        if constexpr (kChunks == 4) return (r >> 2) & 3;
+        else if constexpr (kChunks == 8) return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1 | ((r >> 3) & 1);
+        else if constexpr (sizeof(T) == 2) return (r & 3) << 2 | ((r >> 2) & 3);
+        else return ((r >> 2) & 1) << 3 | (r & 3) << 1 | ((r >> 3) & 1);
+    }
+
+    // Brings `rows` rows in (a multiple of 64 / kChunks times the waves taking part), each wave its share, 1 KB an
+    // instruction straight to LDS: `off(r)` is the byte offset of row r in `map`.
+    template <typename Off>
+    __device__ static __forceinline__ void stage(lds_byte* tile, __amdgpu_buffer_rsrc_t map, int rows, int wave, int waves,
+                                                 int lane, Off off)
+    {
+        constexpr int per = 64 / kChunks;                  // rows an instruction
+        static_assert(kChunks <= 32, "rows of at most 512 bytes");
+#pragma unroll
+        for (int r0 = 0; r0 < rows; r0 += per * waves) {
+            const int first = r0 + wave * per;
+            if (first >= rows) break;
+            const int r = first + lane / kChunks;
+            tiles::load_lds16(map, off(r) + static_cast<uint32_t>(((lane % kChunks) ^ swz(r)) * 16), 0, tile + first * kRow);
+        }
+    }
+
+    // Row r0 + (lane & 31), elements 16 step + 8 (lane >> 5) .. + 7.
+    __device__ static __forceinline__ Frag<T> row_frag(lds_byte* tile, int r0, int step, int lane)
+    {
+        constexpr int parts = sizeof(T) / 2;
+        const int r = r0 + (lane & 31), c = (2 * step + (lane >> 5)) * parts;
+        Frag<T> f;
+#pragma unroll
+        for (int i = 0; i < parts; ++i) {
+            const u32x4_t x = *(lds_ptr<u32x4_t>)(tile + r * kRow + ((c + i) ^ swz(r)) * 16);
+            frag_from(f, x, i);
+        }
+        return f;
+    }
+
+    // Column 32 ct + (lane & 31) of rows r0 + 4h .. + 3 and r0 + 8 + 4h .. + 3 (h = lane >> 5), r0 a multiple of 16.
+    __device__ static __forceinline__ Frag<T> col_frag(lds_byte* tile, int r0, int ct, int lane)
+    {
+        Frag<T> f;
+        const int h = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            // 16 lanes read 4 rows x 32 bytes, 8 bytes each, and receive one column of the four rows each
+            const int i = lane & 15, c = 4 * ct + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
+            short4_t x[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int r = r0 + 8 * u + 4 * h + (i >> 2);
+                x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr<short4_t>)(tile + r * kRow + (c ^ swz(r)) * 16 + (i & 1) * 8));
+            }
+            f.v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const int col = 32 * ct + (lane & 31);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = r0 + 8 * (j >> 2) + 4 * h + (j & 3);
+                f.v[j] = *(lds_ptr<float>)(tile + r * kRow + ((col >> 2) ^ swz(r)) * 16 + (col & 3) * 4);
+            }
+        }
+        return f;
+    }
+};
+
+// Row of result register r in a lane's half h.
+__device__ __forceinline__ constexpr int acc_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+// Four consecutive elements at p (16-byte aligned for fp32, 8 for bf16).
+template <typename T>
+__device__ __forceinline__ void store4(void* base, long long elem, float a, float b, float c, float d)
+{
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + elem) = make_uint2(pack2(a, b), pack2(c, d));
+    } else {
+        *reinterpret_cast<float4*>(static_cast<float*>(base) + elem) = make_float4(a, b, c, d);
+    }
+}
+
+__device__ __forceinline__ const unsigned char* byte_at(const void* p, long long elem, int size)
+{
+    return static_cast<const unsigned char*>(p) + elem * size;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float other_half(float x) { return xchg_f32<32>(x); }
+
+}  // namespace diff
+
+// Backward: the argument block, and what each pass writes.
+struct DiffBwdArgs {
+    DiffArgs f;                 // out, out1 and lse are the forward's (read)
+    const void* dout;           // [B][Nq][heads][2d] contiguous
+    // by rows of one key head, [B][kv_heads][kDiffStats][Rpad] fp32: lse_0, lse_1, t_0, t_1, lambda
+    float* stats;
+    int Rpad;                   // R rounded up to kDiffRowPad; rows behind R are zero
+    void* dq;                   // [B][Nq][2 heads][d]
+    void* dk;                   // [B][Nk][2 kv_heads][d]
+    void* dv;                   // [B][Nk][kv_heads][2d]
+    void* dlam;                 // lambda's type: [B][Nq][heads], or [heads] with lam_heads
+    bool lam_heads;
+    float* dlam_rows;           // fp32 [heads][B * Nq] with lam_heads
+    float grad_scale;           // scale of the logits
+};
+constexpr float kDiffLn2 = 0.693147180559945f;
+constexpr int kDiffStats = 5;
+constexpr int kDiffRowPad = 64;
+
+hipError_t launch_diff_attn(const DiffArgs& a, int d, bool use_bf16, hipStream_t stream);
+hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool use_bf16, hipStream_t stream);
+
+// Rotary positions of one or two tensors.
+struct RotaryTensor {
+    const void* x;
+    void* y;
+    int heads;
+    long long xb, xn, xh, yb, yn, yh;
+};
+struct RotaryArgs {
+    RotaryTensor t[2];
+    int B, N, d, rot, axes, width;
+    bool interleaved, inverse;
+    const double* freqs;        // [rot / 2] radians a position
+    const int32_t* pos;         // [B][N][axes], stride pos_b elements between batch elements; or NULL
+    long long pos_b;
+    int start;
+    float scale;
+    FastDiv div_N, div_W, div_pairs, div_items, div_heads;      // set by the launcher
+    int items, tokens;          // items of a head, tokens of a workgroup; set by the launcher
+};
+hipError_t launch_rotary(const RotaryArgs& a, bool use_bf16, hipStream_t stream);
+
+}  // namespace qta
+
+#endif

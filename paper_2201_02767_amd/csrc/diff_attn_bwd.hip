@@ -1,0 +1,399 @@
+// Differential attention, backward (the mathematics of the tiles is in diff_attn.h).
+//
+// With D = dO V^T, t_m = dO . O_m (O_m = P_m V) and the weights made again from the stored sums:
+//   dS_0 = P_0 (D - t_0),   dS_1 = -lambda P_1 (D - t_1),   dlambda = -t_1
+//   dQ_m = scale dS_m K_m,  dK_m = scale dS_m^T Q_m,        dV = (P_0 - lambda P_1)^T dO
+// Three launches: t_m and lambda by row; dQ, a wave taking 32 rows through the keys; dK and dV, a wave taking 32 keys
+// through the rows of every query head that shares them. D, and in the key pass V's weights, serve both maps, so here
+// a wave holds both. Each result is summed in one place and in one order: no atomics, the same bits every run.
+#include <atomic>
+
+#include "diff_attn.h"
+
+namespace qta {
+namespace {
+
+using namespace diff;
+
+constexpr int kThreads = 256;
+
+// ---- t_m, lambda's gradient ----
+
+// A row (b, i, h) takes 2D / V lanes of one 16-byte chunk each.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void diff_rows_kernel(DiffBwdArgs a)
+{
+    constexpr int V = 16 / static_cast<int>(sizeof(T)), LPR = 2 * D / V;
+    const DiffArgs& f = a.f;
+    const int G = f.heads / f.kv_heads;
+    const long long item = (static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / LPR;
+    const int c = threadIdx.x % LPR;
+    const long long per = a.Rpad, total = per * f.B * f.kv_heads;
+    if (item >= total) return;
+    const int bh = static_cast<int>(item / per), r = static_cast<int>(item - bh * per);
+    float* const st = a.stats + static_cast<size_t>(bh) * kDiffStats * a.Rpad + r;
+    if (r >= f.R) {
+        if (c == 0)
+#pragma unroll
+            for (int p = 0; p < kDiffStats; ++p) st[static_cast<size_t>(p) * a.Rpad] = 0.f;
+        return;
+    }
+    const int b = bh / f.kv_heads, i = fast_div(r, f.div_G), h = (bh - b * f.kv_heads) * G + r - i * G;
+    const long long row = (static_cast<long long>(b) * f.Nq + i) * f.heads + h;
+    const uint4* const go = reinterpret_cast<const uint4*>(a.dout) + row * LPR + c;
+    const uint4* const o = reinterpret_cast<const uint4*>(f.out) + row * LPR + c;
+    const uint4* const o1 = reinterpret_cast<const uint4*>(f.out1) + row * LPR + c;
+    float x[V], y[V], z[V];
+    Storage<T>::unpack(*go, x);
+    Storage<T>::unpack(*o, y);
+    Storage<T>::unpack(*o1, z);
+    float s = 0.f, t1 = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        s = fmaf(x[j], y[j], s);
+        t1 = fmaf(x[j], z[j], t1);
+    }
+    s = group_sum<LPR < 16 ? LPR : 16>(s);
+    t1 = group_sum<LPR < 16 ? LPR : 16>(t1);
+    if constexpr (LPR == 32) {
+        s += xchg_f32<16>(s);
+        t1 += xchg_f32<16>(t1);
+    }
+    if (c != 0) return;
+    const float lam = diff_lambda(f, b, i, h);
+    const float* const lse = f.lse + (static_cast<long long>(b) * f.heads + h) * 2 * f.Nq + i;
+    st[0] = lse[0];
+    st[a.Rpad] = lse[f.Nq];
+    st[2 * static_cast<size_t>(a.Rpad)] = fmaf(lam, t1, s);        // dO . O_0 = dO . (O + lambda O_1)
+    st[3 * static_cast<size_t>(a.Rpad)] = t1;
+    st[4 * static_cast<size_t>(a.Rpad)] = lam;
+    if (a.lam_heads) a.dlam_rows[static_cast<long long>(h) * f.B * f.Nq + static_cast<long long>(b) * f.Nq + i] = -t1;
+    else if (f.lam_bf16) Storage<bf16>::store1(a.dlam, row, -t1);
+    else Storage<float>::store1(a.dlam, row, -t1);
+}
+
+// A weight for each head: its rows' gradients summed, one workgroup a head.
+__global__ __launch_bounds__(1024) void diff_lambda_kernel(const float* rows, long long n, void* dlam, bool lam_bf16)
+{
+    __shared__ float part[16];
+    const float* const p = rows + blockIdx.x * n;
+    float s = 0.f;
+    for (long long i = threadIdx.x; i < n; i += 1024) s += p[i];
+    s = wave_sum_fast(s);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += part[i];
+    if (lam_bf16) Storage<bf16>::store1(dlam, blockIdx.x, t);
+    else Storage<float>::store1(dlam, blockIdx.x, t);
+}
+
+// ---- dQ ----
+
+template <typename T, int D, int BN>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kernel(DiffBwdArgs a)
+{
+    using KT = Tile<T, D>;
+    using VT = Tile<T, 2 * D>;
+    constexpr int ES = sizeof(T), BM = 128;
+    constexpr int kK = KT::bytes(BN), kStage = 2 * kK + VT::bytes(BN);
+    extern __shared__ __align__(16) unsigned char lds_raw[];
+    lds_byte* const lds = (lds_byte*)lds_raw;
+    const DiffArgs& f = a.f;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int tiles_n = (f.R + BM - 1) / BM;
+    const int logical = xcd_remap(blockIdx.x, gridDim.x);
+    const int bh = logical / tiles_n, tile = tiles_n - 1 - (logical - bh * tiles_n);
+    const int b = bh / f.kv_heads, g = bh - b * f.kv_heads, G = f.heads / f.kv_heads;
+    const int row0 = tile * BM, row1 = min(row0 + BM, f.R);
+    const DiffRange range = diff_range(f, b);
+    const int kend = range.limit(fast_div(row1 - 1, f.div_G)), kmask = range.limit(fast_div(row0, f.div_G));
+
+    const int rr = row0 + wave * 32 + (lane & 31), r = min(rr, f.R - 1);
+    const int qi = fast_div(r, f.div_G), h = g * G + r - qi * G, lim = range.limit(qi);
+    const float* const st = a.stats + static_cast<size_t>(bh) * kDiffStats * a.Rpad + r;
+    const float lse0 = st[0], lse1 = st[a.Rpad], t0 = st[2 * static_cast<size_t>(a.Rpad)],
+                t1 = st[3 * static_cast<size_t>(a.Rpad)], nlam = -st[4 * static_cast<size_t>(a.Rpad)];
+    Frag<T> qf[2][D / 16], of[D / 8];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+            qf[m][s] = global_frag<T>(f.q, b * f.qb + qi * f.qn + (2 * h + m) * f.qh + 16 * s + 8 * half);
+    const long long orow = ((static_cast<long long>(b) * f.Nq + qi) * f.heads + h) * (2 * D);
+#pragma unroll
+    for (int s = 0; s < D / 8; ++s) of[s] = global_frag<T>(a.dout, orow + 16 * s + 8 * half);
+    f32x16 acc[2][D / 32];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) acc[m][c] = f32x16{};
+
+    auto stage = [&](int k0, lds_byte* at) {
+        const int last = kend - 1 - k0;
+        const auto kmap0 = tiles::map_resource(byte_at(f.k, b * f.kb + k0 * f.kn + (2 * g) * f.kh, ES));
+        const auto kmap1 = tiles::map_resource(byte_at(f.k, b * f.kb + k0 * f.kn + (2 * g + 1) * f.kh, ES));
+        const auto vmap = tiles::map_resource(byte_at(f.v, b * f.vb + k0 * f.vn + g * f.vh, ES));
+        const uint32_t kstep = static_cast<uint32_t>(f.kn) * ES, vstep = static_cast<uint32_t>(f.vn) * ES;
+        auto koff = [&](int x) { return static_cast<uint32_t>(min(x, last)) * kstep; };
+        auto voff = [&](int x) { return static_cast<uint32_t>(min(x, last)) * vstep; };
+        KT::stage(at, kmap0, BN, wave, 4, lane, koff);
+        KT::stage(at + kK, kmap1, BN, wave, 4, lane, koff);
+        VT::stage(at + 2 * kK, vmap, BN, wave, 4, lane, voff);
+    };
+
+    const int wend = row0 + wave * 32 < f.R ? range.limit(fast_div(min(row0 + wave * 32 + 32, f.R) - 1, f.div_G)) : 0;
+    const int nt = (kend + BN - 1) / BN;
+    if (nt > 0) stage(0, lds);
+    for (int t = 0; t < nt; ++t) {
+        const int k0 = t * BN;
+        lds_byte* const cur = lds + (t & 1) * kStage;
+        tiles::wait_lds_loads();
+        __syncthreads();
+        if (t + 1 < nt) stage(k0 + BN, lds + ((t + 1) & 1) * kStage);
+#pragma unroll
+        for (int u = 0; u < BN / 32; ++u) {
+            if (k0 + 32 * u >= wend) break;
+            f32x16 s0{}, s1{}, dp{};
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+                s0 = mma(KT::row_frag(cur, 32 * u, c, lane), qf[0][c], s0);
+                s1 = mma(KT::row_frag(cur + kK, 32 * u, c, lane), qf[1][c], s1);
+            }
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) dp = mma(VT::row_frag(cur + 2 * kK, 32 * u, c, lane), of[c], dp);
+            const bool edge = k0 + 32 * u + 32 > kmask;
+            float d0[16], d1[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                d0[e] = exp2_fast(fmaf(s0[e], f.scale, -lse0)) * (dp[e] - t0);
+                d1[e] = exp2_fast(fmaf(s1[e], f.scale, -lse1)) * nlam * (dp[e] - t1);
+            }
+            if (edge) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (k0 + 32 * u + acc_row(e, half) >= lim) {
+                        d0[e] = 0.f;
+                        d1[e] = 0.f;
+                    }
+            }
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const Frag<T> f0 = pack_frag<T>(d0 + 8 * w), f1 = pack_frag<T>(d1 + 8 * w);
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    acc[0][c] = mma(KT::col_frag(cur, 32 * u + 16 * w, c, lane), f0, acc[0][c]);
+                    acc[1][c] = mma(KT::col_frag(cur + kK, 32 * u + 16 * w, c, lane), f1, acc[1][c]);
+                }
+            }
+        }
+    }
+    if (rr >= f.R) return;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                store4<T>(a.dq, ((static_cast<long long>(b) * f.Nq + qi) * 2 * f.heads + 2 * h + m) * D + 32 * c + acc_row(e, half),
+                          acc[m][c][e] * a.grad_scale, acc[m][c][e + 1] * a.grad_scale, acc[m][c][e + 2] * a.grad_scale,
+                          acc[m][c][e + 3] * a.grad_scale);
+}
+
+// ---- dK, dV ----
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D == 32 ? 2 : 1) void diff_dkv_kernel(DiffBwdArgs a)
+{
+    using QT = Tile<T, D>;
+    using OT = Tile<T, 2 * D>;
+    constexpr int ES = sizeof(T), BM = 32, BN = 128;
+    constexpr int kQ = QT::bytes(BM), kO = OT::bytes(BM), kStats = 1024, kStage = 2 * kQ + kO + kStats;
+    extern __shared__ __align__(16) unsigned char lds_raw[];
+    lds_byte* const lds = (lds_byte*)lds_raw;
+    const DiffArgs& f = a.f;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    const int tiles_n = (f.Nk + BN - 1) / BN;
+    const int logical = xcd_remap(blockIdx.x, gridDim.x);
+    const int bh = logical / tiles_n, tile = logical - bh * tiles_n;
+    const int b = bh / f.kv_heads, g = bh - b * f.kv_heads, G = f.heads / f.kv_heads;
+    const DiffRange range = diff_range(f, b);
+    const int k0 = tile * BN, wk0 = k0 + wave * 32, key = wk0 + (lane & 31);
+    const long long kc = min(key, f.Nk - 1);
+
+    f32x16 av[2 * D / 32], ak[2][D / 32];
+#pragma unroll
+    for (int c = 0; c < 2 * D / 32; ++c) av[c] = f32x16{};
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) ak[m][c] = f32x16{};
+
+    // rows that see any of these keys: from the first query at or behind k0 on
+    const int i0 = range.causal ? min(max(0, k0 - range.pos), f.Nq) : 0;
+    const int rbeg = (k0 < range.len ? i0 * G : f.R) / BM * BM;
+    const int nt = k0 < range.len ? (f.R - rbeg + BM - 1) / BM : 0;
+
+    if (nt > 0) {
+        Frag<T> kf[2][D / 16], vf[D / 8];
+        // (a key behind the element's last is read as that one; its weights are masked)
+        const long long kv = min(kc, static_cast<long long>(range.len) - 1);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s)
+                kf[m][s] = global_frag<T>(f.k, b * f.kb + kv * f.kn + (2 * g + m) * f.kh + 16 * s + 8 * half);
+#pragma unroll
+        for (int s = 0; s < D / 8; ++s) vf[s] = global_frag<T>(f.v, b * f.vb + kv * f.vn + g * f.vh + 16 * s + 8 * half);
+
+        const auto smap = tiles::map_resource(reinterpret_cast<const unsigned char*>(a.stats + static_cast<size_t>(bh) * kDiffStats * a.Rpad));
+        auto stage = [&](int r0, lds_byte* at) {
+            const int i_first = fast_div(r0, f.div_G);
+            const auto qmap0 = tiles::map_resource(byte_at(f.q, b * f.qb + i_first * f.qn + (2 * g * G) * f.qh, ES));
+            const auto omap = tiles::map_resource(
+                byte_at(a.dout, ((static_cast<long long>(b) * f.Nq + i_first) * f.heads + g * G) * (2 * D), ES));
+            auto place = [&](int r, int* i, int* hh) {
+                const int x = min(r0 + r, f.R - 1);
+                *i = fast_div(x, f.div_G);
+                *hh = x - *i * G;
+                *i -= i_first;
+            };
+            auto qoff = [&](int r) {
+                int i, hh;
+                place(r, &i, &hh);
+                return static_cast<uint32_t>((i * static_cast<int>(f.qn) + 2 * hh * static_cast<int>(f.qh)) * ES);
+            };
+            auto qoff1 = [&](int r) { return qoff(r) + static_cast<uint32_t>(f.qh) * ES; };
+            auto ooff = [&](int r) {
+                int i, hh;
+                place(r, &i, &hh);
+                return static_cast<uint32_t>((i * f.heads + hh) * (2 * D) * ES);
+            };
+            QT::stage(at, qmap0, BM, wave, 4, lane, qoff);
+            QT::stage(at + kQ, qmap0, BM, wave, 4, lane, qoff1);
+            OT::stage(at + 2 * kQ, omap, BM, wave, 4, lane, ooff);
+            // the five statistics of the 32 rows, 128 bytes each (lanes behind the fifth repeat it)
+            if (wave == 0) {
+                const int p = min(lane >> 3, kDiffStats - 1);
+                tiles::load_lds16(smap, (static_cast<uint32_t>(p) * a.Rpad + r0 + 4 * (lane & 7)) * 4u, 0, at + 2 * kQ + kO);
+            }
+        };
+
+        const bool key_ok = key < range.len;
+        stage(rbeg, lds);
+        for (int t = 0; t < nt; ++t) {
+            const int r0 = rbeg + t * BM;
+            lds_byte* const cur = lds + (t & 1) * kStage;
+            tiles::wait_lds_loads();
+            __syncthreads();
+            if (t + 1 < nt) stage(r0 + BM, lds + ((t + 1) & 1) * kStage);
+            // masked: some key behind the element's last or the first row's limit, or rows behind the last
+            const bool edge = wk0 + 32 > range.limit(fast_div(r0, f.div_G)) || r0 + BM > f.R;
+            unsigned seen = 0xFFFFu;
+            if (edge) {
+                seen = 0;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int r = r0 + acc_row(e, half);
+                    if (key_ok && r < f.R && key < range.limit(fast_div(r, f.div_G))) seen |= 1u << e;
+                }
+            }
+            f32x16 dp{};
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) dp = mma(OT::row_frag(cur + 2 * kQ, 0, c, lane), vf[c], dp);
+            lds_byte* const st = cur + 2 * kQ + kO + 16 * half;
+            float w[16];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                f32x16 s{};
+#pragma unroll
+                for (int c = 0; c < D / 16; ++c) s = mma(QT::row_frag(cur + m * kQ, 0, c, lane), kf[m][c], s);
+                float ds[16];
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    lds_byte* const at = st + 8 * e;        // rows 8 (e / 4) + 4 half .. + 3
+                    const f32x4 lse = *(lds_ptr<f32x4>)(at + m * 128), tm = *(lds_ptr<f32x4>)(at + 256 + m * 128);
+                    f32x4 lam{};
+                    if (m == 1) lam = *(lds_ptr<f32x4>)(at + 512);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float p = exp2_fast(fmaf(s[e + j], f.scale, -lse[j]));
+                        if (m == 1) p *= -lam[j];
+                        ds[e + j] = p * (dp[e + j] - tm[j]);
+                        w[e + j] = m == 0 ? p : w[e + j] + p;
+                    }
+                }
+                if (edge) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (!(seen & (1u << e))) ds[e] = w[e] = 0.f;
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const Frag<T> fd = pack_frag<T>(ds + 8 * u);
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) ak[m][c] = mma(QT::col_frag(cur + m * kQ, 16 * u, c, lane), fd, ak[m][c]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const Frag<T> fw = pack_frag<T>(w + 8 * u);
+#pragma unroll
+                for (int c = 0; c < 2 * D / 32; ++c) av[c] = mma(OT::col_frag(cur + 2 * kQ, 16 * u, c, lane), fw, av[c]);
+            }
+        }
+    }
+    if (key >= f.Nk) return;
+    const long long krow = (static_cast<long long>(b) * f.Nk + key) * f.kv_heads + g;
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+                store4<T>(a.dk, (2 * krow + m) * D + 32 * c + acc_row(e, half), ak[m][c][e] * a.grad_scale,
+                          ak[m][c][e + 1] * a.grad_scale, ak[m][c][e + 2] * a.grad_scale, ak[m][c][e + 3] * a.grad_scale);
+#pragma unroll
+        for (int c = 0; c < 2 * D / 32; ++c)
+            store4<T>(a.dv, krow * (2 * D) + 32 * c + acc_row(e, half), av[c][e], av[c][e + 1], av[c][e + 2], av[c][e + 3]);
+    }
+}
+
+template <typename T, int D>
+hipError_t launch_bwd(const DiffBwdArgs& a, hipStream_t stream)
+{
+    static std::atomic<unsigned long long> configured_q{0}, configured_k{0};
+    constexpr int ES = static_cast<int>(sizeof(T)), BN = ES == 2 ? 64 : 32;
+    const long long bh = static_cast<long long>(a.f.B) * a.f.kv_heads;
+    constexpr int lpr = 2 * D * ES / 16;
+    const long long rblocks = (bh * a.Rpad * lpr + kThreads - 1) / kThreads;
+    const long long qblocks = (a.f.R + 127) / 128 * bh, kblocks = (a.f.Nk + 127) / 128 * bh;
+    if (rblocks > 0x7FFFFFFFLL || qblocks > 0x7FFFFFFFLL || kblocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    hipError_t e = set_max_lds_once(reinterpret_cast<const void*>(&diff_dq_kernel<T, D, BN>), configured_q);
+    if (e != hipSuccess) return e;
+    e = set_max_lds_once(reinterpret_cast<const void*>(&diff_dkv_kernel<T, D>), configured_k);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((diff_rows_kernel<T, D>), dim3(static_cast<unsigned>(rblocks)), dim3(kThreads), 0, stream, a);
+    if (a.lam_heads)
+        hipLaunchKernelGGL(diff_lambda_kernel, dim3(static_cast<unsigned>(a.f.heads)), dim3(1024), 0, stream, a.dlam_rows,
+                           static_cast<long long>(a.f.B) * a.f.Nq, a.dlam, a.f.lam_bf16);
+    hipLaunchKernelGGL((diff_dq_kernel<T, D, BN>), dim3(static_cast<unsigned>(qblocks)), dim3(kThreads), 2 * BN * 4 * D * ES,
+                       stream, a);
+    hipLaunchKernelGGL((diff_dkv_kernel<T, D>), dim3(static_cast<unsigned>(kblocks)), dim3(kThreads), 2 * (32 * 4 * D * ES + 1024),
+                       stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool use_bf16, hipStream_t stream)
+{
+    if (use_bf16) return d == 32 ? launch_bwd<bf16, 32>(a, stream) : launch_bwd<bf16, 64>(a, stream);
+    return d == 32 ? launch_bwd<float, 32>(a, stream) : launch_bwd<float, 64>(a, stream);
+}
+
+}  // namespace qta

@@ -1,0 +1,162 @@
+// Rotary positions: pairs of channels turned by an angle that is linear in the token's position.
+//
+//   y1 = m (x1 cos t - x2 sin t),   y2 = m (x2 cos t + x1 sin t),   t = position * freqs[pair]
+//
+// The gradient is the turn by -t. Bound by memory: every element is read and written once, so a workgroup takes
+// whole tokens, makes each (token, pair) cosine and sine once into LDS for all heads of both tensors, and then streams the
+// heads in 16-byte pieces. Angles are products in 64 bits of which only the fraction of a turn is kept: at position
+// 10^6 an fp32 product would be off by 0.06 radians, this one by 10^-9. The turn itself is in fp32, rounded once.
+#include <algorithm>
+
+#include "diff_attn.h"
+
+namespace qta {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Position of a token on an axis.
+__device__ __forceinline__ int token_position(const RotaryArgs& a, int token, int axis)
+{
+    const int b = fast_div(token, a.div_N), n = token - b * a.N;
+    if (a.pos) return a.pos[b * a.pos_b + static_cast<long long>(n) * a.axes + axis];
+    if (a.axes == 1) return a.start + n;
+    const int y = fast_div(n, a.div_W);
+    return axis == 0 ? y : n - y * a.width;
+}
+
+// V elements at p, and back.
+template <typename T, int V>
+struct Piece {
+    float x[V];
+    __device__ __forceinline__ void load(const void* base, long long e)
+    {
+        if constexpr (V * sizeof(T) == 16) {
+            Storage<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(base) + e * static_cast<long long>(sizeof(T))), x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[i] = Storage<T>::load1(base, e + i);
+        }
+    }
+    __device__ __forceinline__ void store(void* base, long long e) const
+    {
+        if constexpr (V * sizeof(T) == 16) {
+            *reinterpret_cast<uint4*>(static_cast<unsigned char*>(base) + e * static_cast<long long>(sizeof(T))) = Storage<T>::pack(x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) Storage<T>::store1(base, e + i, x[i]);
+        }
+    }
+};
+
+// An item is, in one head of one token: V pairs (half layout: two pieces of V; interleaved: one piece of V, or of one
+// pair where V = 1), or, behind the turned channels, a piece that is copied.
+template <typename T, int V, bool INTER>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
+{
+    constexpr int U = INTER && V == 1 ? 2 : V;             // elements of a turned piece
+    extern __shared__ __align__(16) float2 turn[];         // [tokens][rot / 2] (cos, sin) times m
+    const int pairs = a.rot / 2, per = pairs / a.axes;     // pairs of all axes, of one
+    const long long first = static_cast<long long>(blockIdx.x) * a.tokens;
+    const int tokens = static_cast<int>(min(static_cast<long long>(a.tokens), static_cast<long long>(a.B) * a.N - first));
+    for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
+        const int t = fast_div(i, a.div_pairs), p = i - t * pairs;
+        const double turns = token_position(a, static_cast<int>(first) + t, p >= per ? 1 : 0) * (a.freqs[p] * 0.15915494309189535);
+        const float half_turns = static_cast<float>(2.0 * (turns - rint(turns)));
+        float s, c;
+        sincospif(half_turns, &s, &c);
+        turn[i] = make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
+    }
+    __syncthreads();
+    const int heads = a.t[0].heads + a.t[1].heads, turned = INTER ? a.rot / U : pairs / V;
+    const int total = tokens * heads * a.items;
+    for (int i = threadIdx.x; i < total; i += kThreads) {
+        const int q = fast_div(i, a.div_items), it = i - q * a.items;
+        const int t = fast_div(q, a.div_heads), hh = q - t * heads;
+        const int which = hh >= a.t[0].heads ? 1 : 0, h = which ? hh - a.t[0].heads : hh;
+        const RotaryTensor& x = a.t[which];
+        const int token = static_cast<int>(first) + t, b = fast_div(token, a.div_N), n = token - b * a.N;
+        const long long from = b * x.xb + n * x.xn + h * x.xh, to = b * x.yb + n * x.yn + h * x.yh;
+        const float2* const cs = turn + t * pairs;
+        if (it >= turned) {
+            const int c = a.rot + (it - turned) * V;
+            Piece<T, V> p;
+            p.load(x.x, from + c);
+            p.store(x.y, to + c);
+        } else if constexpr (INTER) {
+            Piece<T, U> p;
+            p.load(x.x, from + it * U);
+#pragma unroll
+            for (int j = 0; j < U / 2; ++j) {
+                const float2 w = cs[it * (U / 2) + j];
+                const float u = p.x[2 * j], v = p.x[2 * j + 1];
+                p.x[2 * j] = u * w.x - v * w.y;
+                p.x[2 * j + 1] = v * w.x + u * w.y;
+            }
+            p.store(x.y, to + it * U);
+        } else {
+            const int p0 = it * V, c0 = p0 >= per ? p0 + per : p0;      // the second axis starts at channel 2 per
+            Piece<T, V> p, r;
+            p.load(x.x, from + c0);
+            r.load(x.x, from + c0 + per);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float2 w = cs[p0 + j];
+                const float u = p.x[j], v = r.x[j];
+                p.x[j] = u * w.x - v * w.y;
+                r.x[j] = v * w.x + u * w.y;
+            }
+            p.store(x.y, to + c0);
+            r.store(x.y, to + c0 + per);
+        }
+    }
+}
+
+template <typename T, int V, bool INTER>
+hipError_t launch(const RotaryArgs& a, hipStream_t stream)
+{
+    RotaryArgs p = a;
+    constexpr int U = INTER && V == 1 ? 2 : V;
+    const int pairs = a.rot / 2, heads = a.t[0].heads + a.t[1].heads;
+    p.items = (INTER ? a.rot / U : pairs / V) + (a.d - a.rot) / V;
+    // about four items a thread, and at most 32 KB of angles
+    const long long tokens = static_cast<long long>(a.B) * a.N;
+    long long take = (4LL * kThreads + heads * p.items - 1) / (heads * p.items);
+    take = std::min(take, std::max(1LL, 4096LL / std::max(pairs, 1)));
+    p.tokens = static_cast<int>(std::max(1LL, std::min(take, tokens)));
+    p.div_N = make_fastdiv(a.N);
+    p.div_W = make_fastdiv(a.width > 0 ? a.width : 1);
+    p.div_pairs = make_fastdiv(std::max(pairs, 1));
+    p.div_items = make_fastdiv(p.items);
+    p.div_heads = make_fastdiv(heads);
+    const long long blocks = (tokens + p.tokens - 1) / p.tokens;
+    hipLaunchKernelGGL((rotary_kernel<T, V, INTER>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads),
+                       static_cast<size_t>(p.tokens) * pairs * sizeof(float2), stream, p);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_type(const RotaryArgs& a, hipStream_t stream)
+{
+    // 16-byte pieces where every piece of every row starts on 16 bytes and no piece crosses a border between the
+    // halves of an axis, the axes, or the turned and the copied channels; single elements otherwise
+    constexpr int V = 16 / static_cast<int>(sizeof(T));
+    const int part = a.interleaved ? a.rot : a.rot / a.axes / 2;
+    bool wide = part % V == 0 && (a.d - a.rot) % V == 0;
+    for (const RotaryTensor& t : a.t) {
+        if (t.heads == 0) continue;
+        wide = wide && ((reinterpret_cast<uintptr_t>(t.x) | reinterpret_cast<uintptr_t>(t.y)) & 15u) == 0;
+        for (const long long s : {t.xb, t.xn, t.xh, t.yb, t.yn, t.yh}) wide = wide && s % V == 0;
+    }
+    if (a.interleaved) return wide ? launch<T, V, true>(a, stream) : launch<T, 1, true>(a, stream);
+    return wide ? launch<T, V, false>(a, stream) : launch<T, 1, false>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const RotaryArgs& a, bool use_bf16, hipStream_t stream)
+{
+    return use_bf16 ? launch_type<bf16>(a, stream) : launch_type<float>(a, stream);
+}
+
+}  // namespace qta

@@ -1,0 +1,290 @@
+"""Rotary positions and differential attention (``qta_rotary`` and ``qta_diff_attn*`` of ``include/qta.h``).
+
+Argument marshalling only, like ``qta.py``. Tokens come as sequences ``[B, N, heads, d]`` or as maps
+``[B, H, W, heads, d]`` (fp32 or bf16, on a GPU); views are taken as they are as long as the channels of a head are
+contiguous and, on a map, its rows follow each other at one distance.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+import math
+
+import torch
+
+from .qta import _DTYPES, _SIGS, _check, _dtype_code, _ptr, _scale, _stream, lib
+
+_P, _I, _F, _L = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_int64
+
+
+class RotaryTensor(ctypes.Structure):
+    _fields_ = [("x", _P), ("y", _P), ("heads", _I), ("x_batch", _L), ("x_token", _L), ("x_head", _L),
+                ("y_batch", _L), ("y_token", _L), ("y_head", _L)]
+
+
+class DiffAttnArgs(ctypes.Structure):
+    _fields_ = [("q", _P), ("k", _P), ("v", _P), ("lam", _P), ("B", _I), ("heads", _I), ("kv_heads", _I), ("Nq", _I),
+                ("Nk", _I), ("d", _I), ("dtype", _I), ("lam_dtype", _I), ("q_batch", _L), ("q_token", _L),
+                ("q_head", _L), ("k_batch", _L), ("k_token", _L), ("k_head", _L), ("v_batch", _L), ("v_token", _L),
+                ("v_head", _L), ("lam_batch", _L), ("lam_token", _L), ("lam_head", _L), ("lens", _P), ("q_pos", _P),
+                ("causal", _I), ("scale", _F)]
+
+
+_SIGS.update({
+    "qta_rotary": ([_P, _I, _I, _I, _I, _I, _I, _I, _I, _I, _I, _P, _P, _L, _I, _F, _P], _I),
+    "qta_diff_attn": ([_P, _P, _P, _P, _P], _I),
+    "qta_diff_attn_backward_workspace_bytes": ([_P], ctypes.c_size_t),
+    "qta_diff_attn_backward": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, ctypes.c_size_t, _P], _I),
+})
+
+
+def _tokens(t, name, like=None):
+    """(B, N, heads, channels, and the strides of the first three) of a sequence or a map."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a GPU")
+    if like is not None and (t.device != like.device or t.dtype != like.dtype):
+        raise ValueError(f"{name} must be {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
+    shape, st = t.shape, t.stride()
+    if len(shape) not in (4, 5):
+        raise ValueError(f"{name} must be [B, N, heads, d] or [B, H, W, heads, d], got shape {tuple(shape)}")
+    if shape[-1] > 1 and st[-1] != 1:
+        raise ValueError(f"the channels of {name} must be contiguous")
+    if len(shape) == 4:
+        N, token = shape[1], st[1]
+    else:
+        N, token = shape[1] * shape[2], st[2] if shape[2] > 1 else st[1]
+        if shape[1] > 1 and shape[2] > 1 and st[1] != shape[2] * st[2]:
+            raise ValueError(f"the rows of the map {name} must follow each other at one distance")
+    # (the stride of an axis of one entry is never taken, and may be anything)
+    return (shape[0], N, shape[-2], shape[-1], st[0] if shape[0] > 1 else 0, token if N > 1 else 0,
+            st[-2] if shape[-2] > 1 else 0)
+
+
+def _int32(t, name, like, shapes):
+    if t is None:
+        return
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor")
+    if t.dtype != torch.int32 or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous torch.int32 on {like.device}")
+    if tuple(t.shape) not in shapes:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {' or '.join(str(s) for s in shapes)}")
+
+
+def _on(t):
+    """The device of `t` made current for a call (kernels are launched on the current one)."""
+    return contextlib.nullcontext() if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
+# ------------------------------------------------------------------------------------------------
+# rotary positions
+# ------------------------------------------------------------------------------------------------
+
+def rotary_freqs(rot, *, theta=10000.0, axes=1, factor=1.0, trained=None, low=1.0, high=32.0, device=None):
+    """Frequencies for ``rotary``: fp64 ``[rot/2]``, theta^(-j/n) for the n = rot/2/axes pairs of each axis.
+
+    ``factor`` > 1 stretches the positions to a longer context: every frequency divided by it, or, with ``trained``
+    (the context length in training), only those that turn less than ``low`` times in that length; those that turn
+    more than ``high`` times stay, and between the two the change is blended linearly in the number of turns."""
+    if rot <= 0 or axes not in (1, 2) or rot % (2 * axes) != 0:
+        raise ValueError(f"rot must be a positive multiple of {2 * axes} for {axes} axes, got {rot}")
+    if theta <= 0 or factor < 1.0 or high <= low:
+        raise ValueError("theta > 0, factor >= 1 and high > low are needed")
+    n = rot // 2 // axes
+    f = float(theta) ** (-torch.arange(n, dtype=torch.float64) / n)
+    if trained is not None:
+        keep = ((f * float(trained) / (2.0 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+        f = f * (keep + (1.0 - keep) / factor)
+    else:
+        f = f / factor
+    return f.repeat(axes).to(device) if device is not None else f.repeat(axes)
+
+
+def _rotate(xs, freqs, pos, axes, interleaved, scale, start, inverse, inplace=False):
+    x = xs[0]
+    shapes = [_tokens(t, n, x) for t, n in zip(xs, ("x", "k"))]
+    B, N, _, d = shapes[0][:4]
+    for t, s in zip(xs[1:], shapes[1:]):
+        if t.shape[:-2] != x.shape[:-2] or s[3] != d:
+            raise ValueError(f"k has shape {tuple(t.shape)}, x {tuple(x.shape)}: only the heads may differ")
+    code = _dtype_code(x)
+    axes = (2 if x.dim() == 5 else 1) if axes is None else axes
+    if not isinstance(freqs, torch.Tensor):
+        raise TypeError("freqs must be a tensor")
+    if freqs.dtype != torch.float64 or freqs.device != x.device or freqs.dim() != 1 or not freqs.is_contiguous():
+        raise ValueError(f"freqs must be a contiguous torch.float64 vector on {x.device}")
+    _int32(pos, "pos", x, {(N,), (B, N)} if axes == 1 else {(N, 2), (B, N, 2)})
+    if pos is None and axes == 2 and x.dim() != 5:
+        raise ValueError("two axes need a map or given positions")
+    if pos is not None and start != 0:
+        raise ValueError("start goes with positions that are counted, not with given ones")
+    if inplace:
+        # (a broadcast axis has all its entries in one place)
+        if any(n > 1 and s == 0 for t in xs for n, s in zip(t.shape, t.stride())):
+            raise ValueError("a broadcast tensor cannot be turned in place")
+        ys = xs
+    else:
+        ys = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs]
+    if x.numel() == 0 and all(t.numel() == 0 for t in xs):
+        return ys
+    table = (RotaryTensor * len(xs))()
+    for e, t, y, s in zip(table, xs, ys, shapes):
+        o = s if inplace else _tokens(y, "y")
+        e.x, e.y, e.heads = t.data_ptr(), y.data_ptr(), s[2]
+        e.x_batch, e.x_token, e.x_head = s[4:]
+        e.y_batch, e.y_token, e.y_head = o[4:]
+    shared = pos is not None and pos.dim() == axes
+    with _on(x):
+        _check("qta_rotary", lib().qta_rotary(
+            ctypes.addressof(table), len(xs), B, N, d, 2 * freqs.numel(), axes, x.shape[2] if x.dim() == 5 else 0,
+            int(interleaved), int(inverse), code, _ptr(freqs), _ptr(pos), 0 if pos is None or shared else N * axes,
+            start, scale, _stream(x.device)))
+    return ys
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, freqs, pos, how, *xs):
+        ctx.how = how
+        ctx.save_for_backward(freqs, *([] if pos is None else [pos]))
+        return tuple(_rotate(xs, freqs, pos, *how, False))
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, *dys):
+        freqs, pos = (*ctx.saved_tensors, None)[:2]
+        return (None, None, None, *_rotate([dy.contiguous() for dy in dys], freqs, pos, *ctx.how, True))
+
+
+def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.0, start=0, inverse=False, inplace=False):
+    """Rotary positions: the first ``rot = 2 * len(freqs)`` channels of every head turned pair by pair by
+    position * freqs (fp64, radians; see ``rotary_freqs``), times ``scale``; the other channels are copied. Returns a new
+    tensor, or with ``k`` (the same tokens, its own number of heads) a pair of them from one launch. Differentiable.
+
+    ``axes``: 1, or 2 for row and column positions, the first half of the turned channels going by the row and the rest by
+    the column (the default for maps, ``[B, H, W, heads, d]``). ``pos``: int32 positions ``[N]`` or ``[B, N]``
+    (``[.., N, 2]`` for two axes, N = H*W on a map); None: ``start`` + 0, 1, .. along a sequence, the coordinates of a map.
+    ``interleaved``: pairs are neighbouring channels instead of the two halves of an axis. ``inverse``: turn back.
+    ``inplace``: overwrite x and k (and return them); not differentiable."""
+    xs = [x] if k is None else [x, k]
+    how = (axes, bool(interleaved), float(scale), int(start))
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in xs):
+        if inplace:
+            raise ValueError("in-place rotation of a tensor that requires gradients")
+        if inverse:
+            raise ValueError("inverse is for tensors that do not require gradients")
+        ys = _Rotary.apply(freqs, pos, how, *xs)
+    else:
+        ys = _rotate(xs, freqs, pos, *how, bool(inverse), bool(inplace))
+    return ys[0] if k is None else (ys[0], ys[1])
+
+
+# ------------------------------------------------------------------------------------------------
+# differential attention
+# ------------------------------------------------------------------------------------------------
+
+def _diff_args(q, k, v, lam, scale, causal, lens, q_pos):
+    """The library's arguments, and the shape of the output."""
+    B, Nq, h2, d, qb, qn, qh = _tokens(q, "q")
+    Bk, Nk, k2, dk, kb, kn, kh = _tokens(k, "k", q)
+    Bv, Nv, kv, dv, vb, vn, vh = _tokens(v, "v", q)
+    code = _dtype_code(q)
+    if h2 % 2 or k2 != 2 * kv or kv == 0 or (h2 // 2) % kv:
+        raise ValueError(f"q has {h2} and k {k2} heads and v {kv}: two for each head, and a multiple of v's, are needed")
+    if (Bk, Bv, Nv, dk, dv) != (B, B, Nk, d, 2 * d):
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
+    heads = h2 // 2
+    if not isinstance(lam, torch.Tensor):
+        raise TypeError("lam must be a tensor")
+    if lam.device != q.device or lam.dtype not in (torch.float32, q.dtype):
+        raise ValueError(f"lam must be torch.float32 or {q.dtype} on {q.device}")
+    if tuple(lam.shape) == (heads,):
+        ls = (0, 0, lam.stride(0))
+    elif lam.shape == (*q.shape[:-2], heads):
+        ls = _tokens(lam.unsqueeze(-1), "lam")[4:]
+    else:
+        raise ValueError(f"lam has shape {tuple(lam.shape)}, expected {(heads,)} or {(*q.shape[:-2], heads)}")
+    _int32(lens, "lens", q, {(B,)})
+    _int32(q_pos, "q_pos", q, {(B,)})
+    if q_pos is not None and not causal:
+        raise ValueError("q_pos goes with causal=True")
+    ptr = lambda t: None if t is None else t.data_ptr()
+    args = DiffAttnArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(), B, heads, kv, Nq, Nk, d, code,
+                        _DTYPES[lam.dtype], qb, qn, qh, kb, kn, kh, vb, vn, vh, *ls, ptr(lens), ptr(q_pos),
+                        int(bool(causal)), _scale(scale))
+    return args, (*q.shape[:-2], heads, 2 * d)
+
+
+def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, keep=False):
+    """Differential attention, ``softmax(scale q0 k0^T) v - lam softmax(scale q1 k1^T) v`` for every head, the maps of
+    head i being q's heads 2i and 2i + 1. q ``[B, Nq, 2*heads, d]``, k ``[B, Nk, 2*kv_heads, d]``, v
+    ``[B, Nk, kv_heads, 2*d]`` (or maps ``[B, H, W, ..]``), d 32 or 64, heads a multiple of kv_heads; ``lam`` ``[heads]``
+    or one for every token ``[B, Nq, heads]``, fp32 or q's type. Returns ``[B, Nq, heads, 2*d]``.
+
+    ``lens`` (int32 ``[B]``): keys of each batch element; what lies behind them is never used, so k and v may be the
+    whole of a cache. ``causal``: query i sees the keys up to position ``q_pos[b] + i`` (int32 ``[B]``; None: the
+    queries are the last Nq of Nk tokens). A row that sees no key gives 0. ``scale``: None for 1/sqrt(d).
+    ``keep``: also return what ``diff_attn_backward`` needs."""
+    args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
+    out = torch.empty(shape, dtype=q.dtype, device=q.device)
+    out1 = lse = None
+    if keep:
+        out1 = torch.empty_like(out)
+        lse = torch.empty((args.B, args.heads, 2, args.Nq), dtype=torch.float32, device=q.device)
+    if out.numel() == 0 or args.Nk == 0:
+        out.zero_()
+        if keep:
+            out1.zero_()
+            lse.fill_(-math.inf)
+    else:
+        with _on(q):
+            _check("qta_diff_attn", lib().qta_diff_attn(ctypes.byref(args), _ptr(out), _ptr(out1), _ptr(lse),
+                                                        _stream(q.device)))
+    return (out, (out1, lse)) if keep else out
+
+
+def diff_attn_backward(q, k, v, lam, out, kept, dout, *, scale=None, causal=False, lens=None, q_pos=None):
+    """Gradients (dq, dk, dv, dlam) of ``diff_attn(.., keep=True)`` for the upstream gradient ``dout``, each in the
+    shape and type of its input; ``out`` and ``kept`` are what that call returned, the other arguments the same."""
+    args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
+    out1, lse = kept
+    for t, n in ((out, "out"), (out1, "kept"), (dout, "dout")):
+        if t.dtype != q.dtype or t.device != q.device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+            raise ValueError(f"{n} must be contiguous {q.dtype} {tuple(shape)} on {q.device}")
+    if tuple(lse.shape) != (args.B, args.heads, 2, args.Nq) or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise ValueError("kept is not what diff_attn returned for these shapes")
+    grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v, lam)]
+    if out.numel() == 0 or args.Nk == 0:
+        return tuple(g.zero_() for g in grads)
+    ws = torch.empty(lib().qta_diff_attn_backward_workspace_bytes(ctypes.byref(args)), dtype=torch.uint8, device=q.device)
+    with _on(q):
+        _check("qta_diff_attn_backward", lib().qta_diff_attn_backward(
+            ctypes.byref(args), _ptr(out), _ptr(out1), _ptr(lse), _ptr(dout), *[_ptr(g) for g in grads],
+            int(lam.dim() == 1), _ptr(ws), ws.numel(), _stream(q.device)))
+    return tuple(grads)
+
+
+class _DiffAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, lam, scale, causal, lens, q_pos):
+        out, (out1, lse) = diff_attn(q, k, v, lam, scale=scale, causal=causal, lens=lens, q_pos=q_pos, keep=True)
+        ctx.how = (scale, causal)
+        ctx.save_for_backward(q, k, v, lam, out, out1, lse, lens, q_pos)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        q, k, v, lam, out, out1, lse, lens, q_pos = ctx.saved_tensors
+        dout = dout.contiguous()
+        if dout.data_ptr() % 16:
+            dout = dout.clone()
+        return (*diff_attn_backward(q, k, v, lam, out, (out1, lse), dout, scale=ctx.how[0], causal=ctx.how[1], lens=lens,
+                                    q_pos=q_pos), None, None, None, None)
+
+
+def diff_attention(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None):
+    """Differentiable ``diff_attn``: gradients of q, k, v and lam."""
+    return _DiffAttention.apply(q, k, v, lam, scale, causal, lens, q_pos)

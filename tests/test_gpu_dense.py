@@ -1,0 +1,497 @@
+"""Rotary positions and differential attention on the GPU against tests/dense_ref.py's 64-bit values and its bounds
+(element by element: |gpu - ref| <= bound)."""
+import math
+import sys
+
+import pytest
+import torch
+
+import paper_2201_02767_amd as P
+from tests import dense_ref as R
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU")
+    P.lib()
+    return torch.device("cuda:0")
+
+
+def announce(msg):
+    print(f"[gpu case] {msg}", file=sys.stderr, flush=True)
+
+
+def within(name, got, ref):
+    """Every element within its bound; prints how much of it is used."""
+    value, bound = ref
+    assert got.shape == value.shape, (name, got.shape, value.shape)
+    off = (got.double() - value).abs()
+    worst = float((off / bound.clamp(min=1e-30)).max()) if off.numel() else 0.0
+    print(f"{name}: {worst:.3f} of the bound", file=sys.stderr)
+    assert bool(torch.isfinite(got.double()).all()), name
+    assert bool((off <= bound).all()), f"{name}: {worst} times the bound"
+
+
+def gen(seed, dev):
+    g = torch.Generator(device=dev)
+    g.manual_seed(seed)
+    return lambda *s: torch.randn(*s, generator=g, device=dev)
+
+
+def make(dev, B, Nq, Nk, heads, kv, d, dtype, seed=0, token_lam=False, lam_dtype=None, gain=1.3):
+    r = gen(seed, dev)
+    dt = DT[dtype]
+    q, k, v = (gain * r(B, Nq, 2 * heads, d)).to(dt), r(B, Nk, 2 * kv, d).to(dt), r(B, Nk, kv, 2 * d).to(dt)
+    lam = (0.5 + 0.3 * (r(B, Nq, heads) if token_lam else r(heads))).to(lam_dtype or torch.float32)
+    return q, k, v, lam, r(B, Nq, heads, 2 * d).to(dt)
+
+
+def i32(x, dev):
+    return None if x is None else torch.tensor(x, dtype=torch.int32, device=dev)
+
+
+def check(dev, q, k, v, lam, dout, *, label="", grads=True, ref_kv=None, **how):
+    """The forward, and with grads the forward that keeps its sums and the backward, against the reference."""
+    announce(f"diff_attn {label} q {tuple(q.shape)} k {tuple(k.shape)} lam {tuple(lam.shape)} {q.dtype} {how}")
+    how = {n: (i32(x, dev) if n in ("lens", "q_pos") else x) for n, x in how.items()}
+    rk, rv = ref_kv or (k, v)
+    ref = R.diff_attention(q, rk, rv, lam, dout=dout if grads else None, **how)
+    out = P.diff_attn(q, k, v, lam, **how)
+    torch.cuda.synchronize()
+    within("out", out, ref["out"])
+    if not grads:
+        return out
+    out2, kept = P.diff_attn(q, k, v, lam, keep=True, **how)
+    got = P.diff_attn_backward(q, k, v, lam, out2, kept, dout, **how)
+    torch.cuda.synchronize()
+    within("out (kept)", out2, ref["out"])
+    for n, t in zip(("dq", "dk", "dv", "dlam"), got):
+        within(n, t, ref[n])
+    return out
+
+
+# ---- differential attention ----
+
+SHAPES = [  # B, Nq, Nk, heads, kv_heads
+    (1, 1, 1, 1, 1), (2, 1, 64, 2, 1), (1, 3, 65, 4, 4), (2, 32, 32, 2, 2), (1, 63, 127, 2, 1), (1, 130, 129, 3, 1),
+    (1, 257, 200, 4, 2), (3, 100, 31, 2, 2), (1, 1, 1000, 8, 2), (1, 5, 700, 8, 1), (1, 300, 2, 1, 1),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 64])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_diff_attn_sizes(dev, shape, d, dtype):
+    check(dev, *make(dev, *shape, d, dtype, seed=sum(shape)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 64])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1, 1), (2, 77, 77, 4, 2), (1, 200, 200, 2, 2), (2, 5, 141, 8, 2),
+                                   (1, 40, 300, 2, 1), (1, 140, 60, 2, 1)], ids=lambda s: "x".join(map(str, s)))
+def test_diff_attn_causal(dev, shape, d, dtype):
+    """Nq < Nk: the last queries; Nq > Nk: the first rows see nothing."""
+    check(dev, *make(dev, *shape, d, dtype, seed=7), causal=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("token_lam", [False, True])
+def test_diff_attn_lengths(dev, dtype, token_lam):
+    """Lengths of zero, one, in the middle of a tile, on its border, all, and beyond (clamped)."""
+    lens = [0, 1, 63, 64, 65, 150, 999, -3]
+    check(dev, *make(dev, 8, 37, 150, 4, 2, 64, dtype, seed=3, token_lam=token_lam), lens=lens)
+    check(dev, *make(dev, 8, 150, 150, 2, 2, 32, dtype, seed=4, token_lam=token_lam), lens=lens, causal=True, q_pos=[0] * 8)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_diff_attn_query_positions(dev, dtype):
+    """Queries at given places, some before the first key, some behind the last."""
+    args = make(dev, 6, 9, 200, 4, 1, 32, dtype, seed=5)
+    check(dev, *args, causal=True, q_pos=[-9, -8, -3, 100, 191, 2 ** 31 - 1])
+    check(dev, *args, causal=True, lens=[3, 0, 50, 105, 200, 64], q_pos=[-2 ** 31, 0, 41, 96, 191, 55])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_what_lies_behind_the_lengths_is_not_used(dev, dtype):
+    q, k, v, lam, do = make(dev, 3, 20, 190, 4, 2, 64, dtype, seed=6)
+    lens = [0, 70, 128]
+    rk, rv = k.clone(), v.clone()
+    for b, n in enumerate(lens):
+        k[b, n:], v[b, n:] = math.nan, math.inf
+    check(dev, q, k, v, lam, do, lens=lens, ref_kv=(rk, rv))
+    # no query of the causal call sees the last keys either
+    check(dev, q, k, v, lam, do, lens=[0, 70, 128], causal=True, q_pos=[0, 50, 108], ref_kv=(rk, rv))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_diff_attn_weights(dev, dtype):
+    """lambda zero, negative and large; in both types; a negative zero length of nothing."""
+    q, k, v, _, do = make(dev, 2, 33, 90, 4, 2, 32, dtype, seed=8)
+    for lam in ([0.0, -0.7, 3.0, 1.0], [-0.0, 1e-30, -2.5, 0.25]):
+        lam = torch.tensor(lam, device=dev)
+        check(dev, q, k, v, lam, do)
+        if dtype == "bf16":
+            check(dev, q, k, v, lam.bfloat16(), do)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_diff_attn_large_logits(dev, dtype):
+    """One key takes nearly all the weight; logits in the hundreds, rising along the keys so that maxima keep moving."""
+    q, k, v, lam, do = make(dev, 1, 40, 300, 2, 1, 32, dtype, seed=9, gain=2.0)
+    k = (k.float() * torch.linspace(0.1, 12.0, 300, device=dev)[None, :, None, None]).to(k.dtype)
+    check(dev, q, k, v, lam, do)
+    check(dev, q, k.flip(1).contiguous(), v, lam, do)
+    check(dev, q, k, v, lam, do, scale=0.01)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_diff_attn_views(dev, dtype):
+    """q, k and v as parts of one projection, keys in another order of axes, a broadcast batch, strided weights."""
+    B, N, h, d = 2, 70, 2, 32
+    r = gen(11, dev)
+    fused = r(B, N, 6 * h, d).to(DT[dtype])                    # 2h of q, 2h of k, 2h*d of v
+    q, k, v = fused[:, :, :2 * h], fused[:, :, 2 * h:4 * h], fused[:, :, 4 * h:].unflatten(2, (h, 2)).flatten(3)
+    assert v.data_ptr() == fused[:, :, 4 * h:].data_ptr()
+    lam = (0.5 + 0.1 * r(B, h, N)).transpose(1, 2)
+    do = r(B, N, h, 2 * d).to(DT[dtype])
+    check(dev, q, k, v, lam, do)
+    kt = r(B, 2 * h, N, d).to(DT[dtype]).transpose(1, 2)       # heads before tokens
+    check(dev, q, kt, v, lam, do, causal=True)
+    ke, ve = k[:1].expand(B, -1, -1, -1), v[:, :1].expand(-1, N, -1, -1)
+    check(dev, q, ke, ve, lam[:, :1].expand(-1, N, -1), do)
+
+
+def test_diff_attn_maps(dev):
+    """Maps [B, H, W, ..] are the sequences of their tokens."""
+    r = gen(12, dev)
+    q, k, v = r(2, 5, 7, 4, 32), r(2, 6, 9, 2, 32), r(2, 6, 9, 1, 64)
+    lam, do = r(2, 5, 7, 2), r(2, 5, 7, 2, 64)
+    out, kept = P.diff_attn(q, k, v, lam, keep=True)
+    got = P.diff_attn_backward(q, k, v, lam, out, kept, do)
+    fl = lambda t: t.flatten(1, 2)
+    ref = R.diff_attention(fl(q), fl(k), fl(v), fl(lam), dout=fl(do))
+    within("out", fl(out), ref["out"])
+    for n, t, x in zip(("dq", "dk", "dv", "dlam"), got, (q, k, v, lam)):
+        assert t.shape == x.shape
+        within(n, fl(t), ref[n])
+
+
+def test_diff_attn_far_offsets(dev):
+    """Token strides that take offsets past 32 bits, in a cache and within a batch."""
+    Nk, step = 5000, 1 << 19
+    store = torch.empty(Nk * step + 256, dtype=torch.bfloat16, device=dev)
+    k = store.as_strided((1, Nk, 2, 64), (0, step, 64, 1))
+    v = store[128:].as_strided((1, Nk, 1, 128), (0, step, 128, 1))
+    q, k0, v0, lam, do = make(dev, 1, 3, Nk, 1, 1, 64, "bf16", seed=13)
+    k.copy_(k0)
+    v.copy_(v0)
+    check(dev, q, k, v, lam, do, ref_kv=(k0, v0), lens=[4999])
+
+
+@pytest.mark.parametrize("shape", [(1, 2, 5000, 2, 1), (2, 700, 700, 8, 1), (1, 3000, 40, 2, 2), (4, 1, 3000, 16, 2)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_diff_attn_long(dev, shape, dtype):
+    check(dev, *make(dev, *shape, 64, dtype, seed=14))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_diff_attn_runs_are_identical(dev, dtype):
+    q, k, v, lam, do = make(dev, 2, 150, 300, 8, 2, 64, dtype, seed=15)
+    one = None
+    for _ in range(3):
+        out, kept = P.diff_attn(q, k, v, lam, keep=True)
+        now = (out, P.diff_attn(q, k, v, lam), *kept, *P.diff_attn_backward(q, k, v, lam, out, kept, do))
+        if one is None:
+            one = [t.clone() for t in now]
+            assert torch.equal(now[0], now[1])
+        assert all(torch.equal(a, b) for a, b in zip(one, now))
+
+
+def test_diff_attn_against_differences(dev):
+    """The gradients against central differences of the 64-bit function along random directions."""
+    q, k, v, lam, do = make(dev, 1, 12, 20, 2, 1, 32, "f32", seed=16)
+    out, kept = P.diff_attn(q, k, v, lam, keep=True, causal=True)
+    got = P.diff_attn_backward(q, k, v, lam, out, kept, do, causal=True)
+    r = gen(17, dev)
+    base = [t.double() for t in (q, k, v, lam)]
+    f = lambda a: float((R.diff_attention(*a, causal=True)["out"][0] * do.double()).sum())
+    for i, g in enumerate(got):
+        for _ in range(3):
+            step = r(*g.shape).double()
+            eps = 1e-5
+            num = (f([t + eps * step if j == i else t for j, t in enumerate(base)]) -
+                   f([t - eps * step if j == i else t for j, t in enumerate(base)])) / (2 * eps)
+            ana = float((g.double() * step).sum())
+            # the difference's own error is eps^2 of third derivatives and 1e-16 / eps; the kernel's is fp32 sums
+            assert abs(num - ana) <= 1e-5 * float((g.double() * step).abs().sum()) + 1e-6, (i, num, ana)
+
+
+# ---- rotary positions ----
+
+ROTARY = [  # B, N, heads, k_heads, d, rot
+    (1, 1, 1, 0, 2, 2), (2, 1, 16, 4, 64, 64), (1, 37, 3, 2, 80, 40), (2, 19, 5, 1, 64, 32), (1, 300, 4, 4, 32, 32),
+    (3, 7, 2, 1, 33, 6), (1, 65, 1, 1, 256, 256), (1, 1000, 8, 2, 128, 64), (1, 3, 130, 2, 128, 128), (1, 5, 1, 0, 4096, 4096),
+]
+
+
+def pos_of(pos, B, N, axes, dev, start=0):
+    if pos is None:
+        return (start + torch.arange(N, device=dev))[None, :, None]
+    return (pos if pos.dim() > axes else pos[None]).reshape(-1, N, axes)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("shape", ROTARY, ids=lambda s: "x".join(map(str, s)))
+def test_rotary(dev, shape, interleaved, dtype):
+    B, N, heads, kh, d, rot = shape
+    announce(f"rotary {shape} {interleaved} {dtype}")
+    r = gen(21, dev)
+    x = r(B, N, heads, d).to(DT[dtype])
+    k = r(B, N, kh, d).to(DT[dtype]) if kh else None
+    freqs = P.rotary_freqs(rot, device=dev)
+    far = torch.randint(-1000000, 1000000, (B, N), generator=torch.Generator().manual_seed(5)).to(torch.int32).to(dev)
+    for pos, start in ((None, 0), (None, 12345), (far, 0), (far[0].contiguous(), 0)):
+        got = P.rotary(x, freqs, k=k, pos=pos, start=start, interleaved=interleaved, scale=1.25)
+        p = pos_of(pos, B, N, 1, dev, start)
+        for n, t, y in (("x", x, got[0] if kh else got), *([("k", k, got[1])] if kh else [])):
+            ref = R.rotary(t, freqs, p, interleaved=interleaved, scale=1.25)
+            within(n, y, ref)
+            assert torch.equal(y[..., rot:], t[..., rot:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("H,W,d,rot", [(5, 7, 32, 32), (1, 40, 64, 64), (9, 1, 64, 32), (3, 4, 32, 4)])
+def test_rotary_maps(dev, H, W, d, rot, interleaved, dtype):
+    r = gen(22, dev)
+    x, k = r(2, H, W, 3, d).to(DT[dtype]), r(2, H, W, 2, d).to(DT[dtype])
+    freqs = P.rotary_freqs(rot, axes=2, theta=100.0, device=dev)
+    i = torch.arange(H * W, device=dev)
+    p = torch.stack((i // W, i % W), -1)[None]
+    for got in (P.rotary(x, freqs, k=k, interleaved=interleaved),
+                P.rotary(x, freqs, k=k, interleaved=interleaved, pos=p[0].to(torch.int32).contiguous()),
+                P.rotary(x, freqs, k=k, interleaved=interleaved, pos=p.expand(2, -1, -1).to(torch.int32).contiguous())):
+        for t, y in zip((x, k), got):
+            assert y.shape == t.shape
+            v, e = R.rotary(t.flatten(1, 2), freqs, p, interleaved=interleaved)
+            within("map", y.flatten(1, 2), (v, e))
+    # one axis over the tokens of a map
+    f1 = P.rotary_freqs(rot, device=dev)
+    within("one axis", P.rotary(x, f1, axes=1).flatten(1, 2), R.rotary(x.flatten(1, 2), f1, i[None, :, None]))
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotary_views_and_in_place(dev, interleaved):
+    """Parts of one projection, heads before tokens, tensors that start off 16 bytes; in place gives the same bits."""
+    r = gen(23, dev)
+    for dtype in (torch.float32, torch.bfloat16):
+        fused = r(2, 11, 7, 64).to(dtype)
+        odd = r(2 * 11 * 3 * 64 + 1).to(dtype)[1:].view(2, 11, 3, 64)
+        turned = r(2, 3, 11, 64).to(dtype).transpose(1, 2)
+        freqs = P.rotary_freqs(48, device=dev)
+        p = torch.arange(11, device=dev)[None, :, None]
+        for x, k in ((fused[:, :, :4], fused[:, :, 4:]), (odd, turned), (turned, odd), (fused[:, :, :1], odd)):
+            rx, rk = (R.rotary(t, freqs, p, interleaved=interleaved) for t in (x, k))
+            y, z = P.rotary(x, freqs, k=k, interleaved=interleaved)
+            within("x", y, rx)
+            within("k", z, rk)
+            y2, z2 = P.rotary(x, freqs, k=k, interleaved=interleaved, inplace=True)
+            assert y2.data_ptr() == x.data_ptr() and torch.equal(y2, y) and torch.equal(z2, z)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rotary_gradient(dev, dtype):
+    """The gradient is the turn back: against the reference, and <dy, R x> = <R^T dy, x>."""
+    r = gen(24, dev)
+    x, k = r(2, 9, 4, 64).to(DT[dtype]).requires_grad_(), r(2, 9, 2, 64).to(DT[dtype]).requires_grad_()
+    freqs = P.rotary_freqs(32, device=dev)
+    pos = torch.arange(18, dtype=torch.int32, device=dev).view(2, 9) * 1001
+    y, z = P.rotary(x, freqs, k=k, pos=pos, scale=0.7)
+    dy, dz = torch.randn_like(y), torch.randn_like(z)
+    gx, gk = torch.autograd.grad((y, z), (x, k), (dy, dz))
+    p = pos[..., None]
+    for g, d_ in ((gx, dy), (gk, dz)):
+        ref = R.rotary(d_, freqs, p, scale=0.7, inverse=True)
+        within("gradient", g, ref)
+        assert torch.equal(P.rotary(d_, freqs, pos=pos, scale=0.7, inverse=True), g)
+    if dtype == "f32":
+        assert abs(float((dy.double() * y.detach().double()).sum() - (gx.double() * x.detach().double()).sum())) < 1e-4
+    # one of the two alone, and a gradient that comes expanded
+    y, z = P.rotary(x, freqs, k=k.detach(), pos=pos, scale=0.7)
+    g, = torch.autograd.grad(y.sum(), (x,))
+    within("ones", g, R.rotary(torch.ones_like(x), freqs, p, scale=0.7, inverse=True))
+
+
+# ---- together, as they are used ----
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rotary_then_differential_attention(dev, dtype):
+    """A causal layer's pass: positions, attention, and the gradients back through both."""
+    r = gen(31, dev)
+    B, N, h, kv, d = 2, 90, 4, 2, 32
+    q = r(B, N, 2 * h, d).to(DT[dtype]).requires_grad_()
+    k = r(B, N, 2 * kv, d).to(DT[dtype]).requires_grad_()
+    v = r(B, N, kv, 2 * d).to(DT[dtype]).requires_grad_()
+    lam = (0.5 + 0.1 * r(h)).requires_grad_()
+    do = r(B, N, h, 2 * d).to(DT[dtype])
+    freqs = P.rotary_freqs(d, device=dev)
+    qr, kr = P.rotary(q, freqs, k=k)
+    out = P.diff_attention(qr, kr, v, lam, causal=True)
+    got = torch.autograd.grad(out, (q, k, v, lam, qr, kr), do)
+    ref = R.diff_attention(qr.detach(), kr.detach(), v.detach(), lam.detach(), causal=True, dout=do)
+    within("out", out.detach(), ref["out"])
+    for n, t in zip(("dv", "dlam", "dq", "dk"), got[2:]):
+        within(n, t, ref[n])
+    p = torch.arange(N, device=dev)[None, :, None]
+    for t, up in ((got[0], got[4]), (got[1], got[5])):
+        within("turned back", t, R.rotary(up, freqs, p, inverse=True))
+
+
+def test_serving_a_cache_token_by_token(dev):
+    """Tokens appended one at a time to a cache give the rows of the causal pass over all of them."""
+    r = gen(32, dev)
+    B, N, h, kv, d = 2, 40, 4, 1, 64
+    q, k = r(B, N, 2 * h, d).bfloat16(), r(B, N, 2 * kv, d).bfloat16()
+    v, lam = r(B, N, kv, 2 * d).bfloat16(), 0.5 + 0.1 * r(h)
+    freqs = P.rotary_freqs(d, device=dev)
+    qr, kr = P.rotary(q, freqs, k=k)
+    whole = R.diff_attention(qr, kr, v, lam, causal=True)["out"]
+    kc = torch.full((B, 64, 2 * kv, d), math.nan, dtype=torch.bfloat16, device=dev)
+    vc = torch.full((B, 64, kv, 2 * d), math.nan, dtype=torch.bfloat16, device=dev)
+    for t in range(N):
+        pos = torch.full((B, 1), t, dtype=torch.int32, device=dev)
+        qt, kt = P.rotary(q[:, t:t + 1], freqs, k=k[:, t:t + 1], pos=pos)
+        assert torch.equal(qt, qr[:, t:t + 1]) and torch.equal(kt, kr[:, t:t + 1])
+        kc[:, t], vc[:, t] = kt[:, 0], v[:, t]
+        out = P.diff_attn(qt, kc, vc, lam, lens=torch.full((B,), t + 1, dtype=torch.int32, device=dev))
+        within(f"token {t}", out, tuple(x[:, t:t + 1] for x in whole))
+
+
+def test_rotary_before_quadtree_attention(dev):
+    """On a map, row and column positions of q and k feed the QuadTree layer, and gradients come back through both."""
+    r = gen(33, dev)
+    q, k, v = (r(1, 16, 16, 2, 32).requires_grad_() for _ in range(3))
+    freqs = P.rotary_freqs(32, axes=2, theta=100.0, device=dev)
+    qr, kr = P.rotary(q, freqs, k=k)
+    out = P.attention(qr, kr, v, levels=3, K=4, variant="B", w=torch.full((1, 256, 2, 3), 1 / 3, device=dev))
+    do = r(1, 16, 16, 2, 32)
+    dq, dqr = torch.autograd.grad(out, (q, qr), do)
+    assert torch.equal(out.detach(), P.forward(qr.detach(), kr.detach(), v.detach(), levels=3, K=4, variant="B",
+                                               w=torch.full((1, 256, 2, 3), 1 / 3, device=dev)))
+    i = torch.arange(256, device=dev)
+    p = torch.stack((i // 16, i % 16), -1)[None]
+    within("dq", dq.flatten(1, 2), R.rotary(dqr.flatten(1, 2), freqs, p, inverse=True))
+
+
+# ---- streams, graphs ----
+
+def test_dense_on_another_stream(dev):
+    q, k, v, lam, do = make(dev, 1, 200, 500, 4, 2, 64, "bf16", seed=41)
+    out, kept = P.diff_attn(q, k, v, lam, keep=True)
+    want = [out, *P.diff_attn_backward(q, k, v, lam, out, kept, do)]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        out, kept = P.diff_attn(q, k, v, lam, keep=True)
+        got = [out, *P.diff_attn_backward(q, k, v, lam, out, kept, do)]
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_dense_calls_in_a_graph(dev):
+    """Positions, forward and backward captured once and replayed on new inputs, eager work in between."""
+    q, k, v, lam, do = make(dev, 2, 70, 260, 4, 2, 64, "bf16", seed=42)
+    lens = i32([200, 260], dev)
+    freqs = P.rotary_freqs(64, device=dev)
+
+    def step():
+        qr = P.rotary(q, freqs)
+        kr = P.rotary(k, freqs)
+        out, kept = P.diff_attn(qr, kr, v, lam, lens=lens, keep=True)
+        return [out, *P.diff_attn_backward(qr, kr, v, lam, out, kept, do, lens=lens)]
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        held = step()
+    r = gen(43, dev)
+    for n in ([260, 1], [0, 64], [100, 259]):
+        for t in (q, k, v, do):
+            t.copy_(r(*t.shape))
+        lens.copy_(i32(n, dev))
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, held))
+
+
+# ---- refusals of the binding ----
+
+def test_dense_refusals(dev):
+    q, k, v, lam, do = make(dev, 2, 8, 12, 4, 2, 32, "f32")
+    bad = lambda e, *a, **w: pytest.raises(e, P.diff_attn, *a, **w)
+    bad(ValueError, q, k.bfloat16(), v, lam)
+    bad(ValueError, q, k, v.cpu(), lam)
+    bad(ValueError, q[:, :, :7], k, v, lam)                    # an odd number of maps
+    bad(ValueError, q, k[:, :, :3], v, lam)
+    bad(ValueError, q[:, :, :6], k, v, lam[:3])                # 3 heads over 2
+    bad(ValueError, q, k[:, :11], v, lam)
+    bad(ValueError, q, k, v[..., :32], lam)
+    bad(ValueError, q, k, v, lam[:3])
+    bad(ValueError, q, k, v, lam.double())
+    bad(ValueError, q, k, v, lam.bfloat16())
+    bad(ValueError, q, k, v, lam, lens=torch.zeros(2, device=dev))
+    bad(ValueError, q, k, v, lam, lens=torch.zeros(3, dtype=torch.int32, device=dev))
+    bad(ValueError, q, k, v, lam, q_pos=torch.zeros(2, dtype=torch.int32, device=dev))
+    bad(ValueError, q.half(), k.half(), v.half(), lam)
+    bad(ValueError, q.transpose(2, 3).contiguous().transpose(2, 3), k, v, lam)
+    bad(TypeError, q, k, None, lam)
+    with pytest.raises(P.QtaError):                            # d = 16
+        P.diff_attn(q[..., :16].contiguous(), k[..., :16].contiguous(), v[..., :32].contiguous(), lam)
+    with pytest.raises(P.QtaError):                            # tokens off 16 bytes
+        P.diff_attn(torch.zeros(2 * 8 * 8 * 32 + 1, device=dev)[1:].view(2, 8, 8, 32), k, v, lam)
+    out, kept = P.diff_attn(q, k, v, lam, keep=True)
+    with pytest.raises(ValueError):
+        P.diff_attn_backward(q, k, v, lam, out, kept, do.transpose(1, 2).contiguous().transpose(1, 2))
+    with pytest.raises(ValueError):
+        P.diff_attn_backward(q, k, v, lam, out, (kept[0], kept[1][:, :2]), do)
+    x, f = q, P.rotary_freqs(32, device=dev)
+    badr = lambda *a, **w: pytest.raises((ValueError, P.QtaError), P.rotary, *a, **w)
+    badr(x, f.float())
+    badr(x, P.rotary_freqs(32))
+    badr(x, P.rotary_freqs(34, device=dev))
+    badr(x, f[:0])
+    badr(x, f, axes=2)
+    badr(x, f, pos=torch.zeros(2, 8, device=dev))
+    badr(x, f, pos=torch.zeros(2, 9, dtype=torch.int32, device=dev))
+    badr(x, f, pos=torch.zeros(2, 8, dtype=torch.int32, device=dev), start=1)
+    badr(x, f, k=k)
+    badr(x, f, start=2 ** 31 - 4)
+    badr(x[:, :1].expand(-1, 8, -1, -1), f, inplace=True)
+    badr(x.clone().requires_grad_(), f, inplace=True)
+
+
+def test_dense_empty(dev):
+    """No queries, no batch, no keys: empty results, zeros, and zero gradients."""
+    q, k, v, lam, do = make(dev, 2, 8, 12, 4, 2, 32, "f32")
+    assert P.diff_attn(q[:, :0], k, v, lam).shape == (2, 0, 4, 64)
+    assert P.diff_attn(q[:0], k[:0], v[:0], lam).shape == (0, 8, 4, 64)
+    out, kept = P.diff_attn(q, k[:, :0], v[:, :0], lam, keep=True)
+    assert float(out.abs().max()) == 0.0
+    grads = P.diff_attn_backward(q, k[:, :0], v[:, :0], lam, out, kept, do)
+    assert [g.shape for g in grads] == [q.shape, (2, 0, 4, 32), (2, 0, 2, 64), lam.shape]
+    assert float(grads[0].abs().max()) == 0.0 and float(grads[3].abs().max()) == 0.0
+    grads = P.diff_attn_backward(q[:, :0], k, v, lam, out[:, :0], (kept[0][:, :0], kept[1][..., :0]), do[:, :0])
+    assert float(grads[1].abs().max()) == 0.0 and float(grads[2].abs().max()) == 0.0
+    assert P.rotary(q[:, :0], P.rotary_freqs(32, device=dev)).shape == (2, 0, 8, 32)
