@@ -79,8 +79,8 @@ DiffArgs make_args(const qta_diff_attn_args* a)
 
 // Regions of the backward's workspace.
 struct BwdLayout {
-    size_t stats, dlam_rows, total;
-    int Rpad;
+    size_t stats, dlam_rows, part, total;
+    int Rpad, splits;
 };
 BwdLayout bwd_layout(const qta_diff_attn_args* a, bool lam_heads)
 {
@@ -90,6 +90,9 @@ BwdLayout bwd_layout(const qta_diff_attn_args* a, bool lam_heads)
     size_t off = align_up(static_cast<size_t>(a->B) * a->kv_heads * kDiffStats * L.Rpad * sizeof(float));
     L.dlam_rows = off;
     if (lam_heads) off = align_up(off + static_cast<size_t>(a->B) * a->heads * a->Nq * sizeof(float));
+    L.splits = diff_key_splits(a->B, a->kv_heads, a->Nk, R, a->causal != 0);
+    L.part = off;
+    if (L.splits > 1) off = align_up(off + static_cast<size_t>(L.splits) * a->B * a->Nk * a->kv_heads * 4 * a->d * sizeof(float));
     L.total = off;
     return L;
 }
@@ -142,6 +145,8 @@ qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const void* ou
     a.lam_heads = dlam_heads != 0;
     a.dlam_rows = reinterpret_cast<float*>(ws + L.dlam_rows);
     a.grad_scale = a.f.scale * kDiffLn2;
+    a.splits = L.splits;
+    a.part = reinterpret_cast<float*>(ws + L.part);
     return launch_diff_bwd(a, args->d, args->dtype == QTA_BF16, static_cast<hipStream_t>(stream)) == hipSuccess ? QTA_OK : QTA_ERR_HIP;
 }
 

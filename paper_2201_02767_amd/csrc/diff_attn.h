@@ -125,6 +125,14 @@ __device__ __forceinline__ Frag<T> pack_frag(const float* x)
     return f;
 }
 
+// LDS at a byte address.
+template <typename V>
+__device__ __forceinline__ lds_ptr<V> lds_at(uint32_t at)
+{
+    return (lds_ptr<V>)static_cast<uintptr_t>(at);
+}
+__device__ __forceinline__ uint32_t lds_address(lds_byte* p) { return static_cast<uint32_t>((uintptr_t)p); }
+
 // A tile of rows of W elements in LDS, in 16-byte chunks: chunk c of row r lies at place c ^ swz(r) of its row. The
 // swizzle spreads both ways of reading over all banks: 16 lanes on one chunk of 16 rows (row_frag), and for bf16 four
 // rows times 64 bytes (col_frag, transposed by the read). fp32 column reads meet two to a bank where a row is 128 bytes,
@@ -135,7 +143,8 @@ struct Tile {
     static constexpr int kChunks = kRow / 16;              // 4, 8, 16 or 32
     static constexpr int bytes(int rows) { return rows * kRow; }
 
-    __device__ static __forceinline__ int swz(int r)
+    // (the exclusive or of the swizzles of two rows whose bits do not overlap is that of their sum)
+    __device__ static __forceinline__ constexpr int swz(int r)
     {
         if constexpr (kChunks == 4) return (r >> 2) & 3;
         else if constexpr (kChunks == 8) return ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1 | ((r >> 3) & 1);
@@ -160,46 +169,67 @@ struct Tile {
         }
     }
 
-    // Row r0 + (lane & 31), elements 16 step + 8 (lane >> 5) .. + 7.
-    __device__ static __forceinline__ Frag<T> row_frag(lds_byte* tile, int r0, int step, int lane)
+    // Where a lane's reads start in a tile: row lane & 31 for row fragments, and for column fragments the lane's part of
+    // rows 0 .. 15. A step, a column tile or eight rows more flip bits of these (the swizzle's bits lie above the lane's),
+    // so a read costs one exclusive or and everything else is an immediate.
+    __device__ static __forceinline__ uint32_t row_base(int lane)
     {
         constexpr int parts = sizeof(T) / 2;
-        const int r = r0 + (lane & 31), c = (2 * step + (lane >> 5)) * parts;
+        const int r = lane & 31;
+        return static_cast<uint32_t>(r * kRow + (((lane >> 5) * parts) ^ swz(r)) * 16);
+    }
+    __device__ static __forceinline__ uint32_t col_base(int lane)
+    {
+        const int h = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            // 16 lanes read 4 rows x 32 bytes, 8 bytes each, and receive one column of the four rows each
+            const int i = lane & 15, r = 4 * h + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
+            return static_cast<uint32_t>(r * kRow + (c ^ swz(r)) * 16 + (i & 1) * 8);
+        } else {
+            const int col = lane & 31;
+            return static_cast<uint32_t>(4 * h * kRow + ((col >> 2) ^ swz(4 * h)) * 16 + (col & 3) * 4);
+        }
+    }
+
+    // Row r0 + (lane & 31), elements 16 step + 8 (lane >> 5) .. + 7, of the tile at `tile`; r0 a multiple of 32.
+    __device__ static __forceinline__ Frag<T> row_frag(uint32_t base, uint32_t tile, int r0, int step)
+    {
+        constexpr int parts = sizeof(T) / 2;
         Frag<T> f;
 #pragma unroll
         for (int i = 0; i < parts; ++i) {
-            const u32x4_t x = *(lds_ptr<u32x4_t>)(tile + r * kRow + ((c + i) ^ swz(r)) * 16);
+            const u32x4_t x = *lds_at<u32x4_t>((base ^ static_cast<uint32_t>((2 * step * parts + i) * 16)) + (tile + r0 * kRow));
             frag_from(f, x, i);
         }
         return f;
     }
 
     // Column 32 ct + (lane & 31) of rows r0 + 4h .. + 3 and r0 + 8 + 4h .. + 3 (h = lane >> 5), r0 a multiple of 16.
-    __device__ static __forceinline__ Frag<T> col_frag(lds_byte* tile, int r0, int ct, int lane)
+    __device__ static __forceinline__ Frag<T> col_frag(uint32_t base, uint32_t tile, int r0, int ct)
     {
         Frag<T> f;
-        const int h = lane >> 5;
         if constexpr (sizeof(T) == 2) {
-            // 16 lanes read 4 rows x 32 bytes, 8 bytes each, and receive one column of the four rows each
-            const int i = lane & 15, c = 4 * ct + 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
             short4_t x[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int r = r0 + 8 * u + 4 * h + (i >> 2);
-                x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr<short4_t>)(tile + r * kRow + (c ^ swz(r)) * 16 + (i & 1) * 8));
+                const uint32_t flip = static_cast<uint32_t>((4 * ct ^ swz(8 * u)) * 16);
+                x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<short4_t>((base ^ flip) + (tile + (r0 + 8 * u) * kRow)));
             }
             f.v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            const int col = 32 * ct + (lane & 31);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int r = r0 + 8 * (j >> 2) + 4 * h + (j & 3);
-                f.v[j] = *(lds_ptr<float>)(tile + r * kRow + ((col >> 2) ^ swz(r)) * 16 + (col & 3) * 4);
+                const int r = 8 * (j >> 2) + (j & 3);
+                f.v[j] = *lds_at<float>((base ^ static_cast<uint32_t>((8 * ct ^ swz(r)) * 16)) + (tile + (r0 + r) * kRow));
             }
         }
         return f;
     }
 };
+
+// Keeps a lane's base from being known across iterations: the compiler would otherwise hold every variant of it in a
+// register of its own (32 of them in the key pass).
+__device__ __forceinline__ void opaque(uint32_t& x) { asm("" : "+v"(x)); }
 
 // Row of result register r in a lane's half h.
 __device__ __forceinline__ constexpr int acc_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
@@ -229,7 +259,8 @@ __device__ __forceinline__ float other_half(float x) { return xchg_f32<32>(x); }
 struct DiffBwdArgs {
     DiffArgs f;                 // out, out1 and lse are the forward's (read)
     const void* dout;           // [B][Nq][heads][2d] contiguous
-    // by rows of one key head, [B][kv_heads][kDiffStats][Rpad] fp32: lse_0, lse_1, t_0, t_1, lambda
+    // by rows of one key head, [B][kv_heads][kDiffStats][Rpad] fp32. With s the logits' scale, S the sign of lambda:
+    // -lse_0 / s, -(lse_1 - log2 |lambda|) / s, -t_0, -S (t_0 - t_1), -S for the key pass; -lse_1 / s, t_0 - t_1, t_1
     float* stats;
     int Rpad;                   // R rounded up to kDiffRowPad; rows behind R are zero
     void* dq;                   // [B][Nq][2 heads][d]
@@ -239,10 +270,27 @@ struct DiffBwdArgs {
     bool lam_heads;
     float* dlam_rows;           // fp32 [heads][B * Nq] with lam_heads
     float grad_scale;           // scale of the logits
+    // the key pass in `splits` parts of the rows: fp32 [splits][B][Nk][kv_heads][4d] sums of dK_0, dK_1 and dV (splits > 1)
+    int splits;
+    float* part;
 };
 constexpr float kDiffLn2 = 0.693147180559945f;
-constexpr int kDiffStats = 5;
+constexpr int kDiffStats = 8;
 constexpr int kDiffRowPad = 64;
+constexpr int kDiffKeys = 128;  // keys of a workgroup of the key pass
+
+// Parts of the key pass's rows. One key head's keys in tiles of 128 may be few workgroups, and under a causal mask the
+// first tile meets all rows and the last only its own; parts cost a write and a read of fp32 sums. Two workgroups run on a
+// unit: as many parts as fill the units twice where work is even and four times where it is causal, no part below
+// 8 tiles of 32 rows, at most 8. (2 x 4096 keys, 16 heads over 4, d = 64, bf16, causal: @1@)
+inline int diff_key_splits(int B, int kv_heads, int Nk, int R, bool causal)
+{
+    const long long groups = static_cast<long long>(B) * kv_heads * ((Nk + kDiffKeys - 1) / kDiffKeys);
+    const long long want = static_cast<long long>(device_cu_count()) * (causal ? 4 : 2);
+    const long long most = R / 256;
+    const long long s = (want + groups - 1) / groups;
+    return static_cast<int>(s < 1 || most < 1 ? 1 : (s > most ? most : s) > 8 ? 8 : (s > most ? most : s));
+}
 
 hipError_t launch_diff_attn(const DiffArgs& a, int d, bool use_bf16, hipStream_t stream);
 hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool use_bf16, hipStream_t stream);

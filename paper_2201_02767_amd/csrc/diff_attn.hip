@@ -73,18 +73,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_fwd_ker
         VT::stage(at + 2 * kK, vmap, BN, wave, 4, lane, voff);
     };
 
+    const uint32_t base0 = lds_address(lds);
+    uint32_t krow = KT::row_base(lane), vcol = VT::col_base(lane);
     const int wrow_last = min(row0 + (rb + 1) * 32 * NQ, a.R) - 1;
     const int wend = row0 + rb * 32 * NQ < a.R ? range.limit(fast_div(wrow_last, a.div_G)) : 0;   // this wave's keys
     const int nt = (kend + BN - 1) / BN;
     if (nt > 0) stage(0, lds);
     for (int t = 0; t < nt; ++t) {
         const int k0 = t * BN;
-        lds_byte* const cur = lds + (t & 1) * kStage;
         tiles::wait_lds_loads();
         __syncthreads();
         if (t + 1 < nt) stage(k0 + BN, lds + ((t + 1) & 1) * kStage);
         if (k0 >= wend) continue;
-        lds_byte* const kt = cur + map * kK;
+        opaque(krow);
+        opaque(vcol);
+        const uint32_t kt = base0 + (t & 1) * kStage + map * kK, vt = base0 + (t & 1) * kStage + 2 * kK;
         f32x16 s[BN / 32][NQ];
 #pragma unroll
         for (int u = 0; u < BN / 32; ++u) {
@@ -92,7 +95,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_fwd_ker
             for (int n = 0; n < NQ; ++n) s[u][n] = f32x16{};
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
-                const Frag<T> kf = KT::row_frag(kt, 32 * u, c, lane);
+                const Frag<T> kf = KT::row_frag(krow, kt, 32 * u, c);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) s[u][n] = mma(kf, qf[n][c], s[u][n]);
             }
@@ -138,7 +141,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_fwd_ker
         for (int w = 0; w < BN / 16; ++w)
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
-                const Frag<T> vf = VT::col_frag(cur + 2 * kK, 16 * w, c, lane);
+                const Frag<T> vf = VT::col_frag(vcol, vt, 16 * w, c);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) acc[n][c] = mma(vf, p[n][w], acc[n][c]);
             }

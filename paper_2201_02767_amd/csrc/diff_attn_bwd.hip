@@ -3,9 +3,13 @@
 // With D = dO V^T, t_m = dO . O_m (O_m = P_m V) and the weights made again from the stored sums:
 //   dS_0 = P_0 (D - t_0),   dS_1 = -lambda P_1 (D - t_1),   dlambda = -t_1
 //   dQ_m = scale dS_m K_m,  dK_m = scale dS_m^T Q_m,        dV = (P_0 - lambda P_1)^T dO
-// Three launches: t_m and lambda by row; dQ, a wave taking 32 rows through the keys; dK and dV, a wave taking 32 keys
-// through the rows of every query head that shares them. D, and in the key pass V's weights, serve both maps, so here
-// a wave holds both. Each result is summed in one place and in one order: no atomics, the same bits every run.
+// Launches: the rows' statistics; dQ, a wave taking 32 rows through the keys; dK and dV, a wave taking 32 keys through the
+// rows of every query head that shares them. D, and in the key pass V's weights, serve both maps, so here a wave
+// holds both. Each result is summed in one order: no atomics, the same bits every run.
+//
+// D starts from -t_0 instead of zero, and in the key pass, where a statistic is needed for every register, Q K^T from
+// -lse / scale: a weight is then one product and one power of two away. t_m comes from the stored, rounded O and O_1; the rows of P_1 (D - t_1), which
+// with the exact t_1 sum to zero, give what is missing, and dlambda is exact to fp32.
 #include <atomic>
 
 #include "diff_attn.h"
@@ -17,7 +21,7 @@ using namespace diff;
 
 constexpr int kThreads = 256;
 
-// ---- t_m, lambda's gradient ----
+// ---- the rows' statistics ----
 
 // A row (b, i, h) takes 2D / V lanes of one 16-byte chunk each.
 template <typename T, int D>
@@ -60,16 +64,14 @@ __global__ __launch_bounds__(kThreads) void diff_rows_kernel(DiffBwdArgs a)
         t1 += xchg_f32<16>(t1);
     }
     if (c != 0) return;
-    const float lam = diff_lambda(f, b, i, h);
+    const float lam = diff_lambda(f, b, i, h), inv = -1.0f / f.scale;
     const float* const lse = f.lse + (static_cast<long long>(b) * f.heads + h) * 2 * f.Nq + i;
-    st[0] = lse[0];
-    st[a.Rpad] = lse[f.Nq];
-    st[2 * static_cast<size_t>(a.Rpad)] = fmaf(lam, t1, s);        // dO . O_0 = dO . (O + lambda O_1)
-    st[3 * static_cast<size_t>(a.Rpad)] = t1;
-    st[4 * static_cast<size_t>(a.Rpad)] = lam;
-    if (a.lam_heads) a.dlam_rows[static_cast<long long>(h) * f.B * f.Nq + static_cast<long long>(b) * f.Nq + i] = -t1;
-    else if (f.lam_bf16) Storage<bf16>::store1(a.dlam, row, -t1);
-    else Storage<float>::store1(a.dlam, row, -t1);
+    const float l0 = lse[0], l1 = lse[f.Nq], t0 = fmaf(lam, t1, s);        // dO . O_0 = dO . (O + lambda O_1)
+    const float nsign = lam < 0.f ? 1.0f : -1.0f;
+    const float x_[kDiffStats] = {l0 * inv, (l1 - __builtin_amdgcn_logf(fabsf(lam))) * inv, -t0, nsign * (t0 - t1), nsign,
+                                  l1 * inv, t0 - t1, t1};
+#pragma unroll
+    for (int p = 0; p < kDiffStats; ++p) st[static_cast<size_t>(p) * a.Rpad] = x_[p];
 }
 
 // A weight for each head: its rows' gradients summed, one workgroup a head.
@@ -115,8 +117,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
     const int rr = row0 + wave * 32 + (lane & 31), r = min(rr, f.R - 1);
     const int qi = fast_div(r, f.div_G), h = g * G + r - qi * G, lim = range.limit(qi);
     const float* const st = a.stats + static_cast<size_t>(bh) * kDiffStats * a.Rpad + r;
-    const float lse0 = st[0], lse1 = st[a.Rpad], t0 = st[2 * static_cast<size_t>(a.Rpad)],
-                t1 = st[3 * static_cast<size_t>(a.Rpad)], nlam = -st[4 * static_cast<size_t>(a.Rpad)];
+    const size_t plane = a.Rpad;
+    const float nlse0 = st[0] * f.scale, nlse1 = st[5 * plane] * f.scale, nt0 = st[2 * plane], t01 = st[6 * plane], t1 = st[7 * plane];
+    const float nlam = -diff_lambda(f, b, qi, h);
+    float miss = 0.f;                       // sum of P_1 (D - t_1)
     Frag<T> qf[2][D / 16], of[D / 8];
 #pragma unroll
     for (int m = 0; m < 2; ++m)
@@ -146,33 +150,39 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
     };
 
     const int wend = row0 + wave * 32 < f.R ? range.limit(fast_div(min(row0 + wave * 32 + 32, f.R) - 1, f.div_G)) : 0;
+    const uint32_t base0 = lds_address(lds);
+    uint32_t krow = KT::row_base(lane), kcol = KT::col_base(lane), vrow = VT::row_base(lane);
     const int nt = (kend + BN - 1) / BN;
     if (nt > 0) stage(0, lds);
     for (int t = 0; t < nt; ++t) {
         const int k0 = t * BN;
-        lds_byte* const cur = lds + (t & 1) * kStage;
+        const uint32_t k0t = base0 + (t & 1) * kStage, k1t = k0t + kK, vt = k0t + 2 * kK;
         tiles::wait_lds_loads();
         __syncthreads();
         if (t + 1 < nt) stage(k0 + BN, lds + ((t + 1) & 1) * kStage);
 #pragma unroll
         for (int u = 0; u < BN / 32; ++u) {
             if (k0 + 32 * u >= wend) break;
-            f32x16 s0{}, s1{}, dp{};
+            opaque(krow);
+            opaque(kcol);
+            opaque(vrow);
+            f32x16 s0{}, s1{}, dp;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) dp[e] = nt0;
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
-                s0 = mma(KT::row_frag(cur, 32 * u, c, lane), qf[0][c], s0);
-                s1 = mma(KT::row_frag(cur + kK, 32 * u, c, lane), qf[1][c], s1);
+                s0 = mma(KT::row_frag(krow, k0t, 32 * u, c), qf[0][c], s0);
+                s1 = mma(KT::row_frag(krow, k1t, 32 * u, c), qf[1][c], s1);
             }
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) dp = mma(VT::row_frag(cur + 2 * kK, 32 * u, c, lane), of[c], dp);
-            const bool edge = k0 + 32 * u + 32 > kmask;
+            for (int c = 0; c < D / 8; ++c) dp = mma(VT::row_frag(vrow, vt, 32 * u, c), of[c], dp);
             float d0[16], d1[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                d0[e] = exp2_fast(fmaf(s0[e], f.scale, -lse0)) * (dp[e] - t0);
-                d1[e] = exp2_fast(fmaf(s1[e], f.scale, -lse1)) * nlam * (dp[e] - t1);
+                d0[e] = exp2_fast(fmaf(s0[e], f.scale, nlse0)) * dp[e];
+                d1[e] = exp2_fast(fmaf(s1[e], f.scale, nlse1)) * (dp[e] + t01);
             }
-            if (edge) {
+            if (k0 + 32 * u + 32 > kmask) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (k0 + 32 * u + acc_row(e, half) >= lim) {
@@ -181,17 +191,29 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
                     }
             }
 #pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                miss += d1[e];
+                d1[e] *= nlam;
+            }
+#pragma unroll
             for (int w = 0; w < 2; ++w) {
                 const Frag<T> f0 = pack_frag<T>(d0 + 8 * w), f1 = pack_frag<T>(d1 + 8 * w);
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
-                    acc[0][c] = mma(KT::col_frag(cur, 32 * u + 16 * w, c, lane), f0, acc[0][c]);
-                    acc[1][c] = mma(KT::col_frag(cur + kK, 32 * u + 16 * w, c, lane), f1, acc[1][c]);
+                    acc[0][c] = mma(KT::col_frag(kcol, k0t, 32 * u + 16 * w, c), f0, acc[0][c]);
+                    acc[1][c] = mma(KT::col_frag(kcol, k1t, 32 * u + 16 * w, c), f1, acc[1][c]);
                 }
             }
         }
     }
+    miss += other_half(miss);
     if (rr >= f.R) return;
+    if (half == 0) {
+        const float dl = -(t1 + miss);
+        if (a.lam_heads) a.dlam_rows[static_cast<long long>(h) * f.B * f.Nq + static_cast<long long>(b) * f.Nq + qi] = dl;
+        else if (f.lam_bf16) Storage<bf16>::store1(a.dlam, orow / (2 * D), dl);
+        else Storage<float>::store1(a.dlam, orow / (2 * D), dl);
+    }
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -205,25 +227,28 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
 
 // ---- dK, dV ----
 
+// A wave takes 32 keys; K stays in its registers, V (whose 32 more would leave room for one wave a SIMD only) in LDS.
+// With `splits` > 1 a workgroup takes one part of the rows that see its keys and writes fp32 sums to `part`.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D == 32 ? 2 : 1) void diff_dkv_kernel(DiffBwdArgs a)
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_kernel(DiffBwdArgs a)
 {
     using QT = Tile<T, D>;
     using OT = Tile<T, 2 * D>;
-    constexpr int ES = sizeof(T), BM = 32, BN = 128;
+    constexpr int ES = sizeof(T), BM = 32, BN = kDiffKeys;
     constexpr int kQ = QT::bytes(BM), kO = OT::bytes(BM), kStats = 1024, kStage = 2 * kQ + kO + kStats;
     extern __shared__ __align__(16) unsigned char lds_raw[];
     lds_byte* const lds = (lds_byte*)lds_raw;
+    lds_byte* const vt = lds + 2 * kStage;
     const DiffArgs& f = a.f;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int tiles_n = (f.Nk + BN - 1) / BN;
     const int logical = xcd_remap(blockIdx.x, gridDim.x);
-    const int bh = logical / tiles_n, tile = logical - bh * tiles_n;
+    const int bh = logical / (tiles_n * a.splits), rest = logical - bh * tiles_n * a.splits;
+    const int tile = rest / a.splits, split = rest - tile * a.splits;      // the keys that most rows see first
     const int b = bh / f.kv_heads, g = bh - b * f.kv_heads, G = f.heads / f.kv_heads;
     const DiffRange range = diff_range(f, b);
     const int k0 = tile * BN, wk0 = k0 + wave * 32, key = wk0 + (lane & 31);
-    const long long kc = min(key, f.Nk - 1);
 
     f32x16 av[2 * D / 32], ak[2][D / 32];
 #pragma unroll
@@ -233,22 +258,26 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D == 32 ? 2 : 1) void d
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) ak[m][c] = f32x16{};
 
-    // rows that see any of these keys: from the first query at or behind k0 on
+    // rows that see any of these keys: from the first query at or behind k0 on; this workgroup's tiles of them
     const int i0 = range.causal ? min(max(0, k0 - range.pos), f.Nq) : 0;
     const int rbeg = (k0 < range.len ? i0 * G : f.R) / BM * BM;
-    const int nt = k0 < range.len ? (f.R - rbeg + BM - 1) / BM : 0;
+    const int all = k0 < range.len ? (f.R - rbeg + BM - 1) / BM : 0;
+    const int t0 = static_cast<int>(static_cast<long long>(all) * split / a.splits);
+    const int t1 = static_cast<int>(static_cast<long long>(all) * (split + 1) / a.splits);
 
-    if (nt > 0) {
-        Frag<T> kf[2][D / 16], vf[D / 8];
-        // (a key behind the element's last is read as that one; its weights are masked)
-        const long long kv = min(kc, static_cast<long long>(range.len) - 1);
+    if (t0 < t1) {
+        // (keys behind the element's last are read as that one; their weights are masked)
+        const int last = range.len - 1;
+        const auto vmap = tiles::map_resource(byte_at(f.v, b * f.vb + k0 * f.vn + g * f.vh, ES));
+        OT::stage(vt, vmap, BN, wave, 4, lane,
+                  [&](int r) { return static_cast<uint32_t>(min(r, last - k0)) * (static_cast<uint32_t>(f.vn) * ES); });
+        Frag<T> kf[2][D / 16];
+        const long long kr = min(key, last);
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
             for (int s = 0; s < D / 16; ++s)
-                kf[m][s] = global_frag<T>(f.k, b * f.kb + kv * f.kn + (2 * g + m) * f.kh + 16 * s + 8 * half);
-#pragma unroll
-        for (int s = 0; s < D / 8; ++s) vf[s] = global_frag<T>(f.v, b * f.vb + kv * f.vn + g * f.vh + 16 * s + 8 * half);
+                kf[m][s] = global_frag<T>(f.k, b * f.kb + kr * f.kn + (2 * g + m) * f.kh + 16 * s + 8 * half);
 
         const auto smap = tiles::map_resource(reinterpret_cast<const unsigned char*>(a.stats + static_cast<size_t>(bh) * kDiffStats * a.Rpad));
         auto stage = [&](int r0, lds_byte* at) {
@@ -276,91 +305,136 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D == 32 ? 2 : 1) void d
             QT::stage(at, qmap0, BM, wave, 4, lane, qoff);
             QT::stage(at + kQ, qmap0, BM, wave, 4, lane, qoff1);
             OT::stage(at + 2 * kQ, omap, BM, wave, 4, lane, ooff);
-            // the five statistics of the 32 rows, 128 bytes each (lanes behind the fifth repeat it)
+            // five statistics of the 32 rows, 128 bytes each (lanes behind the fifth repeat it)
             if (wave == 0) {
-                const int p = min(lane >> 3, kDiffStats - 1);
+                const int p = min(lane >> 3, 4);
                 tiles::load_lds16(smap, (static_cast<uint32_t>(p) * a.Rpad + r0 + 4 * (lane & 7)) * 4u, 0, at + 2 * kQ + kO);
             }
         };
 
-        const bool key_ok = key < range.len;
-        stage(rbeg, lds);
-        for (int t = 0; t < nt; ++t) {
-            const int r0 = rbeg + t * BM;
-            lds_byte* const cur = lds + (t & 1) * kStage;
-            tiles::wait_lds_loads();
-            __syncthreads();
-            if (t + 1 < nt) stage(r0 + BM, lds + ((t + 1) & 1) * kStage);
-            // masked: some key behind the element's last or the first row's limit, or rows behind the last
-            const bool edge = wk0 + 32 > range.limit(fast_div(r0, f.div_G)) || r0 + BM > f.R;
-            unsigned seen = 0xFFFFu;
-            if (edge) {
-                seen = 0;
+        // the first row that sees this lane's key, and one that sees every key of the wave (R: none)
+        auto first_row = [&](int x) { return x >= range.len ? f.R : range.causal ? min(max(0, x - range.pos), f.Nq) * G : 0; };
+        const int see = first_row(key), wave_see = first_row(wk0 + 31);
+        const uint32_t base0 = lds_address(lds), vw = lds_address(vt) + 32 * wave * OT::kRow;
+        uint32_t qrow = QT::row_base(lane), qcol = QT::col_base(lane), orow = OT::row_base(lane), ocol = OT::col_base(lane);
+        const uint32_t srow = 16 * half;
+        // the 32 rows from r0 on, in the stage at cur
+        auto rows = [&](int r0, uint32_t cur) {
+            opaque(qrow);
+            opaque(qcol);
+            opaque(orow);
+            opaque(ocol);
+            const bool edge = r0 < wave_see || r0 + BM > f.R;
+            // four rows' statistics at a time: rows 8 (e / 4) + 4 half .. + 3
+            const uint32_t st = cur + 2 * kQ + kO;
+            auto stat = [&](int plane, int e) { return *lds_at<f32x4>(srow + (st + plane * 128 + 8 * e)); };
+            auto from = [&](int plane) {
+                f32x16 x;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int r = r0 + acc_row(e, half);
-                    if (key_ok && r < f.R && key < range.limit(fast_div(r, f.div_G))) seen |= 1u << e;
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4 y = stat(plane, e);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[e + j] = y[j];
                 }
-            }
-            f32x16 dp{};
+                return x;
+            };
+            f32x16 dp = from(2);
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) dp = mma(OT::row_frag(cur + 2 * kQ, 0, c, lane), vf[c], dp);
-            lds_byte* const st = cur + 2 * kQ + kO + 16 * half;
+            for (int c = 0; c < D / 8; ++c) {
+                dp = mma(OT::row_frag(orow, cur + 2 * kQ, 0, c), OT::row_frag(orow, vw, 0, c), dp);
+                if (c % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
             float w[16];
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                f32x16 s{};
+                f32x16 s = from(m);
 #pragma unroll
-                for (int c = 0; c < D / 16; ++c) s = mma(QT::row_frag(cur + m * kQ, 0, c, lane), kf[m][c], s);
+                for (int c = 0; c < D / 16; ++c) s = mma(QT::row_frag(qrow, cur + m * kQ, 0, c), kf[m][c], s);
                 float ds[16];
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
-                    lds_byte* const at = st + 8 * e;        // rows 8 (e / 4) + 4 half .. + 3
-                    const f32x4 lse = *(lds_ptr<f32x4>)(at + m * 128), tm = *(lds_ptr<f32x4>)(at + 256 + m * 128);
-                    f32x4 lam{};
-                    if (m == 1) lam = *(lds_ptr<f32x4>)(at + 512);
+                    f32x4 t{}, sign{};
+                    if (m == 1) {
+                        t = stat(3, e);
+                        sign = stat(4, e);
+                    }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        float p = exp2_fast(fmaf(s[e + j], f.scale, -lse[j]));
-                        if (m == 1) p *= -lam[j];
-                        ds[e + j] = p * (dp[e + j] - tm[j]);
-                        w[e + j] = m == 0 ? p : w[e + j] + p;
+                        const float p = exp2_fast(s[e + j] * f.scale);
+                        ds[e + j] = p * (m == 0 ? dp[e + j] : fmaf(sign[j], dp[e + j], t[j]));
+                        w[e + j] = m == 0 ? p : fmaf(sign[j], p, w[e + j]);
                     }
                 }
                 if (edge) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (!(seen & (1u << e))) ds[e] = w[e] = 0.f;
+                    for (int e = 0; e < 16; ++e) {
+                        const int r = r0 + acc_row(e, half);
+                        if (r < see || r >= f.R) ds[e] = w[e] = 0.f;
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const Frag<T> fd = pack_frag<T>(ds + 8 * u);
 #pragma unroll
-                    for (int c = 0; c < D / 32; ++c) ak[m][c] = mma(QT::col_frag(cur + m * kQ, 16 * u, c, lane), fd, ak[m][c]);
+                    for (int c = 0; c < D / 32; ++c) ak[m][c] = mma(QT::col_frag(qcol, cur + m * kQ, 16 * u, c), fd, ak[m][c]);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const Frag<T> fw = pack_frag<T>(w + 8 * u);
 #pragma unroll
-                for (int c = 0; c < 2 * D / 32; ++c) av[c] = mma(OT::col_frag(cur + 2 * kQ, 16 * u, c, lane), fw, av[c]);
+                for (int c = 0; c < 2 * D / 32; ++c) av[c] = mma(OT::col_frag(ocol, cur + 2 * kQ, 16 * u, c), fw, av[c]);
             }
+        };
+        stage(rbeg + t0 * BM, lds);
+        for (int t = t0; t < t1; ++t) {
+            tiles::wait_lds_loads();
+            __syncthreads();
+            if (t + 1 < t1) stage(rbeg + (t + 1) * BM, lds + ((t - t0 + 1) & 1) * kStage);
+            rows(rbeg + t * BM, base0 + ((t - t0) & 1) * kStage);
         }
     }
     if (key >= f.Nk) return;
     const long long krow = (static_cast<long long>(b) * f.Nk + key) * f.kv_heads + g;
+    auto write = [&](auto type, void* dk, void* dv, long long at, int row, float scale) {
+        using O = decltype(type);
 #pragma unroll
-    for (int e = 0; e < 16; e += 4) {
+        for (int e = 0; e < 16; e += 4) {
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c)
-                store4<T>(a.dk, (2 * krow + m) * D + 32 * c + acc_row(e, half), ak[m][c][e] * a.grad_scale,
-                          ak[m][c][e + 1] * a.grad_scale, ak[m][c][e + 2] * a.grad_scale, ak[m][c][e + 3] * a.grad_scale);
+                for (int c = 0; c < D / 32; ++c)
+                    store4<O>(dk, at * row + m * D + 32 * c + acc_row(e, half), ak[m][c][e] * scale, ak[m][c][e + 1] * scale,
+                              ak[m][c][e + 2] * scale, ak[m][c][e + 3] * scale);
 #pragma unroll
-        for (int c = 0; c < 2 * D / 32; ++c)
-            store4<T>(a.dv, krow * (2 * D) + 32 * c + acc_row(e, half), av[c][e], av[c][e + 1], av[c][e + 2], av[c][e + 3]);
+            for (int c = 0; c < 2 * D / 32; ++c)
+                store4<O>(dv, at * row + 32 * c + acc_row(e, half), av[c][e], av[c][e + 1], av[c][e + 2], av[c][e + 3]);
+        }
+    };
+    if (a.splits == 1) {
+        write(T{}, a.dk, a.dv, krow, 2 * D, a.grad_scale);
+    } else {
+        // [split][key row][dK_0, dK_1, dV]
+        const long long rows = static_cast<long long>(f.B) * f.Nk * f.kv_heads;
+        write(float{}, a.part, a.part + 2 * D, split * rows + krow, 4 * D, 1.0f);
     }
+}
+
+// The parts' sums, in their order: four channels of one key row a thread.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void diff_dkv_join_kernel(DiffBwdArgs a)
+{
+    const long long item = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
+    const long long total = static_cast<long long>(a.f.B) * a.f.Nk * a.f.kv_heads * D;
+    if (item >= total) return;
+    const f32x4* p = reinterpret_cast<const f32x4*>(a.part) + item;
+    f32x4 x = *p;
+    for (int s = 1; s < a.splits; ++s) x += p[s * total];
+    const long long row = item / D;
+    const int c = 4 * static_cast<int>(item - row * D);
+    if (c < 2 * D) store4<T>(a.dk, row * (2 * D) + c, x[0] * a.grad_scale, x[1] * a.grad_scale, x[2] * a.grad_scale, x[3] * a.grad_scale);
+    else store4<T>(a.dv, row * (2 * D) + c - 2 * D, x[0], x[1], x[2], x[3]);
 }
 
 template <typename T, int D>
@@ -371,20 +445,25 @@ hipError_t launch_bwd(const DiffBwdArgs& a, hipStream_t stream)
     const long long bh = static_cast<long long>(a.f.B) * a.f.kv_heads;
     constexpr int lpr = 2 * D * ES / 16;
     const long long rblocks = (bh * a.Rpad * lpr + kThreads - 1) / kThreads;
-    const long long qblocks = (a.f.R + 127) / 128 * bh, kblocks = (a.f.Nk + 127) / 128 * bh;
+    const long long qblocks = (a.f.R + 127) / 128 * bh, kblocks = (a.f.Nk + kDiffKeys - 1) / kDiffKeys * bh * a.splits;
     if (rblocks > 0x7FFFFFFFLL || qblocks > 0x7FFFFFFFLL || kblocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     hipError_t e = set_max_lds_once(reinterpret_cast<const void*>(&diff_dq_kernel<T, D, BN>), configured_q);
     if (e != hipSuccess) return e;
     e = set_max_lds_once(reinterpret_cast<const void*>(&diff_dkv_kernel<T, D>), configured_k);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((diff_rows_kernel<T, D>), dim3(static_cast<unsigned>(rblocks)), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((diff_dq_kernel<T, D, BN>), dim3(static_cast<unsigned>(qblocks)), dim3(kThreads), 2 * BN * 4 * D * ES,
+                       stream, a);
     if (a.lam_heads)
         hipLaunchKernelGGL(diff_lambda_kernel, dim3(static_cast<unsigned>(a.f.heads)), dim3(1024), 0, stream, a.dlam_rows,
                            static_cast<long long>(a.f.B) * a.f.Nq, a.dlam, a.f.lam_bf16);
-    hipLaunchKernelGGL((diff_dq_kernel<T, D, BN>), dim3(static_cast<unsigned>(qblocks)), dim3(kThreads), 2 * BN * 4 * D * ES,
-                       stream, a);
-    hipLaunchKernelGGL((diff_dkv_kernel<T, D>), dim3(static_cast<unsigned>(kblocks)), dim3(kThreads), 2 * (32 * 4 * D * ES + 1024),
-                       stream, a);
+    hipLaunchKernelGGL((diff_dkv_kernel<T, D>), dim3(static_cast<unsigned>(kblocks)), dim3(kThreads),
+                       2 * (32 * 4 * D * ES + 1024) + kDiffKeys * 2 * D * ES, stream, a);
+    if (a.splits > 1) {
+        const long long items = static_cast<long long>(a.f.B) * a.f.Nk * a.f.kv_heads * D;
+        hipLaunchKernelGGL((diff_dkv_join_kernel<T, D>), dim3(static_cast<unsigned>((items + kThreads - 1) / kThreads)),
+                           dim3(kThreads), 0, stream, a);
+    }
     return hipGetLastError();
 }
 

@@ -258,8 +258,9 @@ def diff_attn_backward(q, k, v, lam, out, kept, dout, *, scale=None, causal=Fals
     grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v, lam)]
     if out.numel() == 0 or args.Nk == 0:
         return tuple(g.zero_() for g in grads)
-    ws = torch.empty(lib().qta_diff_attn_backward_workspace_bytes(ctypes.byref(args)), dtype=torch.uint8, device=q.device)
     with _on(q):
+        ws = torch.empty(lib().qta_diff_attn_backward_workspace_bytes(ctypes.byref(args)), dtype=torch.uint8,
+                         device=q.device)
         _check("qta_diff_attn_backward", lib().qta_diff_attn_backward(
             ctypes.byref(args), _ptr(out), _ptr(out1), _ptr(lse), _ptr(dout), *[_ptr(g) for g in grads],
             int(lam.dim() == 1), _ptr(ws), ws.numel(), _stream(q.device)))
