@@ -425,8 +425,13 @@ typedef struct {
  *   out         [B][Nq][heads][2d] dtype, 16-byte aligned.
  *   out1, lse   for qta_diff_attn_backward: P_1 V as out, and fp32 [B][heads][2][Nq], the base-2 logarithm of each row's
  *               sum of weights (-inf for an empty row). Both NULL for inference.
+ *   workspace   256-byte aligned, qta_diff_attn_workspace_bytes bytes (at least 256 for valid shapes, 0 otherwise), in which
+ *               calls of few rows and many keys put the parts of their keys; may be NULL where 256 are asked for.
+ *               Need not be preserved or cleared; calls that may run at the same time need one each.
  */
-qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, void* out1, float* lse, void* stream);
+size_t qta_diff_attn_workspace_bytes(const qta_diff_attn_args* args);
+qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, void* out1, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream);
 
 /*
  * qta_diff_attn_backward - gradients for dout = dLoss/dout, the arguments and out, out1, lse being the forward's.

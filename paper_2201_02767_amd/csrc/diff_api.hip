@@ -77,6 +77,23 @@ DiffArgs make_args(const qta_diff_attn_args* a)
     return x;
 }
 
+// Regions of the forward's workspace.
+struct FwdLayout {
+    DiffParts parts;
+    size_t part_sums, total;
+};
+FwdLayout fwd_layout(const qta_diff_attn_args* a)
+{
+    FwdLayout L{};
+    const int R = a->Nq * (a->heads / a->kv_heads);
+    L.parts = diff_key_parts(a->B, a->kv_heads, a->Nk, R);
+    if (L.parts.splits == 1) return L;
+    const size_t rows = static_cast<size_t>(L.parts.splits) * a->B * a->kv_heads * 2 * R;
+    L.part_sums = align_up(rows * 2 * a->d * sizeof(float));
+    L.total = L.part_sums + align_up(rows * 2 * sizeof(float));
+    return L;
+}
+
 // Regions of the backward's workspace.
 struct BwdLayout {
     size_t stats, dlam_rows, part, total;
@@ -101,15 +118,32 @@ BwdLayout bwd_layout(const qta_diff_attn_args* a, bool lam_heads)
 
 extern "C" {
 
-qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, void* out1, float* lse, void* stream)
+size_t qta_diff_attn_workspace_bytes(const qta_diff_attn_args* args)
+{
+    if (check_diff(args, true) != QTA_OK) return 0;
+    const size_t n = fwd_layout(args).total;
+    return n < kAlign ? kAlign : n;
+}
+
+qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, void* out1, float* lse, void* workspace,
+                         size_t workspace_bytes, void* stream)
 {
     const qta_status st = check_diff(args, false);
     if (st != QTA_OK) return st;
     if (!out || !aligned(out, 16) || (out1 != nullptr) != (lse != nullptr) || !aligned(out1, 16) || !aligned(lse, 4)) return QTA_ERR_INVALID;
+    const FwdLayout L = fwd_layout(args);
+    if (L.total > 0) {
+        if (workspace_bytes < L.total) return QTA_ERR_WORKSPACE;
+        if (!workspace || !aligned(workspace, kAlign)) return QTA_ERR_INVALID;
+    }
     DiffArgs a = make_args(args);
     a.out = out;
     a.out1 = out1;
     a.lse = lse;
+    a.keys_apart = L.parts.keys_apart;
+    a.splits = L.parts.splits;
+    a.part = static_cast<float*>(workspace);
+    a.part_sums = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + L.part_sums);
     return launch_diff_attn(a, args->d, args->dtype == QTA_BF16, static_cast<hipStream_t>(stream)) == hipSuccess ? QTA_OK : QTA_ERR_HIP;
 }
 

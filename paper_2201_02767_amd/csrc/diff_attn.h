@@ -34,7 +34,32 @@ struct DiffArgs {
     // [B][heads][2][Nq] (-inf where a row sees nothing)
     void* out1;
     float* lse;
+    // few rows: waves split the keys of a tile instead of rows, and the keys come in `splits` parts (see diff_key_parts),
+    // whose results go to part, fp32 [splits][B][kv_heads][2][R][2d], and part_sums, [..][R][2] (maximum, sum)
+    bool keys_apart;
+    int splits;
+    float* part;
+    float* part_sums;
 };
+
+// How a forward's keys are split. @2@
+struct DiffParts {
+    bool keys_apart;
+    int splits;
+};
+inline DiffParts diff_key_parts(int B, int kv_heads, int Nk, int R)
+{
+    const long long groups = static_cast<long long>(B) * kv_heads, cus = device_cu_count();
+    DiffParts p{false, 1};
+    const long long tiles = groups * ((R + 63) / 64);
+    if (tiles >= cus && R > 32) return p;
+    p.keys_apart = R <= 32;
+    const long long work = groups * ((R + (p.keys_apart ? 31 : 63)) / (p.keys_apart ? 32 : 64));
+    const long long want = (4 * cus + work - 1) / work, most = Nk / 128;
+    p.splits = static_cast<int>(most < 1 ? 1 : want < 1 ? 1 : want > most ? most : want);
+    if (p.splits > 64) p.splits = 64;
+    return p;
+}
 
 // The visible range of one batch element: keys [0, len), and for query i of a causal call those up to pos + i.
 struct DiffRange {

@@ -1,10 +1,10 @@
 // Differential attention, forward (the mathematics of the tiles is in diff_attn.h).
 //
 // One pass over the keys with running maxima and sums, S^T = K Q^T so that a lane holds one query's scores and its
-// rescaling is a lane's own. The two softmax maps share nothing but V and the rows, so a wave takes one map of 32 NQ
-// rows, and the difference is formed once at the end through LDS: a wave that held both maps' results would need twice the
-// accumulators and could take only half the rows, reading K and V from LDS twice as often.
+// rescaling is a lane's own. The two softmax maps share nothing but V and the rows, so a wave takes one map of 32 rows, and
+// the difference is formed once at the end through LDS.
 #include <atomic>
+#include <type_traits>
 
 #include "diff_attn.h"
 
@@ -15,49 +15,46 @@ using namespace diff;
 
 constexpr int kThreads = 256;
 
-// Four waves: wave w takes map w & 1 of the 32 NQ rows of block w >> 1. K_0, K_1 and V come in tiles of BN keys, two in LDS.
-template <typename T, int D, int NQ, int BN>
+// Maxima lag: a row's running maximum is raised only when a tile exceeds it by 2^8 or more, so that most tiles rescale
+// nothing. Weights then go up to 2^8, which costs neither fp32 sums nor bf16 weights any of their bits.
+constexpr float kLag = 8.0f;
+
+// Four waves over a tile of 64 rows: wave w takes map w & 1 of the 32 rows of block w >> 1. With KEYS, for calls of few
+// rows, over a tile of 32 rows: w >> 1 is then the half of every key tile that the wave takes. K_0, K_1 and V come in tiles of BN
+// keys, two of them in LDS. With a.splits > 1 a workgroup takes one part of its rows' keys and leaves the results as they
+// are, with their maxima and sums, to diff_join_kernel.
+template <typename T, int D, int BN, bool KEYS>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_fwd_kernel(DiffArgs a)
 {
     using KT = Tile<T, D>;
     using VT = Tile<T, 2 * D>;
-    constexpr int ES = sizeof(T), CT = 2 * D / 32, BM = 64 * NQ;
+    constexpr int ES = sizeof(T), CT = 2 * D / 32, BM = KEYS ? 32 : 64, U = KEYS ? BN / 64 : BN / 32;   // 32-key blocks of a wave
     constexpr int kK = KT::bytes(BN), kStage = 2 * kK + VT::bytes(BN);
+    static_assert(U >= 1, "a block of keys for every wave");
     extern __shared__ __align__(16) unsigned char lds_raw[];
     lds_byte* const lds = (lds_byte*)lds_raw;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int map = wave & 1, rb = wave >> 1, half = lane >> 5;
+    const int map = wave & 1, rb = KEYS ? 0 : wave >> 1, kb = KEYS ? wave >> 1 : 0, half = lane >> 5;
     const int tiles_n = (a.R + BM - 1) / BM;
     const int logical = xcd_remap(blockIdx.x, gridDim.x);
-    const int bh = logical / tiles_n, tile = tiles_n - 1 - (logical - bh * tiles_n);     // the longest rows first
+    const int work = logical / a.splits, split = logical - work * a.splits;
+    const int bh = work / tiles_n, tile = tiles_n - 1 - (work - bh * tiles_n);     // the longest rows first
     const int b = bh / a.kv_heads, g = bh - b * a.kv_heads, G = a.heads / a.kv_heads;
     const int row0 = tile * BM, row1 = min(row0 + BM, a.R);
     const DiffRange range = diff_range(a, b);
     const int kend = range.limit(fast_div(row1 - 1, a.div_G)), kmask = range.limit(fast_div(row0, a.div_G));
 
-    // this lane's rows
-    int lim[NQ], qi[NQ], qg[NQ];
-    Frag<T> qf[NQ][D / 16];
+    // this lane's row
+    const int rr = row0 + rb * 32 + (lane & 31), r = min(rr, a.R - 1);
+    const int qi = fast_div(r, a.div_G), h = g * G + r - qi * G, lim = range.limit(qi);
+    Frag<T> qf[D / 16];
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const int r = min(row0 + rb * 32 * NQ + n * 32 + (lane & 31), a.R - 1);
-        qi[n] = fast_div(r, a.div_G);
-        qg[n] = r - qi[n] * G;
-        lim[n] = range.limit(qi[n]);
-        const long long at = b * a.qb + qi[n] * a.qn + (2 * (g * G + qg[n]) + map) * a.qh;
+    for (int s = 0; s < D / 16; ++s) qf[s] = global_frag<T>(a.q, b * a.qb + qi * a.qn + (2 * h + map) * a.qh + 16 * s + 8 * half);
+    f32x16 acc[CT];
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) qf[n][s] = global_frag<T>(a.q, at + 16 * s + 8 * half);
-    }
-    f32x16 acc[NQ][CT];
-    float mx[NQ], sum[NQ];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        mx[n] = -INFINITY;
-        sum[n] = 0.f;
-#pragma unroll
-        for (int c = 0; c < CT; ++c) acc[n][c] = f32x16{};
-    }
+    for (int c = 0; c < CT; ++c) acc[c] = f32x16{};
+    float mx = -INFINITY, sum = 0.f;
 
     // rows behind the last visible key are read as that key (they are masked)
     auto stage = [&](int k0, lds_byte* at) {
@@ -66,148 +63,228 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_fwd_ker
         const auto kmap1 = tiles::map_resource(byte_at(a.k, b * a.kb + k0 * a.kn + (2 * g + 1) * a.kh, ES));
         const auto vmap = tiles::map_resource(byte_at(a.v, b * a.vb + k0 * a.vn + g * a.vh, ES));
         const uint32_t kstep = static_cast<uint32_t>(a.kn) * ES, vstep = static_cast<uint32_t>(a.vn) * ES;
-        auto koff = [&](int r) { return static_cast<uint32_t>(min(r, last)) * kstep; };
-        auto voff = [&](int r) { return static_cast<uint32_t>(min(r, last)) * vstep; };
+        auto koff = [&](int x) { return static_cast<uint32_t>(min(x, last)) * kstep; };
+        auto voff = [&](int x) { return static_cast<uint32_t>(min(x, last)) * vstep; };
         KT::stage(at, kmap0, BN, wave, 4, lane, koff);
         KT::stage(at + kK, kmap1, BN, wave, 4, lane, koff);
         VT::stage(at + 2 * kK, vmap, BN, wave, 4, lane, voff);
     };
 
-    const uint32_t base0 = lds_address(lds);
-    uint32_t krow = KT::row_base(lane), vcol = VT::col_base(lane);
-    const int wrow_last = min(row0 + (rb + 1) * 32 * NQ, a.R) - 1;
-    const int wend = row0 + rb * 32 * NQ < a.R ? range.limit(fast_div(wrow_last, a.div_G)) : 0;   // this wave's keys
-    const int nt = (kend + BN - 1) / BN;
-    if (nt > 0) stage(0, lds);
-    for (int t = 0; t < nt; ++t) {
-        const int k0 = t * BN;
-        tiles::wait_lds_loads();
-        __syncthreads();
-        if (t + 1 < nt) stage(k0 + BN, lds + ((t + 1) & 1) * kStage);
-        if (k0 >= wend) continue;
-        opaque(krow);
-        opaque(vcol);
-        const uint32_t kt = base0 + (t & 1) * kStage + map * kK, vt = base0 + (t & 1) * kStage + 2 * kK;
-        f32x16 s[BN / 32][NQ];
+    // this wave's keys, and this workgroup's part of the tiles
+    const int wend = rr - (lane & 31) < a.R ? range.limit(fast_div(min(row0 + rb * 32 + 32, a.R) - 1, a.div_G)) : 0;
+    const int all = (kend + BN - 1) / BN;
+    const int t0 = static_cast<int>(static_cast<long long>(all) * split / a.splits);
+    const int t1 = static_cast<int>(static_cast<long long>(all) * (split + 1) / a.splits);
+    const uint32_t base0 = lds_address(lds), krow = KT::row_base(lane) + map * kK + kb * (BN / 2) * KT::kRow,
+                   vcol = VT::col_base(lane) + 2 * kK + kb * (BN / 2) * VT::kRow;
+    auto keys = [&](int k0, auto odd) {
+        constexpr uint32_t at = odd.value * kStage;
+        f32x16 s[U];
 #pragma unroll
-        for (int u = 0; u < BN / 32; ++u) {
+        for (int u = 0; u < U; ++u) {
+            s[u] = f32x16{};
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) s[u][n] = f32x16{};
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-                const Frag<T> kf = KT::row_frag(krow, kt, 32 * u, c);
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) s[u][n] = mma(kf, qf[n][c], s[u][n]);
-            }
+            for (int c = 0; c < D / 16; ++c) s[u] = mma(KT::row_frag(krow, base0 + at, 32 * u, c), qf[c], s[u]);
         }
         if (k0 + BN > kmask) {
 #pragma unroll
-            for (int n = 0; n < NQ; ++n)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int u = 0; u < BN / 32; ++u)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (k0 + 32 * u + acc_row(r, half) >= lim[n]) s[u][n][r] = -INFINITY;
+                for (int e = 0; e < 16; ++e)
+                    if (k0 + kb * (BN / 2) + 32 * u + acc_row(e, half) >= lim) s[u][e] = -INFINITY;
         }
-        Frag<T> p[NQ][BN / 16];
+        float m = s[0][0];
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            float m = s[0][n][0];
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int u = 0; u < BN / 32; ++u)
+            for (int e = 0; e < 16; ++e) m = fmaxf(m, s[u][e]);
+        m = fmaxf(m, other_half(m)) * a.scale;
+        if (__any(m > mx + kLag)) {
+            m = fmaxf(m, mx);
+            const float alpha = exp2_fast(mx - (m == -INFINITY ? 0.f : m));
+            mx = m;
+            sum *= alpha;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) m = fmaxf(m, s[u][n][r]);
-            m = fmaxf(mx[n], fmaxf(m, other_half(m)) * a.scale);
-            // (a row that has seen nothing yet keeps -inf; its weights are exp2(-inf - 0))
-            const float base = m == -INFINITY ? 0.f : m;
-            const float alpha = exp2_fast(mx[n] - base);
-            mx[n] = m;
-            sum[n] *= alpha;
+            for (int c = 0; c < CT; ++c) acc[c] *= alpha;
+        }
+        // (a row that has seen nothing yet keeps -inf: its weights are exp2(-inf - 0))
+        const float base = mx == -INFINITY ? 0.f : -mx;
+        Frag<T> p[2 * U];
 #pragma unroll
-            for (int c = 0; c < CT; ++c) acc[n][c] *= alpha;
+        for (int u = 0; u < U; ++u) {
+            float x[16];
 #pragma unroll
-            for (int u = 0; u < BN / 32; ++u) {
-                float x[16];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    x[r] = exp2_fast(fmaf(s[u][n][r], a.scale, -base));
-                    sum[n] += x[r];
-                }
-                p[n][2 * u] = pack_frag<T>(x);
-                p[n][2 * u + 1] = pack_frag<T>(x + 8);
+            for (int e = 0; e < 16; ++e) {
+                x[e] = exp2_fast(fmaf(s[u][e], a.scale, base));
+                sum += x[e];
             }
+            p[2 * u] = pack_frag<T>(x);
+            p[2 * u + 1] = pack_frag<T>(x + 8);
         }
 #pragma unroll
-        for (int w = 0; w < BN / 16; ++w)
+        for (int w = 0; w < 2 * U; ++w)
 #pragma unroll
-            for (int c = 0; c < CT; ++c) {
-                const Frag<T> vf = VT::col_frag(vcol, vt, 16 * w, c);
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) acc[n][c] = mma(vf, p[n][w], acc[n][c]);
-            }
+            for (int c = 0; c < CT; ++c) acc[c] = mma(VT::col_frag(vcol, base0 + at, 16 * w, c), p[w], acc[c]);
+    };
+    if (t0 < t1) stage(t0 * BN, lds);
+    for (int t = t0; t < t1; t += 2) {
+        tiles::wait_lds_loads();
+        __syncthreads();
+        if (t + 1 < t1) stage((t + 1) * BN, lds + kStage);
+        if (t * BN < wend) keys(t * BN, std::integral_constant<int, 0>{});
+        if (t + 1 >= t1) break;
+        tiles::wait_lds_loads();
+        __syncthreads();
+        if (t + 2 < t1) stage((t + 2) * BN, lds);
+        if ((t + 1) * BN < wend) keys((t + 1) * BN, std::integral_constant<int, 1>{});
     }
+    sum += other_half(sum);
 
-    // the second map's normalised result goes to the first map's wave of the same rows, lane by lane
-    float* const box = reinterpret_cast<float*>(lds_raw) + rb * (CT * 16 * 64);
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const float total = sum[n] + other_half(sum[n]);
-        const float inv = total > 0.f ? 1.0f / total : 0.f;
-        const int r = row0 + rb * 32 * NQ + n * 32 + (lane & 31), h = g * G + qg[n];
-        const long long row = (static_cast<long long>(b) * a.Nq + qi[n]) * a.heads + h;
+    // results pass between waves of the same rows through LDS, lane by lane
+    constexpr int kBox = (CT * 16 + 2) * 64;
+    float* const boxes = reinterpret_cast<float*>(lds_raw);
+    if constexpr (KEYS) {
+        float* const box = boxes + map * kBox + lane;
         __syncthreads();
-        if (map == 1) {
+        if (kb == 1) {
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) box[(c * 16 + e) * 64 + lane] = acc[n][c][e] * inv;
+                for (int e = 0; e < 16; ++e) box[(c * 16 + e) * 64] = acc[c][e];
+            box[CT * 16 * 64] = mx;
+            box[(CT * 16 + 1) * 64] = sum;
         }
-        if (r < a.R && a.lse && half == 0)
-            a.lse[((static_cast<long long>(b) * a.heads + h) * 2 + map) * a.Nq + qi[n]] =
-                total > 0.f ? mx[n] + __builtin_amdgcn_logf(total) : -INFINITY;
         __syncthreads();
-        if (map == 0 && r < a.R) {
-            const float lam = diff_lambda(a, b, qi[n], h);
+        if (kb == 0) {
+            const float m1 = box[CT * 16 * 64], m = fmaxf(mx, m1), base = m == -INFINITY ? 0.f : m;
+            const float f0 = exp2_fast(mx - base), f1 = exp2_fast(m1 - base);
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
-                for (int e = 0; e < 16; e += 4) {
-                    float o1[4], o[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        o1[j] = box[(c * 16 + e + j) * 64 + lane];
-                        o[j] = acc[n][c][e + j] * inv - lam * o1[j];
-                    }
-                    const long long at = row * (2 * D) + 32 * c + acc_row(e, half);
-                    store4<T>(a.out, at, o[0], o[1], o[2], o[3]);
-                    if (a.out1) store4<T>(a.out1, at, o1[0], o1[1], o1[2], o1[3]);
-                }
+                for (int e = 0; e < 16; ++e) acc[c][e] = acc[c][e] * f0 + box[(c * 16 + e) * 64] * f1;
+            sum = sum * f0 + box[(CT * 16 + 1) * 64] * f1;
+            mx = m;
         }
     }
+    if (a.splits > 1) {
+        if (kb == 1 || rr >= a.R) return;
+        const long long at = (((static_cast<long long>(split) * a.B * a.kv_heads + bh) * 2 + map) * a.R + r);
+        if (half == 0) *reinterpret_cast<float2*>(a.part_sums + at * 2) = make_float2(mx, sum);
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4)
+                store4<float>(a.part, at * (2 * D) + 32 * c + acc_row(e, half), acc[c][e], acc[c][e + 1], acc[c][e + 2], acc[c][e + 3]);
+        return;
+    }
+    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+    const long long row = (static_cast<long long>(b) * a.Nq + qi) * a.heads + h;
+    float* const box = boxes + rb * kBox + lane;
+    __syncthreads();
+    if (map == 1 && kb == 0) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) box[(c * 16 + e) * 64] = acc[c][e] * inv;
+    }
+    if (rr < a.R && a.lse && half == 0 && kb == 0)
+        a.lse[((static_cast<long long>(b) * a.heads + h) * 2 + map) * a.Nq + qi] =
+            sum > 0.f ? mx + __builtin_amdgcn_logf(sum) : -INFINITY;
+    __syncthreads();
+    if (map == 1 || kb == 1 || rr >= a.R) return;
+    const float lam = diff_lambda(a, b, qi, h);
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            float o1[4], o[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                o1[j] = box[(c * 16 + e + j) * 64];
+                o[j] = acc[c][e + j] * inv - lam * o1[j];
+            }
+            const long long at = row * (2 * D) + 32 * c + acc_row(e, half);
+            store4<T>(a.out, at, o[0], o[1], o[2], o[3]);
+            if (a.out1) store4<T>(a.out1, at, o1[0], o1[1], o1[2], o1[3]);
+        }
 }
 
-template <typename T, int D, int NQ, int BN>
+// The parts' results joined: four channels of one row a thread, its maxima first.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffArgs a)
+{
+    constexpr int LPR = D / 2;                              // threads of a row
+    const long long item = (static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / LPR;
+    const int c = 4 * (threadIdx.x % LPR);
+    const long long rows = static_cast<long long>(a.B) * a.kv_heads * a.R;
+    if (item >= rows) return;
+    const long long bh = item / a.R;
+    const int r = static_cast<int>(item - bh * a.R), G = a.heads / a.kv_heads;
+    const int b = static_cast<int>(bh / a.kv_heads), qi = fast_div(r, a.div_G);
+    const int h = static_cast<int>(bh - static_cast<long long>(b) * a.kv_heads) * G + r - qi * G;
+    const long long step = 2 * rows;
+    f32x4 o[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+        const long long at = (bh * 2 + m) * a.R + r;
+        const float2* const ms = reinterpret_cast<const float2*>(a.part_sums) + at;
+        const f32x4* const x = reinterpret_cast<const f32x4*>(a.part + at * (2 * D) + c);
+        float top = -INFINITY;
+        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ms[s * step].x);
+        const float base = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+        f32x4 y{};
+#pragma unroll 4
+        for (int s = 0; s < a.splits; ++s) {
+            const float2 v = ms[s * step];
+            const float f = exp2_fast(v.x - base);
+            sum = fmaf(v.y, f, sum);
+            y += x[s * step * (D / 2)] * f;
+        }
+        o[m] = y * (sum > 0.f ? 1.0f / sum : 0.f);
+        if (a.lse && c == 0)
+            a.lse[((static_cast<long long>(b) * a.heads + h) * 2 + m) * a.Nq + qi] = sum > 0.f ? top + __builtin_amdgcn_logf(sum) : -INFINITY;
+    }
+    const float lam = diff_lambda(a, b, qi, h);
+    const long long at = ((static_cast<long long>(b) * a.Nq + qi) * a.heads + h) * (2 * D) + c;
+    store4<T>(a.out, at, o[0][0] - lam * o[1][0], o[0][1] - lam * o[1][1], o[0][2] - lam * o[1][2], o[0][3] - lam * o[1][3]);
+    if (a.out1) store4<T>(a.out1, at, o[1][0], o[1][1], o[1][2], o[1][3]);
+}
+
+template <typename T, int D, int BN, bool KEYS>
 hipError_t launch_fwd(const DiffArgs& a, hipStream_t stream)
 {
     static std::atomic<unsigned long long> configured{0};
+    constexpr int BM = KEYS ? 32 : 64;
     constexpr int stage = BN * 4 * D * static_cast<int>(sizeof(T));
-    constexpr int box = 2 * (2 * D / 32) * 16 * 64 * 4;
-    constexpr int lds = 2 * stage > box ? 2 * stage : box;
-    const void* fn = reinterpret_cast<const void*>(&diff_fwd_kernel<T, D, NQ, BN>);
+    constexpr int boxes = 2 * (2 * D / 32 * 16 + 2) * 64 * 4;
+    constexpr int lds = 2 * stage > boxes ? 2 * stage : boxes;
+    const void* fn = reinterpret_cast<const void*>(&diff_fwd_kernel<T, D, BN, KEYS>);
     const hipError_t e = set_max_lds_once(fn, configured);
     if (e != hipSuccess) return e;
-    const long long blocks = static_cast<long long>((a.R + 64 * NQ - 1) / (64 * NQ)) * a.B * a.kv_heads;
-    if (blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((diff_fwd_kernel<T, D, NQ, BN>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), lds, stream, a);
+    const long long groups = static_cast<long long>(a.B) * a.kv_heads;
+    const long long blocks = (a.R + BM - 1) / BM * groups * a.splits;
+    const long long join = (groups * a.R * (D / 2) + kThreads - 1) / kThreads;
+    if (blocks > 0x7FFFFFFFLL || join > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((diff_fwd_kernel<T, D, BN, KEYS>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), lds, stream, a);
+    if (a.splits > 1)
+        hipLaunchKernelGGL((diff_join_kernel<T, D>), dim3(static_cast<unsigned>(join)), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch_type(const DiffArgs& a, hipStream_t stream)
+{
+    if (a.keys_apart) return launch_fwd<T, D, 64, true>(a, stream);
+    return launch_fwd<T, D, sizeof(T) == 2 ? 64 : 32, false>(a, stream);
 }
 
 }  // namespace
 
 hipError_t launch_diff_attn(const DiffArgs& a, int d, bool use_bf16, hipStream_t stream)
 {
-    if (use_bf16) return d == 32 ? launch_fwd<bf16, 32, 1, 64>(a, stream) : launch_fwd<bf16, 64, 1, 64>(a, stream);
-    return d == 32 ? launch_fwd<float, 32, 1, 32>(a, stream) : launch_fwd<float, 64, 1, 32>(a, stream);
+    if (use_bf16) return d == 32 ? launch_type<bf16, 32>(a, stream) : launch_type<bf16, 64>(a, stream);
+    return d == 32 ? launch_type<float, 32>(a, stream) : launch_type<float, 64>(a, stream);
 }
 
 }  // namespace qta

@@ -32,7 +32,8 @@ class DiffAttnArgs(ctypes.Structure):
 
 _SIGS.update({
     "qta_rotary": ([_P, _I, _I, _I, _I, _I, _I, _I, _I, _I, _I, _P, _P, _L, _I, _F, _P], _I),
-    "qta_diff_attn": ([_P, _P, _P, _P, _P], _I),
+    "qta_diff_attn_workspace_bytes": ([_P], ctypes.c_size_t),
+    "qta_diff_attn": ([_P, _P, _P, _P, _P, ctypes.c_size_t, _P], _I),
     "qta_diff_attn_backward_workspace_bytes": ([_P], ctypes.c_size_t),
     "qta_diff_attn_backward": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, ctypes.c_size_t, _P], _I),
 })
@@ -240,8 +241,10 @@ def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, 
             lse.fill_(-math.inf)
     else:
         with _on(q):
-            _check("qta_diff_attn", lib().qta_diff_attn(ctypes.byref(args), _ptr(out), _ptr(out1), _ptr(lse),
-                                                        _stream(q.device)))
+            nbytes = lib().qta_diff_attn_workspace_bytes(ctypes.byref(args))
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes > 256 else None
+            _check("qta_diff_attn", lib().qta_diff_attn(ctypes.byref(args), _ptr(out), _ptr(out1), _ptr(lse), _ptr(ws),
+                                                        nbytes if nbytes > 256 else 0, _stream(q.device)))
     return (out, (out1, lse)) if keep else out
 
 

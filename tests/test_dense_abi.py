@@ -23,8 +23,8 @@ def diff_args(**kw):
     return DiffAttnArgs(**a)
 
 
-def forward(out=FAKE, out1=None, lse=None, **kw):
-    return P.lib().qta_diff_attn(ctypes.byref(diff_args(**kw)), out, out1, lse, None)
+def forward(out=FAKE, out1=None, lse=None, ws=None, nbytes=0, **kw):
+    return P.lib().qta_diff_attn(ctypes.byref(diff_args(**kw)), out, out1, lse, ws, nbytes, None)
 
 
 def backward(ws=FAKE, nbytes=0, heads_lam=1, kw={}, **p):
@@ -34,7 +34,7 @@ def backward(ws=FAKE, nbytes=0, heads_lam=1, kw={}, **p):
 
 
 def test_diff_attn_validation():
-    assert P.lib().qta_diff_attn(None, FAKE, None, None, None) == INVALID
+    assert P.lib().qta_diff_attn(None, FAKE, None, None, None, 0, None) == INVALID
     for n in ("q", "k", "v", "lam"):
         assert forward(**{n: None}) == INVALID, n
     for n in ("q", "k", "v"):
@@ -57,6 +57,22 @@ def test_diff_attn_validation():
     assert forward(k_token=1 << 24) == UNSUPPORTED and forward(v_token=1 << 24) == UNSUPPORTED
     assert forward(q_token=1 << 24) == UNSUPPORTED and forward(q_head=1 << 28) == UNSUPPORTED
     assert forward(Nq=1 << 27) == UNSUPPORTED and forward(Nk=1 << 29) == UNSUPPORTED
+
+
+def test_diff_attn_workspace():
+    """Few rows over many keys need room for their parts."""
+    size = P.lib().qta_diff_attn_workspace_bytes
+    long = dict(Nq=1, Nk=8192, k_batch=128 * 8192, v_batch=128 * 8192)
+    need = size(ctypes.byref(diff_args(**long)))
+    assert need > 256 and need % 256 == 0
+    assert size(ctypes.byref(diff_args())) == 256
+    assert forward(ws=FAKE, nbytes=need - 1, **long) == WORKSPACE
+    assert forward(**long) == WORKSPACE
+    assert forward(ws=None, nbytes=need, **long) == INVALID
+    assert forward(ws=FAKE + 16, nbytes=need, **long) == INVALID
+    for kw in (dict(B=0), dict(d=48), dict(heads=3), dict(dtype=7)):
+        assert size(ctypes.byref(diff_args(**kw))) == 0
+    assert size(None) == 0
 
 
 def test_diff_attn_backward_validation():
