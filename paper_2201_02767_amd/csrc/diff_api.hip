@@ -86,7 +86,7 @@ FwdLayout fwd_layout(const qta_diff_attn_args* a)
 {
     FwdLayout L{};
     const int R = a->Nq * (a->heads / a->kv_heads);
-    L.parts = diff_key_parts(a->B, a->kv_heads, a->Nk, R);
+    L.parts = diff_key_parts(a->B, a->kv_heads, a->Nk, R, a->dtype == QTA_BF16);
     if (L.parts.splits == 1) return L;
     const size_t rows = static_cast<size_t>(L.parts.splits) * a->B * a->kv_heads * 2 * R;
     L.part_sums = align_up(rows * 2 * a->d * sizeof(float));

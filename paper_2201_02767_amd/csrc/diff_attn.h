@@ -47,15 +47,15 @@ struct DiffParts {
     bool keys_apart;
     int splits;
 };
-inline DiffParts diff_key_parts(int B, int kv_heads, int Nk, int R)
+inline DiffParts diff_key_parts(int B, int kv_heads, int Nk, int R, bool bf16_inputs)
 {
     const long long groups = static_cast<long long>(B) * kv_heads, cus = device_cu_count();
     DiffParts p{false, 1};
     const long long tiles = groups * ((R + 63) / 64);
-    if (tiles >= cus && R > 32) return p;
+    if (tiles >= (bf16_inputs ? cus : 2 * cus) && R > 32) return p;
     p.keys_apart = R <= 32;
     const long long work = groups * ((R + (p.keys_apart ? 31 : 63)) / (p.keys_apart ? 32 : 64));
-    const long long want = (4 * cus + work - 1) / work, most = Nk / 128;
+    const long long want = (4 * cus + work - 1) / work, most = Nk / 256;
     p.splits = static_cast<int>(most < 1 ? 1 : want < 1 ? 1 : want > most ? most : want);
     if (p.splits > 64) p.splits = 64;
     return p;
@@ -251,6 +251,9 @@ struct Tile {
         return f;
     }
 };
+
+// Stands in a branch that few tiles take, which the compiler would otherwise turn into selects that all of them take.
+__device__ __forceinline__ void branch_here() { asm volatile(""); }
 
 // Keeps a lane's base from being known across iterations: the compiler would otherwise hold every variant of it in a
 // register of its own (32 of them in the key pass).

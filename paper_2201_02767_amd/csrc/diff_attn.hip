@@ -24,14 +24,14 @@ constexpr float kLag = 8.0f;
 // keys, two of them in LDS. With a.splits > 1 a workgroup takes one part of its rows' keys and leaves the results as they
 // are, with their maxima and sums, to diff_join_kernel.
 template <typename T, int D, int BN, bool KEYS>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_fwd_kernel(DiffArgs a)
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (KEYS ? 2 : 4) : 1) void diff_fwd_kernel(DiffArgs a)
 {
     using KT = Tile<T, D>;
     using VT = Tile<T, 2 * D>;
     constexpr int ES = sizeof(T), CT = 2 * D / 32, BM = KEYS ? 32 : 64, U = KEYS ? BN / 64 : BN / 32;   // 32-key blocks of a wave
     constexpr int kK = KT::bytes(BN), kStage = 2 * kK + VT::bytes(BN);
     static_assert(U >= 1, "a block of keys for every wave");
-    extern __shared__ __align__(16) unsigned char lds_raw[];
+    extern __shared__ __align__(1024) unsigned char lds_raw[];
     lds_byte* const lds = (lds_byte*)lds_raw;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -71,12 +71,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_fwd_ker
     };
 
     // this wave's keys, and this workgroup's part of the tiles
-    const int wend = rr - (lane & 31) < a.R ? range.limit(fast_div(min(row0 + rb * 32 + 32, a.R) - 1, a.div_G)) : 0;
+    const int wend = row0 + rb * 32 < a.R ? range.limit(fast_div(min(row0 + rb * 32 + 32, a.R) - 1, a.div_G)) : 0;
     const int all = (kend + BN - 1) / BN;
     const int t0 = static_cast<int>(static_cast<long long>(all) * split / a.splits);
     const int t1 = static_cast<int>(static_cast<long long>(all) * (split + 1) / a.splits);
-    const uint32_t base0 = lds_address(lds), krow = KT::row_base(lane) + map * kK + kb * (BN / 2) * KT::kRow,
-                   vcol = VT::col_base(lane) + 2 * kK + kb * (BN / 2) * VT::kRow;
+    // (whole rows are added, so that the bases keep their bits below)
+    const uint32_t krow = lds_address(lds) + KT::row_base(lane) + map * kK + kb * (BN / 2) * KT::kRow,
+                   vcol = lds_address(lds) + VT::col_base(lane) + 2 * kK + kb * (BN / 2) * VT::kRow;
     auto keys = [&](int k0, auto odd) {
         constexpr uint32_t at = odd.value * kStage;
         f32x16 s[U];
@@ -84,9 +85,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_fwd_ker
         for (int u = 0; u < U; ++u) {
             s[u] = f32x16{};
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) s[u] = mma(KT::row_frag(krow, base0 + at, 32 * u, c), qf[c], s[u]);
+            for (int c = 0; c < D / 16; ++c) s[u] = mma(KT::row_frag(krow, at, 32 * u, c), qf[c], s[u]);
         }
         if (k0 + BN > kmask) {
+            branch_here();
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_fwd_ker
 #pragma unroll
         for (int w = 0; w < 2 * U; ++w)
 #pragma unroll
-            for (int c = 0; c < CT; ++c) acc[c] = mma(VT::col_frag(vcol, base0 + at, 16 * w, c), p[w], acc[c]);
+            for (int c = 0; c < CT; ++c) acc[c] = mma(VT::col_frag(vcol, at, 16 * w, c), p[w], acc[c]);
     };
     if (t0 < t1) stage(t0 * BN, lds);
     for (int t = t0; t < t1; t += 2) {
@@ -209,46 +211,52 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_fwd_ker
         }
 }
 
-// The parts' results joined: four channels of one row a thread, its maxima first.
+// The parts' results joined: a wave a row, lane s holding the maxima and sums of part s (at most 64), every lane D / 32
+// channels of both maps.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffArgs a)
 {
-    constexpr int LPR = D / 2;                              // threads of a row
-    const long long item = (static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / LPR;
-    const int c = 4 * (threadIdx.x % LPR);
+    constexpr int V = D / 32;
+    typedef float piece __attribute__((ext_vector_type(V)));
+    const int lane = threadIdx.x & 63;
     const long long rows = static_cast<long long>(a.B) * a.kv_heads * a.R;
+    const long long item = static_cast<long long>(blockIdx.x) * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= rows) return;
-    const long long bh = item / a.R;
-    const int r = static_cast<int>(item - bh * a.R), G = a.heads / a.kv_heads;
-    const int b = static_cast<int>(bh / a.kv_heads), qi = fast_div(r, a.div_G);
-    const int h = static_cast<int>(bh - static_cast<long long>(b) * a.kv_heads) * G + r - qi * G;
+    const int bh = static_cast<int>(item / a.R);
+    const int r = static_cast<int>(item - static_cast<long long>(bh) * a.R), G = a.heads / a.kv_heads;
+    const int b = bh / a.kv_heads, qi = fast_div(r, a.div_G), h = (bh - b * a.kv_heads) * G + r - qi * G;
     const long long step = 2 * rows;
-    f32x4 o[2];
+    float f[2], inv[2], top[2], sum[2];
+    const float* x[2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-        const long long at = (bh * 2 + m) * a.R + r;
-        const float2* const ms = reinterpret_cast<const float2*>(a.part_sums) + at;
-        const f32x4* const x = reinterpret_cast<const f32x4*>(a.part + at * (2 * D) + c);
-        float top = -INFINITY;
-        for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ms[s * step].x);
-        const float base = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
-        f32x4 y{};
-#pragma unroll 4
-        for (int s = 0; s < a.splits; ++s) {
-            const float2 v = ms[s * step];
-            const float f = exp2_fast(v.x - base);
-            sum = fmaf(v.y, f, sum);
-            y += x[s * step * (D / 2)] * f;
-        }
-        o[m] = y * (sum > 0.f ? 1.0f / sum : 0.f);
-        if (a.lse && c == 0)
-            a.lse[((static_cast<long long>(b) * a.heads + h) * 2 + m) * a.Nq + qi] = sum > 0.f ? top + __builtin_amdgcn_logf(sum) : -INFINITY;
+        const long long at = (static_cast<long long>(bh) * 2 + m) * a.R + r;
+        const float2 ms = lane < a.splits ? reinterpret_cast<const float2*>(a.part_sums)[at + lane * step] : make_float2(-INFINITY, 0.f);
+        top[m] = wave_max_fast(ms.x);
+        f[m] = exp2_fast(ms.x - (top[m] == -INFINITY ? 0.f : top[m]));
+        sum[m] = wave_sum_fast(ms.y * f[m]);
+        inv[m] = sum[m] > 0.f ? 1.0f / sum[m] : 0.f;
+        x[m] = a.part + at * (2 * D) + lane * V;
     }
+    piece o[2] = {};
+#pragma unroll 8
+    for (int s = 0; s < a.splits; ++s)
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+            o[m] += *reinterpret_cast<const piece*>(x[m] + s * step * (2 * D)) *
+                    __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f[m]), s));
     const float lam = diff_lambda(a, b, qi, h);
-    const long long at = ((static_cast<long long>(b) * a.Nq + qi) * a.heads + h) * (2 * D) + c;
-    store4<T>(a.out, at, o[0][0] - lam * o[1][0], o[0][1] - lam * o[1][1], o[0][2] - lam * o[1][2], o[0][3] - lam * o[1][3]);
-    if (a.out1) store4<T>(a.out1, at, o[1][0], o[1][1], o[1][2], o[1][3]);
+    const long long row = (static_cast<long long>(b) * a.Nq + qi) * a.heads + h;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const float o1 = o[1][v] * inv[1];
+        Storage<T>::store1(a.out, row * (2 * D) + lane * V + v, o[0][v] * inv[0] - lam * o1);
+        if (a.out1) Storage<T>::store1(a.out1, row * (2 * D) + lane * V + v, o1);
+    }
+    if (a.lse && lane < 2) {
+        const float t = lane ? top[1] : top[0], z = lane ? sum[1] : sum[0];
+        a.lse[((static_cast<long long>(b) * a.heads + h) * 2 + lane) * a.Nq + qi] = z > 0.f ? t + __builtin_amdgcn_logf(z) : -INFINITY;
+    }
 }
 
 template <typename T, int D, int BN, bool KEYS>
@@ -264,7 +272,7 @@ hipError_t launch_fwd(const DiffArgs& a, hipStream_t stream)
     if (e != hipSuccess) return e;
     const long long groups = static_cast<long long>(a.B) * a.kv_heads;
     const long long blocks = (a.R + BM - 1) / BM * groups * a.splits;
-    const long long join = (groups * a.R * (D / 2) + kThreads - 1) / kThreads;
+    const long long join = (groups * a.R + kThreads / kWave - 1) / (kThreads / kWave);
     if (blocks > 0x7FFFFFFFLL || join > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     hipLaunchKernelGGL((diff_fwd_kernel<T, D, BN, KEYS>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), lds, stream, a);
     if (a.splits > 1)
@@ -276,7 +284,7 @@ template <typename T, int D>
 hipError_t launch_type(const DiffArgs& a, hipStream_t stream)
 {
     if (a.keys_apart) return launch_fwd<T, D, 64, true>(a, stream);
-    return launch_fwd<T, D, sizeof(T) == 2 ? 64 : 32, false>(a, stream);
+    return launch_fwd<T, D, sizeof(T) == 2 && D == 32 ? 64 : 32, false>(a, stream);
 }
 
 }  // namespace

@@ -11,6 +11,7 @@
 // -lse / scale: a weight is then one product and one power of two away. t_m comes from the stored, rounded O and O_1; the rows of P_1 (D - t_1), which
 // with the exact t_1 sum to zero, give what is missing, and dlambda is exact to fp32.
 #include <atomic>
+#include <type_traits>
 
 #include "diff_attn.h"
 
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
     using VT = Tile<T, 2 * D>;
     constexpr int ES = sizeof(T), BM = 128;
     constexpr int kK = KT::bytes(BN), kStage = 2 * kK + VT::bytes(BN);
-    extern __shared__ __align__(16) unsigned char lds_raw[];
+    extern __shared__ __align__(1024) unsigned char lds_raw[];
     lds_byte* const lds = (lds_byte*)lds_raw;
     const DiffArgs& f = a.f;
 
@@ -150,22 +151,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
     };
 
     const int wend = row0 + wave * 32 < f.R ? range.limit(fast_div(min(row0 + wave * 32 + 32, f.R) - 1, f.div_G)) : 0;
-    const uint32_t base0 = lds_address(lds);
-    uint32_t krow = KT::row_base(lane), kcol = KT::col_base(lane), vrow = VT::row_base(lane);
-    const int nt = (kend + BN - 1) / BN;
-    if (nt > 0) stage(0, lds);
-    for (int t = 0; t < nt; ++t) {
-        const int k0 = t * BN;
-        const uint32_t k0t = base0 + (t & 1) * kStage, k1t = k0t + kK, vt = k0t + 2 * kK;
-        tiles::wait_lds_loads();
-        __syncthreads();
-        if (t + 1 < nt) stage(k0 + BN, lds + ((t + 1) & 1) * kStage);
+    const uint32_t krow = lds_address(lds) + KT::row_base(lane), kcol = lds_address(lds) + KT::col_base(lane),
+                   vrow = lds_address(lds) + VT::row_base(lane);
+    auto keys = [&](int k0, auto odd) {
+        constexpr uint32_t k0t = odd.value * kStage, k1t = k0t + kK, vt = k0t + 2 * kK;
 #pragma unroll
         for (int u = 0; u < BN / 32; ++u) {
             if (k0 + 32 * u >= wend) break;
-            opaque(krow);
-            opaque(kcol);
-            opaque(vrow);
             f32x16 s0{}, s1{}, dp;
 #pragma unroll
             for (int e = 0; e < 16; ++e) dp[e] = nt0;
@@ -183,6 +175,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
                 d1[e] = exp2_fast(fmaf(s1[e], f.scale, nlse1)) * (dp[e] + t01);
             }
             if (k0 + 32 * u + 32 > kmask) {
+                branch_here();
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
                     if (k0 + 32 * u + acc_row(e, half) >= lim) {
@@ -205,6 +198,19 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
                 }
             }
         }
+    };
+    const int nt = (kend + BN - 1) / BN;
+    if (nt > 0) stage(0, lds);
+    for (int t = 0; t < nt; t += 2) {
+        tiles::wait_lds_loads();
+        __syncthreads();
+        if (t + 1 < nt) stage((t + 1) * BN, lds + kStage);
+        keys(t * BN, std::integral_constant<int, 0>{});
+        if (t + 1 >= nt) break;
+        tiles::wait_lds_loads();
+        __syncthreads();
+        if (t + 2 < nt) stage((t + 2) * BN, lds);
+        keys((t + 1) * BN, std::integral_constant<int, 1>{});
     }
     miss += other_half(miss);
     if (rr >= f.R) return;
@@ -236,7 +242,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
     using OT = Tile<T, 2 * D>;
     constexpr int ES = sizeof(T), BM = 32, BN = kDiffKeys;
     constexpr int kQ = QT::bytes(BM), kO = OT::bytes(BM), kStats = 1024, kStage = 2 * kQ + kO + kStats;
-    extern __shared__ __align__(16) unsigned char lds_raw[];
+    extern __shared__ __align__(1024) unsigned char lds_raw[];
     lds_byte* const lds = (lds_byte*)lds_raw;
     lds_byte* const vt = lds + 2 * kStage;
     const DiffArgs& f = a.f;
@@ -366,6 +372,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
                     }
                 }
                 if (edge) {
+                    branch_here();
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int r = r0 + acc_row(e, half);
@@ -441,7 +448,7 @@ template <typename T, int D>
 hipError_t launch_bwd(const DiffBwdArgs& a, hipStream_t stream)
 {
     static std::atomic<unsigned long long> configured_q{0}, configured_k{0};
-    constexpr int ES = static_cast<int>(sizeof(T)), BN = ES == 2 ? 64 : 32;
+    constexpr int ES = static_cast<int>(sizeof(T)), BN = 32;
     const long long bh = static_cast<long long>(a.f.B) * a.f.kv_heads;
     constexpr int lpr = 2 * D * ES / 16;
     const long long rblocks = (bh * a.Rpad * lpr + kThreads - 1) / kThreads;

@@ -6,13 +6,13 @@ contiguous and, on a map, its rows follow each other at one distance.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 
 import torch
+from torch._C import _cuda_getCurrentRawStream as _raw_stream      # (torch.cuda.current_stream: 2 us a call)
 
-from .qta import _DTYPES, _SIGS, _check, _dtype_code, _ptr, _scale, _stream, lib
+from .qta import _DTYPES, _SIGS, _check, _dtype_code, _scale, lib
 
 _P, _I, _F, _L = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_int64
 
@@ -45,7 +45,7 @@ def _tokens(t, name, like=None):
         raise TypeError(f"{name} must be a tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a GPU")
-    if like is not None and (t.device != like.device or t.dtype != like.dtype):
+    if like is not None and (t.dtype is not like.dtype or t.device != like.device):
         raise ValueError(f"{name} must be {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
     shape, st = t.shape, t.stride()
     if len(shape) not in (4, 5):
@@ -63,20 +63,26 @@ def _tokens(t, name, like=None):
             st[-2] if shape[-2] > 1 else 0)
 
 
-def _int32(t, name, like, shapes):
-    if t is None:
-        return
+def _int32(t, name, like, *shapes):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a tensor")
-    if t.dtype != torch.int32 or t.device != like.device or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.device != like.device or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous torch.int32 on {like.device}")
-    if tuple(t.shape) not in shapes:
+    if t.shape not in shapes:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {' or '.join(str(s) for s in shapes)}")
+    return t.data_ptr()
 
 
-def _on(t):
-    """The device of `t` made current for a call (kernels are launched on the current one)."""
-    return contextlib.nullcontext() if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+def _call(name, t, *args):
+    """The library's function on t's device, which is made current for it, and on torch's current stream there."""
+    dev = t.get_device()
+    if dev == torch.cuda.current_device():
+        status = getattr(lib(), name)(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            status = getattr(lib(), name)(*args, _raw_stream(dev))
+    if status:
+        _check(name, status)
 
 
 # ------------------------------------------------------------------------------------------------
@@ -110,17 +116,22 @@ def _rotate(xs, freqs, pos, axes, interleaved, scale, start, inverse, inplace=Fa
     for t, s in zip(xs[1:], shapes[1:]):
         if t.shape[:-2] != x.shape[:-2] or s[3] != d:
             raise ValueError(f"k has shape {tuple(t.shape)}, x {tuple(x.shape)}: only the heads may differ")
-    code = _dtype_code(x)
+    code = _DTYPES.get(x.dtype)
+    if code is None:
+        _dtype_code(x)
     axes = (2 if x.dim() == 5 else 1) if axes is None else axes
     if not isinstance(freqs, torch.Tensor):
         raise TypeError("freqs must be a tensor")
-    if freqs.dtype != torch.float64 or freqs.device != x.device or freqs.dim() != 1 or not freqs.is_contiguous():
+    if freqs.dtype is not torch.float64 or freqs.device != x.device or freqs.dim() != 1 or not freqs.is_contiguous():
         raise ValueError(f"freqs must be a contiguous torch.float64 vector on {x.device}")
-    _int32(pos, "pos", x, {(N,), (B, N)} if axes == 1 else {(N, 2), (B, N, 2)})
-    if pos is None and axes == 2 and x.dim() != 5:
+    at, pos_batch = None, 0
+    if pos is not None:
+        if start != 0:
+            raise ValueError("start goes with positions that are counted, not with given ones")
+        at = _int32(pos, "pos", x, *(((N,), (B, N)) if axes == 1 else ((N, 2), (B, N, 2))))
+        pos_batch = N * axes if pos.dim() > axes else 0
+    elif axes == 2 and x.dim() != 5:
         raise ValueError("two axes need a map or given positions")
-    if pos is not None and start != 0:
-        raise ValueError("start goes with positions that are counted, not with given ones")
     if inplace:
         # (a broadcast axis has all its entries in one place)
         if any(n > 1 and s == 0 for t in xs for n, s in zip(t.shape, t.stride())):
@@ -128,20 +139,13 @@ def _rotate(xs, freqs, pos, axes, interleaved, scale, start, inverse, inplace=Fa
         ys = xs
     else:
         ys = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs]
-    if x.numel() == 0 and all(t.numel() == 0 for t in xs):
+    if B == 0 or N == 0 or all(t.numel() == 0 for t in xs):
         return ys
-    table = (RotaryTensor * len(xs))()
-    for e, t, y, s in zip(table, xs, ys, shapes):
-        o = s if inplace else _tokens(y, "y")
-        e.x, e.y, e.heads = t.data_ptr(), y.data_ptr(), s[2]
-        e.x_batch, e.x_token, e.x_head = s[4:]
-        e.y_batch, e.y_token, e.y_head = o[4:]
-    shared = pos is not None and pos.dim() == axes
-    with _on(x):
-        _check("qta_rotary", lib().qta_rotary(
-            ctypes.addressof(table), len(xs), B, N, d, 2 * freqs.numel(), axes, x.shape[2] if x.dim() == 5 else 0,
-            int(interleaved), int(inverse), code, _ptr(freqs), _ptr(pos), 0 if pos is None or shared else N * axes,
-            start, scale, _stream(x.device)))
+    table = (RotaryTensor * len(xs))(*[
+        RotaryTensor(t.data_ptr(), y.data_ptr(), s[2], *s[4:], *(s[4:] if inplace else (N * s[2] * d, s[2] * d, d)))
+        for t, y, s in zip(xs, ys, shapes)])
+    _call("qta_rotary", x, ctypes.addressof(table), len(xs), B, N, d, 2 * freqs.numel(), axes,
+          x.shape[2] if x.dim() == 5 else 0, interleaved, inverse, code, freqs.data_ptr(), at, pos_batch, start, scale)
     return ys
 
 
@@ -191,7 +195,9 @@ def _diff_args(q, k, v, lam, scale, causal, lens, q_pos):
     B, Nq, h2, d, qb, qn, qh = _tokens(q, "q")
     Bk, Nk, k2, dk, kb, kn, kh = _tokens(k, "k", q)
     Bv, Nv, kv, dv, vb, vn, vh = _tokens(v, "v", q)
-    code = _dtype_code(q)
+    code = _DTYPES.get(q.dtype)
+    if code is None:
+        _dtype_code(q)
     if h2 % 2 or k2 != 2 * kv or kv == 0 or (h2 // 2) % kv:
         raise ValueError(f"q has {h2} and k {k2} heads and v {kv}: two for each head, and a multiple of v's, are needed")
     if (Bk, Bv, Nv, dk, dv) != (B, B, Nk, d, 2 * d):
@@ -199,23 +205,32 @@ def _diff_args(q, k, v, lam, scale, causal, lens, q_pos):
     heads = h2 // 2
     if not isinstance(lam, torch.Tensor):
         raise TypeError("lam must be a tensor")
-    if lam.device != q.device or lam.dtype not in (torch.float32, q.dtype):
+    if lam.dtype not in (torch.float32, q.dtype) or lam.device != q.device:
         raise ValueError(f"lam must be torch.float32 or {q.dtype} on {q.device}")
-    if tuple(lam.shape) == (heads,):
-        ls = (0, 0, lam.stride(0))
+    if lam.shape == (heads,):
+        lb, ln, lh = 0, 0, lam.stride(0)
     elif lam.shape == (*q.shape[:-2], heads):
-        ls = _tokens(lam.unsqueeze(-1), "lam")[4:]
+        lb, ln, lh = _tokens(lam.unsqueeze(-1), "lam")[4:]
     else:
         raise ValueError(f"lam has shape {tuple(lam.shape)}, expected {(heads,)} or {(*q.shape[:-2], heads)}")
-    _int32(lens, "lens", q, {(B,)})
-    _int32(q_pos, "q_pos", q, {(B,)})
     if q_pos is not None and not causal:
         raise ValueError("q_pos goes with causal=True")
-    ptr = lambda t: None if t is None else t.data_ptr()
     args = DiffAttnArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(), B, heads, kv, Nq, Nk, d, code,
-                        _DTYPES[lam.dtype], qb, qn, qh, kb, kn, kh, vb, vn, vh, *ls, ptr(lens), ptr(q_pos),
-                        int(bool(causal)), _scale(scale))
+                        _DTYPES[lam.dtype], qb, qn, qh, kb, kn, kh, vb, vn, vh, lb, ln, lh,
+                        None if lens is None else _int32(lens, "lens", q, (B,)),
+                        None if q_pos is None else _int32(q_pos, "q_pos", q, (B,)), bool(causal), _scale(scale))
     return args, (*q.shape[:-2], heads, 2 * d)
+
+
+def _workspace(name, args, like):
+    """Device memory for a call, or nothing where the library needs none (it then asks for 256 bytes)."""
+    dev = like.get_device()
+    if dev == torch.cuda.current_device():
+        n = getattr(lib(), name)(ctypes.byref(args))
+    else:
+        with torch.cuda.device(dev):
+            n = getattr(lib(), name)(ctypes.byref(args))
+    return (torch.empty(n, dtype=torch.uint8, device=like.device), n) if n > 256 else (None, 0)
 
 
 def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, keep=False):
@@ -234,17 +249,15 @@ def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, 
     if keep:
         out1 = torch.empty_like(out)
         lse = torch.empty((args.B, args.heads, 2, args.Nq), dtype=torch.float32, device=q.device)
-    if out.numel() == 0 or args.Nk == 0:
+    if args.Nk == 0 or out.numel() == 0:
         out.zero_()
         if keep:
             out1.zero_()
             lse.fill_(-math.inf)
     else:
-        with _on(q):
-            nbytes = lib().qta_diff_attn_workspace_bytes(ctypes.byref(args))
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes > 256 else None
-            _check("qta_diff_attn", lib().qta_diff_attn(ctypes.byref(args), _ptr(out), _ptr(out1), _ptr(lse), _ptr(ws),
-                                                        nbytes if nbytes > 256 else 0, _stream(q.device)))
+        ws, nbytes = _workspace("qta_diff_attn_workspace_bytes", args, q)
+        _call("qta_diff_attn", q, ctypes.byref(args), out.data_ptr(), out1.data_ptr() if keep else None,
+              lse.data_ptr() if keep else None, None if ws is None else ws.data_ptr(), nbytes)
     return (out, (out1, lse)) if keep else out
 
 
@@ -254,19 +267,16 @@ def diff_attn_backward(q, k, v, lam, out, kept, dout, *, scale=None, causal=Fals
     args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
     out1, lse = kept
     for t, n in ((out, "out"), (out1, "kept"), (dout, "dout")):
-        if t.dtype != q.dtype or t.device != q.device or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        if t.dtype is not q.dtype or t.device != q.device or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{n} must be contiguous {q.dtype} {tuple(shape)} on {q.device}")
-    if tuple(lse.shape) != (args.B, args.heads, 2, args.Nq) or lse.dtype != torch.float32 or not lse.is_contiguous():
+    if lse.shape != (args.B, args.heads, 2, args.Nq) or lse.dtype is not torch.float32 or not lse.is_contiguous():
         raise ValueError("kept is not what diff_attn returned for these shapes")
     grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v, lam)]
     if out.numel() == 0 or args.Nk == 0:
         return tuple(g.zero_() for g in grads)
-    with _on(q):
-        ws = torch.empty(lib().qta_diff_attn_backward_workspace_bytes(ctypes.byref(args)), dtype=torch.uint8,
-                         device=q.device)
-        _check("qta_diff_attn_backward", lib().qta_diff_attn_backward(
-            ctypes.byref(args), _ptr(out), _ptr(out1), _ptr(lse), _ptr(dout), *[_ptr(g) for g in grads],
-            int(lam.dim() == 1), _ptr(ws), ws.numel(), _stream(q.device)))
+    ws, nbytes = _workspace("qta_diff_attn_backward_workspace_bytes", args, q)
+    _call("qta_diff_attn_backward", q, ctypes.byref(args), out.data_ptr(), out1.data_ptr(), lse.data_ptr(),
+          dout.data_ptr(), *[g.data_ptr() for g in grads], lam.dim() == 1, ws.data_ptr(), nbytes)
     return tuple(grads)
 
 
