@@ -96,8 +96,8 @@ FwdLayout fwd_layout(const qta_diff_attn_args* a)
 
 // Regions of the backward's workspace.
 struct BwdLayout {
-    size_t stats, dlam_rows, part, total;
-    int Rpad, splits;
+    size_t stats, dlam_rows, part, q_part, q_miss, total;
+    int Rpad, splits, q_splits;
 };
 BwdLayout bwd_layout(const qta_diff_attn_args* a, bool lam_heads)
 {
@@ -110,6 +110,14 @@ BwdLayout bwd_layout(const qta_diff_attn_args* a, bool lam_heads)
     L.splits = diff_key_splits(a->B, a->kv_heads, a->Nk, R, a->causal != 0);
     L.part = off;
     if (L.splits > 1) off = align_up(off + static_cast<size_t>(L.splits) * a->B * a->Nk * a->kv_heads * 4 * a->d * sizeof(float));
+    L.q_splits = diff_query_splits(a->B, a->kv_heads, a->Nk, R);
+    if (L.q_splits > 1) {
+        const size_t rows = static_cast<size_t>(L.q_splits) * a->B * a->kv_heads * R;
+        L.q_part = off;
+        off = align_up(off + rows * 2 * a->d * sizeof(float));
+        L.q_miss = off;
+        off = align_up(off + rows * sizeof(float));
+    }
     L.total = off;
     return L;
 }
@@ -181,6 +189,9 @@ qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const void* ou
     a.grad_scale = a.f.scale * kDiffLn2;
     a.splits = L.splits;
     a.part = reinterpret_cast<float*>(ws + L.part);
+    a.q_splits = L.q_splits;
+    a.q_part = reinterpret_cast<float*>(ws + L.q_part);
+    a.q_miss = reinterpret_cast<float*>(ws + L.q_miss);
     return launch_diff_bwd(a, args->d, args->dtype == QTA_BF16, static_cast<hipStream_t>(stream)) == hipSuccess ? QTA_OK : QTA_ERR_HIP;
 }
 

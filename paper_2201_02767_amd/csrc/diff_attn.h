@@ -301,6 +301,11 @@ struct DiffBwdArgs {
     // the key pass in `splits` parts of the rows: fp32 [splits][B][Nk][kv_heads][4d] sums of dK_0, dK_1 and dV (splits > 1)
     int splits;
     float* part;
+    // the query pass in `q_splits` parts of the keys: fp32 [q_splits][B][kv_heads][R][2][d] sums of dQ_0 and dQ_1, and
+    // [..][R] those of P_1 (D - t_1) (q_splits > 1)
+    int q_splits;
+    float* q_part;
+    float* q_miss;
 };
 constexpr float kDiffLn2 = 0.693147180559945f;
 constexpr int kDiffStats = 8;
@@ -310,14 +315,22 @@ constexpr int kDiffKeys = 128;  // keys of a workgroup of the key pass
 // Parts of the key pass's rows. One key head's keys in tiles of 128 may be few workgroups, and under a causal mask the
 // first tile meets all rows and the last only its own; parts cost a write and a read of fp32 sums. Two workgroups run on a
 // unit: as many parts as fill the units twice where work is even and four times where it is causal, no part below
-// 8 tiles of 32 rows, at most 8. (2 x 4096 keys, 16 heads over 4, d = 64, bf16, causal: @1@)
+// 4 tiles of 32 rows, at most 8. (2 x 4096 keys, 16 heads over 4, d = 64, bf16, causal: @1@)
 inline int diff_key_splits(int B, int kv_heads, int Nk, int R, bool causal)
 {
     const long long groups = static_cast<long long>(B) * kv_heads * ((Nk + kDiffKeys - 1) / kDiffKeys);
     const long long want = static_cast<long long>(device_cu_count()) * (causal ? 4 : 2);
-    const long long most = R / 256;
+    const long long most = R / 128;
     const long long s = (want + groups - 1) / groups;
     return static_cast<int>(s < 1 || most < 1 ? 1 : (s > most ? most : s) > 8 ? 8 : (s > most ? most : s));
+}
+
+// Parts of the query pass's keys: enough to fill the units twice, none below 256 keys, at most 16.
+inline int diff_query_splits(int B, int kv_heads, int Nk, int R)
+{
+    const long long groups = static_cast<long long>(B) * kv_heads * ((R + 127) / 128), most = Nk / 256;
+    const long long s = (2LL * device_cu_count() + groups - 1) / groups;
+    return static_cast<int>(s < 1 || most < 1 ? 1 : (s > most ? most : s) > 16 ? 16 : (s > most ? most : s));
 }
 
 hipError_t launch_diff_attn(const DiffArgs& a, int d, bool use_bf16, hipStream_t stream);

@@ -22,6 +22,14 @@ using namespace diff;
 
 constexpr int kThreads = 256;
 
+__device__ __forceinline__ void store_dlambda(const DiffBwdArgs& a, int b, int i, int h, float x)
+{
+    const long long row = static_cast<long long>(b) * a.f.Nq + i;
+    if (a.lam_heads) a.dlam_rows[static_cast<long long>(h) * a.f.B * a.f.Nq + row] = x;
+    else if (a.f.lam_bf16) Storage<bf16>::store1(a.dlam, row * a.f.heads + h, x);
+    else Storage<float>::store1(a.dlam, row * a.f.heads + h, x);
+}
+
 // ---- the rows' statistics ----
 
 // A row (b, i, h) takes 2D / V lanes of one 16-byte chunk each.
@@ -95,6 +103,7 @@ __global__ __launch_bounds__(1024) void diff_lambda_kernel(const float* rows, lo
 
 // ---- dQ ----
 
+// With `q_splits` > 1 a workgroup takes one part of its rows' keys and writes fp32 sums to `q_part` and `q_miss`.
 template <typename T, int D, int BN>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kernel(DiffBwdArgs a)
 {
@@ -109,7 +118,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int tiles_n = (f.R + BM - 1) / BM;
     const int logical = xcd_remap(blockIdx.x, gridDim.x);
-    const int bh = logical / tiles_n, tile = tiles_n - 1 - (logical - bh * tiles_n);
+    const int work = logical / a.q_splits, split = logical - work * a.q_splits;
+    const int bh = work / tiles_n, tile = tiles_n - 1 - (work - bh * tiles_n);     // the longest rows first
     const int b = bh / f.kv_heads, g = bh - b * f.kv_heads, G = f.heads / f.kv_heads;
     const int row0 = tile * BM, row1 = min(row0 + BM, f.R);
     const DiffRange range = diff_range(f, b);
@@ -199,27 +209,37 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
             }
         }
     };
-    const int nt = (kend + BN - 1) / BN;
-    if (nt > 0) stage(0, lds);
-    for (int t = 0; t < nt; t += 2) {
+    const int all = (kend + BN - 1) / BN;
+    const int first = static_cast<int>(static_cast<long long>(all) * split / a.q_splits);
+    const int end = static_cast<int>(static_cast<long long>(all) * (split + 1) / a.q_splits);
+    if (first < end) stage(first * BN, lds);
+    for (int t = first; t < end; t += 2) {
         tiles::wait_lds_loads();
         __syncthreads();
-        if (t + 1 < nt) stage((t + 1) * BN, lds + kStage);
+        if (t + 1 < end) stage((t + 1) * BN, lds + kStage);
         keys(t * BN, std::integral_constant<int, 0>{});
-        if (t + 1 >= nt) break;
+        if (t + 1 >= end) break;
         tiles::wait_lds_loads();
         __syncthreads();
-        if (t + 2 < nt) stage((t + 2) * BN, lds);
+        if (t + 2 < end) stage((t + 2) * BN, lds);
         keys((t + 1) * BN, std::integral_constant<int, 1>{});
     }
     miss += other_half(miss);
     if (rr >= f.R) return;
-    if (half == 0) {
-        const float dl = -(t1 + miss);
-        if (a.lam_heads) a.dlam_rows[static_cast<long long>(h) * f.B * f.Nq + static_cast<long long>(b) * f.Nq + qi] = dl;
-        else if (f.lam_bf16) Storage<bf16>::store1(a.dlam, orow / (2 * D), dl);
-        else Storage<float>::store1(a.dlam, orow / (2 * D), dl);
+    if (a.q_splits > 1) {
+        const long long at = (static_cast<long long>(split) * f.B * f.kv_heads + bh) * f.R + r;
+        if (half == 0) a.q_miss[at] = miss;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    store4<float>(a.q_part, (2 * at + m) * D + 32 * c + acc_row(e, half), acc[m][c][e], acc[m][c][e + 1],
+                                  acc[m][c][e + 2], acc[m][c][e + 3]);
+        return;
     }
+    if (half == 0) store_dlambda(a, b, qi, h, -(t1 + miss));
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -229,6 +249,29 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
                 store4<T>(a.dq, ((static_cast<long long>(b) * f.Nq + qi) * 2 * f.heads + 2 * h + m) * D + 32 * c + acc_row(e, half),
                           acc[m][c][e] * a.grad_scale, acc[m][c][e + 1] * a.grad_scale, acc[m][c][e + 2] * a.grad_scale,
                           acc[m][c][e + 3] * a.grad_scale);
+}
+
+// The parts' sums, in their order: four channels of one row a thread.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void diff_dq_join_kernel(DiffBwdArgs a)
+{
+    const DiffArgs& f = a.f;
+    const long long item = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x, rows = static_cast<long long>(f.B) * f.kv_heads * f.R;
+    const long long at = item / (D / 2);
+    if (at >= rows) return;
+    const int c = 4 * static_cast<int>(item - at * (D / 2));
+    const int bh = static_cast<int>(at / f.R), r = static_cast<int>(at - static_cast<long long>(bh) * f.R), G = f.heads / f.kv_heads;
+    const int b = bh / f.kv_heads, i = fast_div(r, f.div_G), h = (bh - b * f.kv_heads) * G + r - i * G;
+    const f32x4* const p = reinterpret_cast<const f32x4*>(a.q_part) + item;
+    f32x4 x = *p;
+#pragma unroll 4
+    for (int s = 1; s < a.q_splits; ++s) x += p[s * rows * (D / 2)];
+    store4<T>(a.dq, ((static_cast<long long>(b) * f.Nq + i) * f.heads + h) * (2 * D) + c, x[0] * a.grad_scale, x[1] * a.grad_scale,
+              x[2] * a.grad_scale, x[3] * a.grad_scale);
+    if (c != 0) return;
+    float miss = a.stats[(static_cast<size_t>(bh) * kDiffStats + 7) * a.Rpad + r];
+    for (int s = 0; s < a.q_splits; ++s) miss += a.q_miss[s * rows + at];
+    store_dlambda(a, b, i, h, -miss);
 }
 
 // ---- dK, dV ----
@@ -452,7 +495,7 @@ hipError_t launch_bwd(const DiffBwdArgs& a, hipStream_t stream)
     const long long bh = static_cast<long long>(a.f.B) * a.f.kv_heads;
     constexpr int lpr = 2 * D * ES / 16;
     const long long rblocks = (bh * a.Rpad * lpr + kThreads - 1) / kThreads;
-    const long long qblocks = (a.f.R + 127) / 128 * bh, kblocks = (a.f.Nk + kDiffKeys - 1) / kDiffKeys * bh * a.splits;
+    const long long qblocks = (a.f.R + 127) / 128 * bh * a.q_splits, kblocks = (a.f.Nk + kDiffKeys - 1) / kDiffKeys * bh * a.splits;
     if (rblocks > 0x7FFFFFFFLL || qblocks > 0x7FFFFFFFLL || kblocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     hipError_t e = set_max_lds_once(reinterpret_cast<const void*>(&diff_dq_kernel<T, D, BN>), configured_q);
     if (e != hipSuccess) return e;
@@ -461,6 +504,11 @@ hipError_t launch_bwd(const DiffBwdArgs& a, hipStream_t stream)
     hipLaunchKernelGGL((diff_rows_kernel<T, D>), dim3(static_cast<unsigned>(rblocks)), dim3(kThreads), 0, stream, a);
     hipLaunchKernelGGL((diff_dq_kernel<T, D, BN>), dim3(static_cast<unsigned>(qblocks)), dim3(kThreads), 2 * BN * 4 * D * ES,
                        stream, a);
+    if (a.q_splits > 1) {
+        const long long items = bh * a.f.R * (D / 2);
+        hipLaunchKernelGGL((diff_dq_join_kernel<T, D>), dim3(static_cast<unsigned>((items + kThreads - 1) / kThreads)),
+                           dim3(kThreads), 0, stream, a);
+    }
     if (a.lam_heads)
         hipLaunchKernelGGL(diff_lambda_kernel, dim3(static_cast<unsigned>(a.f.heads)), dim3(1024), 0, stream, a.dlam_rows,
                            static_cast<long long>(a.f.B) * a.f.Nq, a.dlam, a.f.lam_bf16);
