@@ -364,18 +364,22 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
         // the first row that sees this lane's key, and one that sees every key of the wave (R: none)
         auto first_row = [&](int x) { return x >= range.len ? f.R : range.causal ? min(max(0, x - range.pos), f.Nq) * G : 0; };
         const int see = first_row(key), wave_see = first_row(wk0 + 31);
-        const uint32_t base0 = lds_address(lds), vw = lds_address(vt) + 32 * wave * OT::kRow;
-        uint32_t qrow = QT::row_base(lane), qcol = QT::col_base(lane), orow = OT::row_base(lane), ocol = OT::col_base(lane);
-        const uint32_t srow = 16 * half;
-        // the 32 rows from r0 on, in the stage at cur
-        auto rows = [&](int r0, uint32_t cur) {
+        // (whole rows are added, so that the bases keep their bits below)
+        const uint32_t base0 = lds_address(lds);
+        uint32_t qrow = base0 + QT::row_base(lane), qcol = base0 + QT::col_base(lane), orow = base0 + OT::row_base(lane),
+                 ocol = base0 + OT::col_base(lane), vrow = orow + 32 * wave * OT::kRow;
+        uint32_t srow = base0 + 16 * half;
+        // the 32 rows from r0 on; the bases are those of their stage, so that everything else is an immediate
+        auto rows = [&](int r0) {
+            constexpr uint32_t cur = 0, vw = 2 * kStage;
             opaque(qrow);
             opaque(qcol);
             opaque(orow);
             opaque(ocol);
+            opaque(vrow);
             const bool edge = r0 < wave_see || r0 + BM > f.R;
             // four rows' statistics at a time: rows 8 (e / 4) + 4 half .. + 3
-            const uint32_t st = cur + 2 * kQ + kO;
+            constexpr uint32_t st = cur + 2 * kQ + kO;
             auto stat = [&](int plane, int e) { return *lds_at<f32x4>(srow + (st + plane * 128 + 8 * e)); };
             auto from = [&](int plane) {
                 f32x16 x;
@@ -390,7 +394,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
             f32x16 dp = from(2);
 #pragma unroll
             for (int c = 0; c < D / 8; ++c) {
-                dp = mma(OT::row_frag(orow, cur + 2 * kQ, 0, c), OT::row_frag(orow, vw, 0, c), dp);
+                dp = mma(OT::row_frag(orow, cur + 2 * kQ, 0, c), OT::row_frag(vrow, vw, 0, c), dp);
                 if (c % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
             float w[16];
@@ -439,10 +443,17 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
         };
         stage(rbeg + t0 * BM, lds);
         for (int t = t0; t < t1; ++t) {
+            const bool odd = (t - t0) & 1;
             tiles::wait_lds_loads();
             __syncthreads();
-            if (t + 1 < t1) stage(rbeg + (t + 1) * BM, lds + ((t - t0 + 1) & 1) * kStage);
-            rows(rbeg + t * BM, base0 + ((t - t0) & 1) * kStage);
+            if (t + 1 < t1) stage(rbeg + (t + 1) * BM, odd ? lds : lds + kStage);
+            rows(rbeg + t * BM);
+            const uint32_t move = odd ? -kStage : kStage;
+            qrow += move;
+            qcol += move;
+            orow += move;
+            ocol += move;
+            srow += move;
         }
     }
     if (key >= f.Nk) return;
