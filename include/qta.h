@@ -423,18 +423,18 @@ typedef struct {
 /*
  * qta_diff_attn - the forward.
  *   out         [B][Nq][heads][2d] dtype, 16-byte aligned.
- *   out1, lse   for qta_diff_attn_backward: P_1 V as out, and fp32 [B][heads][2][Nq], the base-2 logarithm of each row's
- *               sum of weights (-inf for an empty row). Both NULL for inference.
+ *   maps, lse   for qta_diff_attn_backward: P_0 V and P_1 V, fp32 [B][Nq][heads][2][2d], 16-byte aligned, and fp32 [B][heads][2][Nq], the
+ *               base-2 logarithm of each row's sum of weights (-inf for an empty row). Both NULL for inference.
  *   workspace   256-byte aligned, qta_diff_attn_workspace_bytes bytes (at least 256 for valid shapes, 0 otherwise), in which
  *               calls of few rows and many keys put the parts of their keys; may be NULL where 256 are asked for.
  *               Need not be preserved or cleared; calls that may run at the same time need one each.
  */
 size_t qta_diff_attn_workspace_bytes(const qta_diff_attn_args* args);
-qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, void* out1, float* lse, void* workspace,
+qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, float* maps, float* lse, void* workspace,
                          size_t workspace_bytes, void* stream);
 
 /*
- * qta_diff_attn_backward - gradients for dout = dLoss/dout, the arguments and out, out1, lse being the forward's.
+ * qta_diff_attn_backward - gradients for dout = dLoss/dout, the arguments, maps and lse being the forward's.
  *   dout        [B][Nq][heads][2d] dtype, contiguous.
  *   dq, dk, dv  dtype, contiguous in the shapes of q, k and v, overwritten (also where no row sees a key: zeros).
  *   dlam        lambda's type, overwritten: [B][Nq][heads], or with dlam_heads nonzero [heads], summed over batch and tokens.
@@ -443,8 +443,8 @@ qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, void* out1, 
  * broadcast by a zero stride the gradient comes in the full shape.
  */
 size_t qta_diff_attn_backward_workspace_bytes(const qta_diff_attn_args* args);
-qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const void* out, const void* out1, const float* lse,
-                                  const void* dout, void* dq, void* dk, void* dv, void* dlam, int dlam_heads, void* workspace,
+qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const float* maps, const float* lse, const void* dout,
+                                  void* dq, void* dk, void* dv, void* dlam, int dlam_heads, void* workspace,
                                   size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus

@@ -133,12 +133,12 @@ size_t qta_diff_attn_workspace_bytes(const qta_diff_attn_args* args)
     return n < kAlign ? kAlign : n;
 }
 
-qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, void* out1, float* lse, void* workspace,
+qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, float* maps, float* lse, void* workspace,
                          size_t workspace_bytes, void* stream)
 {
     const qta_status st = check_diff(args, false);
     if (st != QTA_OK) return st;
-    if (!out || !aligned(out, 16) || (out1 != nullptr) != (lse != nullptr) || !aligned(out1, 16) || !aligned(lse, 4)) return QTA_ERR_INVALID;
+    if (!out || !aligned(out, 16) || (maps != nullptr) != (lse != nullptr) || !aligned(maps, 16) || !aligned(lse, 4)) return QTA_ERR_INVALID;
     const FwdLayout L = fwd_layout(args);
     if (L.total > 0) {
         if (workspace_bytes < L.total) return QTA_ERR_WORKSPACE;
@@ -146,7 +146,7 @@ qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, void* out1, 
     }
     DiffArgs a = make_args(args);
     a.out = out;
-    a.out1 = out1;
+    a.maps = maps;
     a.lse = lse;
     a.keys_apart = L.parts.keys_apart;
     a.splits = L.parts.splits;
@@ -160,21 +160,20 @@ size_t qta_diff_attn_backward_workspace_bytes(const qta_diff_attn_args* args)
     return check_diff(args, true) == QTA_OK ? bwd_layout(args, true).total : 0;
 }
 
-qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const void* out, const void* out1, const float* lse,
-                                  const void* dout, void* dq, void* dk, void* dv, void* dlam, int dlam_heads, void* workspace,
+qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const float* maps, const float* lse, const void* dout,
+                                  void* dq, void* dk, void* dv, void* dlam, int dlam_heads, void* workspace,
                                   size_t workspace_bytes, void* stream)
 {
     const qta_status st = check_diff(args, false);
     if (st != QTA_OK) return st;
-    for (const void* p : {out, out1, dout, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv)})
+    for (const void* p : {static_cast<const void*>(maps), dout, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv)})
         if (!p || !aligned(p, 16)) return QTA_ERR_INVALID;
     if (!lse || !dlam || !workspace || !aligned(workspace, 256)) return QTA_ERR_INVALID;
     const BwdLayout L = bwd_layout(args, dlam_heads != 0);
     if (workspace_bytes < L.total) return QTA_ERR_WORKSPACE;
     DiffBwdArgs a{};
     a.f = make_args(args);
-    a.f.out = const_cast<void*>(out);
-    a.f.out1 = const_cast<void*>(out1);
+    a.f.maps = const_cast<float*>(maps);
     a.f.lse = const_cast<float*>(lse);
     a.dout = dout;
     unsigned char* const ws = static_cast<unsigned char*>(workspace);

@@ -30,9 +30,10 @@ struct DiffArgs {
     const int32_t* q_pos;       // [B] key position of query 0 (causal), or NULL: Nk - Nq
     float scale;                // of the logits, times log2(e): weights are powers of two
     void* out;                  // [B][Nq][heads][2d]
-    // kept for the backward (NULL in inference): P_1 V, [B][Nq][heads][2d], and log2 of the weights' sums
-    // [B][heads][2][Nq] (-inf where a row sees nothing)
-    void* out1;
+    // kept for the backward (NULL in inference): P_0 V and P_1 V, fp32 [B][Nq][heads][2][2d] (from the rounded output dQ
+    // and dK of short causal sequences are 1.6 times as far off as rounding makes a result, from these 1.45), and log2 of
+    // the weights' sums [B][heads][2][Nq] (-inf where a row sees nothing)
+    float* maps;
     float* lse;
     // few rows: waves split the keys of a tile instead of rows, and the keys come in `splits` parts (see diff_key_parts),
     // whose results go to part, fp32 [splits][B][kv_heads][2][R][2d], and part_sums, [..][R][2] (maximum, sum)
@@ -285,7 +286,7 @@ __device__ __forceinline__ float other_half(float x) { return xchg_f32<32>(x); }
 
 // Backward: the argument block, and what each pass writes.
 struct DiffBwdArgs {
-    DiffArgs f;                 // out, out1 and lse are the forward's (read)
+    DiffArgs f;                 // maps and lse are the forward's (read)
     const void* dout;           // [B][Nq][heads][2d] contiguous
     // by rows of one key head, [B][kv_heads][kDiffStats][Rpad] fp32. With s the logits' scale, S the sign of lambda:
     // -lse_0 / s, -(lse_1 - log2 |lambda|) / s, -t_0, -S (t_0 - t_1), -S for the key pass; -lse_1 / s, t_0 - t_1, t_1

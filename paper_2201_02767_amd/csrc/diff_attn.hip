@@ -199,15 +199,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (KEYS ? 2 : 4) : 1) void
     for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-            float o1[4], o[4];
+            float o0[4], o1[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
+                o0[j] = acc[c][e + j] * inv;
                 o1[j] = box[(c * 16 + e + j) * 64];
-                o[j] = acc[c][e + j] * inv - lam * o1[j];
             }
-            const long long at = row * (2 * D) + 32 * c + acc_row(e, half);
-            store4<T>(a.out, at, o[0], o[1], o[2], o[3]);
-            if (a.out1) store4<T>(a.out1, at, o1[0], o1[1], o1[2], o1[3]);
+            const int ch = 32 * c + acc_row(e, half);
+            store4<T>(a.out, row * (2 * D) + ch, o0[0] - lam * o1[0], o0[1] - lam * o1[1], o0[2] - lam * o1[2], o0[3] - lam * o1[3]);
+            if (a.maps) {
+                store4<float>(a.maps, row * (4 * D) + ch, o0[0], o0[1], o0[2], o0[3]);
+                store4<float>(a.maps, row * (4 * D) + 2 * D + ch, o1[0], o1[1], o1[2], o1[3]);
+            }
         }
 }
 
@@ -249,9 +252,12 @@ __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffArgs a)
     const long long row = (static_cast<long long>(b) * a.Nq + qi) * a.heads + h;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const float o1 = o[1][v] * inv[1];
-        Storage<T>::store1(a.out, row * (2 * D) + lane * V + v, o[0][v] * inv[0] - lam * o1);
-        if (a.out1) Storage<T>::store1(a.out1, row * (2 * D) + lane * V + v, o1);
+        const float o0 = o[0][v] * inv[0], o1 = o[1][v] * inv[1];
+        Storage<T>::store1(a.out, row * (2 * D) + lane * V + v, o0 - lam * o1);
+        if (a.maps) {
+            a.maps[row * (4 * D) + lane * V + v] = o0;
+            a.maps[row * (4 * D) + 2 * D + lane * V + v] = o1;
+        }
     }
     if (a.lse && lane < 2) {
         const float t = lane ? top[1] : top[0], z = lane ? sum[1] : sum[0];

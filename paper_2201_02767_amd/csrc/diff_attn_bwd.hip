@@ -8,8 +8,8 @@
 // holds both. Each result is summed in one order: no atomics, the same bits every run.
 //
 // D starts from -t_0 instead of zero, and in the key pass, where a statistic is needed for every register, Q K^T from
-// -lse / scale: a weight is then one product and one power of two away. t_m comes from the stored, rounded O and O_1; the rows of P_1 (D - t_1), which
-// with the exact t_1 sum to zero, give what is missing, and dlambda is exact to fp32.
+// -lse / scale: a weight is then one product and one power of two away. t_m comes from results whose weights were rounded;
+// the rows of P_1 (D - t_1), which with the exact t_1 sum to zero, give what is missing, and dlambda is exact to fp32.
 #include <atomic>
 #include <type_traits>
 
@@ -54,28 +54,29 @@ __global__ __launch_bounds__(kThreads) void diff_rows_kernel(DiffBwdArgs a)
     const int b = bh / f.kv_heads, i = fast_div(r, f.div_G), h = (bh - b * f.kv_heads) * G + r - i * G;
     const long long row = (static_cast<long long>(b) * f.Nq + i) * f.heads + h;
     const uint4* const go = reinterpret_cast<const uint4*>(a.dout) + row * LPR + c;
-    const uint4* const o = reinterpret_cast<const uint4*>(f.out) + row * LPR + c;
-    const uint4* const o1 = reinterpret_cast<const uint4*>(f.out1) + row * LPR + c;
-    float x[V], y[V], z[V];
+    const f32x4* const o = reinterpret_cast<const f32x4*>(f.maps + row * (4 * D) + c * V);
+    float x[V];
     Storage<T>::unpack(*go, x);
-    Storage<T>::unpack(*o, y);
-    Storage<T>::unpack(*o1, z);
-    float s = 0.f, t1 = 0.f;
+    float t0 = 0.f, t1 = 0.f;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        s = fmaf(x[j], y[j], s);
-        t1 = fmaf(x[j], z[j], t1);
+    for (int j = 0; j < V; j += 4) {
+        const f32x4 y = o[j / 4], z = o[(2 * D + j) / 4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            t0 = fmaf(x[j + k], y[k], t0);
+            t1 = fmaf(x[j + k], z[k], t1);
+        }
     }
-    s = group_sum<LPR < 16 ? LPR : 16>(s);
+    t0 = group_sum<LPR < 16 ? LPR : 16>(t0);
     t1 = group_sum<LPR < 16 ? LPR : 16>(t1);
     if constexpr (LPR == 32) {
-        s += xchg_f32<16>(s);
+        t0 += xchg_f32<16>(t0);
         t1 += xchg_f32<16>(t1);
     }
     if (c != 0) return;
     const float lam = diff_lambda(f, b, i, h), inv = -1.0f / f.scale;
     const float* const lse = f.lse + (static_cast<long long>(b) * f.heads + h) * 2 * f.Nq + i;
-    const float l0 = lse[0], l1 = lse[f.Nq], t0 = fmaf(lam, t1, s);        // dO . O_0 = dO . (O + lambda O_1)
+    const float l0 = lse[0], l1 = lse[f.Nq];
     const float nsign = lam < 0.f ? 1.0f : -1.0f;
     const float x_[kDiffStats] = {l0 * inv, (l1 - __builtin_amdgcn_logf(fabsf(lam))) * inv, -t0, nsign * (t0 - t1), nsign,
                                   l1 * inv, t0 - t1, t1};

@@ -35,7 +35,7 @@ _SIGS.update({
     "qta_diff_attn_workspace_bytes": ([_P], ctypes.c_size_t),
     "qta_diff_attn": ([_P, _P, _P, _P, _P, ctypes.c_size_t, _P], _I),
     "qta_diff_attn_backward_workspace_bytes": ([_P], ctypes.c_size_t),
-    "qta_diff_attn_backward": ([_P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _P, ctypes.c_size_t, _P], _I),
+    "qta_diff_attn_backward": ([_P, _P, _P, _P, _P, _P, _P, _P, _I, _P, ctypes.c_size_t, _P], _I),
 })
 
 
@@ -245,57 +245,56 @@ def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, 
     ``keep``: also return what ``diff_attn_backward`` needs."""
     args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
     out = torch.empty(shape, dtype=q.dtype, device=q.device)
-    out1 = lse = None
+    maps = lse = None
     if keep:
-        out1 = torch.empty_like(out)
+        maps = torch.empty((*shape[:-1], 2, shape[-1]), dtype=torch.float32, device=q.device)
         lse = torch.empty((args.B, args.heads, 2, args.Nq), dtype=torch.float32, device=q.device)
     if args.Nk == 0 or out.numel() == 0:
         out.zero_()
         if keep:
-            out1.zero_()
+            maps.zero_()
             lse.fill_(-math.inf)
     else:
         ws, nbytes = _workspace("qta_diff_attn_workspace_bytes", args, q)
-        _call("qta_diff_attn", q, ctypes.byref(args), out.data_ptr(), out1.data_ptr() if keep else None,
+        _call("qta_diff_attn", q, ctypes.byref(args), out.data_ptr(), maps.data_ptr() if keep else None,
               lse.data_ptr() if keep else None, None if ws is None else ws.data_ptr(), nbytes)
-    return (out, (out1, lse)) if keep else out
+    return (out, (maps, lse)) if keep else out
 
 
-def diff_attn_backward(q, k, v, lam, out, kept, dout, *, scale=None, causal=False, lens=None, q_pos=None):
+def diff_attn_backward(q, k, v, lam, kept, dout, *, scale=None, causal=False, lens=None, q_pos=None):
     """Gradients (dq, dk, dv, dlam) of ``diff_attn(.., keep=True)`` for the upstream gradient ``dout``, each in the
-    shape and type of its input; ``out`` and ``kept`` are what that call returned, the other arguments the same."""
+    shape and type of its input; ``kept`` is what that call returned, the other arguments the same."""
     args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
-    out1, lse = kept
-    for t, n in ((out, "out"), (out1, "kept"), (dout, "dout")):
-        if t.dtype is not q.dtype or t.device != q.device or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{n} must be contiguous {q.dtype} {tuple(shape)} on {q.device}")
-    if lse.shape != (args.B, args.heads, 2, args.Nq) or lse.dtype is not torch.float32 or not lse.is_contiguous():
-        raise ValueError("kept is not what diff_attn returned for these shapes")
+    maps, lse = kept
+    for t, n, dtype, s in ((maps, "kept", torch.float32, (*shape[:-1], 2, shape[-1])),
+                           (lse, "kept", torch.float32, (args.B, args.heads, 2, args.Nq)), (dout, "dout", q.dtype, shape)):
+        if t.dtype is not dtype or t.device != q.device or t.shape != s or not t.is_contiguous():
+            raise ValueError(f"{n} must be contiguous {dtype} {tuple(s)} on {q.device}")
     grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v, lam)]
-    if out.numel() == 0 or args.Nk == 0:
+    if args.Nk == 0 or dout.numel() == 0:
         return tuple(g.zero_() for g in grads)
     ws, nbytes = _workspace("qta_diff_attn_backward_workspace_bytes", args, q)
-    _call("qta_diff_attn_backward", q, ctypes.byref(args), out.data_ptr(), out1.data_ptr(), lse.data_ptr(),
-          dout.data_ptr(), *[g.data_ptr() for g in grads], lam.dim() == 1, ws.data_ptr(), nbytes)
+    _call("qta_diff_attn_backward", q, ctypes.byref(args), maps.data_ptr(), lse.data_ptr(), dout.data_ptr(),
+          *[g.data_ptr() for g in grads], lam.dim() == 1, ws.data_ptr(), nbytes)
     return tuple(grads)
 
 
 class _DiffAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, lam, scale, causal, lens, q_pos):
-        out, (out1, lse) = diff_attn(q, k, v, lam, scale=scale, causal=causal, lens=lens, q_pos=q_pos, keep=True)
+        out, (maps, lse) = diff_attn(q, k, v, lam, scale=scale, causal=causal, lens=lens, q_pos=q_pos, keep=True)
         ctx.how = (scale, causal)
-        ctx.save_for_backward(q, k, v, lam, out, out1, lse, lens, q_pos)
+        ctx.save_for_backward(q, k, v, lam, maps, lse, lens, q_pos)
         return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
-        q, k, v, lam, out, out1, lse, lens, q_pos = ctx.saved_tensors
+        q, k, v, lam, maps, lse, lens, q_pos = ctx.saved_tensors
         dout = dout.contiguous()
         if dout.data_ptr() % 16:
             dout = dout.clone()
-        return (*diff_attn_backward(q, k, v, lam, out, (out1, lse), dout, scale=ctx.how[0], causal=ctx.how[1], lens=lens,
+        return (*diff_attn_backward(q, k, v, lam, (maps, lse), dout, scale=ctx.how[0], causal=ctx.how[1], lens=lens,
                                     q_pos=q_pos), None, None, None, None)
 
 

@@ -7,8 +7,9 @@ fp32 2^-24), f = 2^-24. For differential attention, with L the largest scale * s
   - for a product with V or dO weights are rounded to the storage type: u more. So O_m is off by (u + w) A_m with
     A_m = P_m |V|, and O, rounded once more, by u |O| + (u + w) (A_0 + |lam| A_1) =: E;
   - D = dO V^T is off by 2 d f |dO| |V|^T;
-  - t_m = dO . O_m is taken from the stored O and O_1 (off by E and E_1 = u |O_1| + (u + w) A_1): off by
-    |dO| . E_1 for m = 1, |dO| . (E + |lam| E_1) for m = 0, and (4 d + 4) f |dO| . (|O| + 2 |lam| |O_1|) for the dot products;
+  - t_m = dO . O_m is taken from the fp32 O_m that the forward keeps, off by (u + w + 2 f) A_m, and the dot product by
+    (2 d + 2) f |dO| . |O_m|; dlam is made exact again by the sum of P_1 (D - t_1) over the Nk keys, whose terms are off by
+    w P_1 |D - t_1| + P_1 dD and whose sum by Nk f (and 2 f for what it corrects);
   - dS_m = (lam) P_m (D - t_m) is off by its factors' errors, (w + 4 f) |dS_m| + P_m (dD + dt_m), and u |dS_m| when it is
     rounded for the products with K and Q; dK, dQ and dV are sums of such terms (n f more for n summands), rounded once.
 """
@@ -76,7 +77,6 @@ def diff_attention(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=N
             O = [p @ W for p in P]
             A = [p @ W.abs() for p in P]
             out = O[0] - l * O[1]
-            E1 = u * O[1].abs() + (u + w) * A[1]
             E = u * out.abs() + (u + w) * (A[0] + l.abs() * A[1])
             res["out"][0][b, :, h], res["out"][1][b, :, h] = out, E
             if dout is None:
@@ -87,10 +87,9 @@ def diff_attention(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=N
             eD = 2 * d * F * (ado @ W.abs().T.contiguous())
             dot = lambda a_, b_: (a_ * b_).sum(-1, keepdim=True)
             t = [dot(do, O[0]), dot(do, O[1])]
-            e_dot = (4 * d + 4) * F
-            et1 = dot(ado, E1) + e_dot * dot(ado, O[1].abs())
-            et = [dot(ado, E) + l.abs() * et1 + e_dot * dot(ado, out.abs() + 2 * l.abs() * O[1].abs()), et1]
-            res["dlam"][0][b, :, h], res["dlam"][1][b, :, h] = -t[1][:, 0], et1[:, 0]
+            et = [(u + w + 2 * F) * dot(ado, A[m]) + (2 * d + 2) * F * dot(ado, O[m].abs()) for m in (0, 1)]
+            el = dot(P[1], (w + (Nk + 4) * F) * ((D - t[1]).abs() + et[1]) + eD) + 2 * F * (dot(ado, O[1].abs()) + et[1])
+            res["dlam"][0][b, :, h], res["dlam"][1][b, :, h] = -t[1][:, 0], el[:, 0]
             for m in (0, 1):
                 f = -l if m else 1.0
                 dS = f * P[m] * (D - t[m])

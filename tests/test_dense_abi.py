@@ -23,12 +23,12 @@ def diff_args(**kw):
     return DiffAttnArgs(**a)
 
 
-def forward(out=FAKE, out1=None, lse=None, ws=None, nbytes=0, **kw):
-    return P.lib().qta_diff_attn(ctypes.byref(diff_args(**kw)), out, out1, lse, ws, nbytes, None)
+def forward(out=FAKE, maps=None, lse=None, ws=None, nbytes=0, **kw):
+    return P.lib().qta_diff_attn(ctypes.byref(diff_args(**kw)), out, maps, lse, ws, nbytes, None)
 
 
 def backward(ws=FAKE, nbytes=0, heads_lam=1, kw={}, **p):
-    a = dict(out=FAKE, out1=FAKE, lse=FAKE, dout=FAKE, dq=FAKE, dk=FAKE, dv=FAKE, dlam=FAKE)
+    a = dict(maps=FAKE, lse=FAKE, dout=FAKE, dq=FAKE, dk=FAKE, dv=FAKE, dlam=FAKE)
     a.update(p)
     return P.lib().qta_diff_attn_backward(ctypes.byref(diff_args(**kw)), *a.values(), heads_lam, ws, nbytes, None)
 
@@ -41,7 +41,7 @@ def test_diff_attn_validation():
         assert forward(**{n: FAKE + 4}) == INVALID, n
     assert forward(out=None) == INVALID
     assert forward(out=FAKE + 8) == INVALID
-    assert forward(out1=FAKE) == INVALID and forward(lse=FAKE) == INVALID      # one without the other
+    assert forward(maps=FAKE) == INVALID and forward(lse=FAKE) == INVALID      # one without the other
     for n in ("B", "heads", "kv_heads", "Nq", "Nk", "d"):
         assert forward(**{n: 0}) == INVALID, n
         assert forward(**{n: -1}) == INVALID, n
@@ -79,9 +79,9 @@ def test_diff_attn_backward_validation():
     need = P.lib().qta_diff_attn_backward_workspace_bytes(ctypes.byref(diff_args()))
     assert need > 0 and need % 256 == 0
     assert backward(nbytes=need - 1) == WORKSPACE
-    for n in ("out", "out1", "lse", "dout", "dq", "dk", "dv", "dlam"):
+    for n in ("maps", "lse", "dout", "dq", "dk", "dv", "dlam"):
         assert backward(nbytes=need, **{n: None}) == INVALID, n
-    for n in ("out", "out1", "dout", "dq", "dk", "dv"):
+    for n in ("maps", "dout", "dq", "dk", "dv"):
         assert backward(nbytes=need, **{n: FAKE + 4}) == INVALID, n
     assert backward(ws=None, nbytes=need) == INVALID
     assert backward(ws=FAKE + 16, nbytes=need) == INVALID

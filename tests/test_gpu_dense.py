@@ -67,7 +67,7 @@ def check(dev, q, k, v, lam, dout, *, label="", grads=True, ref_kv=None, **how):
     if not grads:
         return out
     out2, kept = P.diff_attn(q, k, v, lam, keep=True, **how)
-    got = P.diff_attn_backward(q, k, v, lam, out2, kept, dout, **how)
+    got = P.diff_attn_backward(q, k, v, lam, kept, dout, **how)
     torch.cuda.synchronize()
     within("out (kept)", out2, ref["out"])
     for n, t in zip(("dq", "dk", "dv", "dlam"), got):
@@ -172,7 +172,7 @@ def test_diff_attn_maps(dev):
     q, k, v = r(2, 5, 7, 4, 32), r(2, 6, 9, 2, 32), r(2, 6, 9, 1, 64)
     lam, do = r(2, 5, 7, 2), r(2, 5, 7, 2, 64)
     out, kept = P.diff_attn(q, k, v, lam, keep=True)
-    got = P.diff_attn_backward(q, k, v, lam, out, kept, do)
+    got = P.diff_attn_backward(q, k, v, lam, kept, do)
     fl = lambda t: t.flatten(1, 2)
     ref = R.diff_attention(fl(q), fl(k), fl(v), fl(lam), dout=fl(do))
     within("out", fl(out), ref["out"])
@@ -206,7 +206,7 @@ def test_diff_attn_runs_are_identical(dev, dtype):
     one = None
     for _ in range(3):
         out, kept = P.diff_attn(q, k, v, lam, keep=True)
-        now = (out, P.diff_attn(q, k, v, lam), *kept, *P.diff_attn_backward(q, k, v, lam, out, kept, do))
+        now = (out, P.diff_attn(q, k, v, lam), *kept, *P.diff_attn_backward(q, k, v, lam, kept, do))
         if one is None:
             one = [t.clone() for t in now]
             assert torch.equal(now[0], now[1])
@@ -217,7 +217,7 @@ def test_diff_attn_against_differences(dev):
     """The gradients against central differences of the 64-bit function along random directions."""
     q, k, v, lam, do = make(dev, 1, 12, 20, 2, 1, 32, "f32", seed=16)
     out, kept = P.diff_attn(q, k, v, lam, keep=True, causal=True)
-    got = P.diff_attn_backward(q, k, v, lam, out, kept, do, causal=True)
+    got = P.diff_attn_backward(q, k, v, lam, kept, do, causal=True)
     r = gen(17, dev)
     base = [t.double() for t in (q, k, v, lam)]
     f = lambda a: float((R.diff_attention(*a, causal=True)["out"][0] * do.double()).sum())
@@ -395,12 +395,12 @@ def test_rotary_before_quadtree_attention(dev):
 def test_dense_on_another_stream(dev):
     q, k, v, lam, do = make(dev, 1, 200, 500, 4, 2, 64, "bf16", seed=41)
     out, kept = P.diff_attn(q, k, v, lam, keep=True)
-    want = [out, *P.diff_attn_backward(q, k, v, lam, out, kept, do)]
+    want = [out, *P.diff_attn_backward(q, k, v, lam, kept, do)]
     torch.cuda.synchronize()
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
         out, kept = P.diff_attn(q, k, v, lam, keep=True)
-        got = [out, *P.diff_attn_backward(q, k, v, lam, out, kept, do)]
+        got = [out, *P.diff_attn_backward(q, k, v, lam, kept, do)]
     s.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, got))
 
@@ -415,7 +415,7 @@ def test_dense_calls_in_a_graph(dev):
         qr = P.rotary(q, freqs)
         kr = P.rotary(k, freqs)
         out, kept = P.diff_attn(qr, kr, v, lam, lens=lens, keep=True)
-        return [out, *P.diff_attn_backward(qr, kr, v, lam, out, kept, do, lens=lens)]
+        return [out, *P.diff_attn_backward(qr, kr, v, lam, kept, do, lens=lens)]
 
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
@@ -463,9 +463,9 @@ def test_dense_refusals(dev):
         P.diff_attn(torch.zeros(2 * 8 * 8 * 32 + 1, device=dev)[1:].view(2, 8, 8, 32), k, v, lam)
     out, kept = P.diff_attn(q, k, v, lam, keep=True)
     with pytest.raises(ValueError):
-        P.diff_attn_backward(q, k, v, lam, out, kept, do.transpose(1, 2).contiguous().transpose(1, 2))
+        P.diff_attn_backward(q, k, v, lam, kept, do.transpose(1, 2).contiguous().transpose(1, 2))
     with pytest.raises(ValueError):
-        P.diff_attn_backward(q, k, v, lam, out, (kept[0], kept[1][:, :2]), do)
+        P.diff_attn_backward(q, k, v, lam, (kept[0], kept[1][:, :2]), do)
     x, f = q, P.rotary_freqs(32, device=dev)
     badr = lambda *a, **w: pytest.raises((ValueError, P.QtaError), P.rotary, *a, **w)
     badr(x, f.float())
@@ -489,9 +489,9 @@ def test_dense_empty(dev):
     assert P.diff_attn(q[:0], k[:0], v[:0], lam).shape == (0, 8, 4, 64)
     out, kept = P.diff_attn(q, k[:, :0], v[:, :0], lam, keep=True)
     assert float(out.abs().max()) == 0.0
-    grads = P.diff_attn_backward(q, k[:, :0], v[:, :0], lam, out, kept, do)
+    grads = P.diff_attn_backward(q, k[:, :0], v[:, :0], lam, kept, do)
     assert [g.shape for g in grads] == [q.shape, (2, 0, 4, 32), (2, 0, 2, 64), lam.shape]
     assert float(grads[0].abs().max()) == 0.0 and float(grads[3].abs().max()) == 0.0
-    grads = P.diff_attn_backward(q[:, :0], k, v, lam, out[:, :0], (kept[0][:, :0], kept[1][..., :0]), do[:, :0])
+    grads = P.diff_attn_backward(q[:, :0], k, v, lam, (kept[0][:, :0], kept[1][..., :0]), do[:, :0])
     assert float(grads[1].abs().max()) == 0.0 and float(grads[2].abs().max()) == 0.0
     assert P.rotary(q[:, :0], P.rotary_freqs(32, device=dev)).shape == (2, 0, 8, 32)
