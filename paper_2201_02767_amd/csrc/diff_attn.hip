@@ -24,7 +24,7 @@ constexpr float kLag = 8.0f;
 // keys, two of them in LDS. With a.splits > 1 a workgroup takes one part of its rows' keys and leaves the results as they
 // are, with their maxima and sums, to diff_join_kernel.
 template <typename T, int D, int BN, bool KEYS>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (KEYS ? 2 : 4) : 1) void diff_fwd_kernel(DiffArgs a)
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (KEYS ? 2 : 3) : 1) void diff_fwd_kernel(DiffArgs a)
 {
     using KT = Tile<T, D>;
     using VT = Tile<T, 2 * D>;
@@ -195,6 +195,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (KEYS ? 2 : 4) : 1) void
     __syncthreads();
     if (map == 1 || kb == 1 || rr >= a.R) return;
     const float lam = diff_lambda(a, b, qi, h);
+    T* const out = static_cast<T*>(a.out) + row * (2 * D) + 4 * half;
+    float* const maps = a.maps + row * (4 * D) + 4 * half;
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
@@ -205,11 +207,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (KEYS ? 2 : 4) : 1) void
                 o0[j] = acc[c][e + j] * inv;
                 o1[j] = box[(c * 16 + e + j) * 64];
             }
-            const int ch = 32 * c + acc_row(e, half);
-            store4<T>(a.out, row * (2 * D) + ch, o0[0] - lam * o1[0], o0[1] - lam * o1[1], o0[2] - lam * o1[2], o0[3] - lam * o1[3]);
+            const int ch = 32 * c + 2 * e;
+            store4<T>(out, ch, o0[0] - lam * o1[0], o0[1] - lam * o1[1], o0[2] - lam * o1[2], o0[3] - lam * o1[3]);
             if (a.maps) {
-                store4<float>(a.maps, row * (4 * D) + ch, o0[0], o0[1], o0[2], o0[3]);
-                store4<float>(a.maps, row * (4 * D) + 2 * D + ch, o1[0], o1[1], o1[2], o1[3]);
+                store4<float>(maps, ch, o0[0], o0[1], o0[2], o0[3]);
+                store4<float>(maps, 2 * D + ch, o1[0], o1[1], o1[2], o1[3]);
             }
         }
 }
