@@ -43,7 +43,15 @@ struct DiffArgs {
     float* part_sums;
 };
 
-// How a forward's keys are split. @2@
+// How a forward's keys are split. Up to 32 rows of a key head (a token or a few, of all the query heads that share it): the
+// waves of a workgroup take halves of each key tile, since half of them would find no rows (16 tokens over caches of 16384
+// to 32768 keys, 32 heads over 8, d = 64, bf16: 265 us, by rows 292; 8 x 5 tokens over 4097 keys, 16 heads over 4,
+// d = 32, fp32: 22 us, by rows 32). And where the rows do not give every unit a workgroup (fp32, whose products take 16
+// times as long: two), the keys come in parts that make four workgroups a unit, none below 256 keys (4800 fp32 tokens,
+// 4 heads, d = 32: 510 us whole, 381 in two parts, 327 in four; the long caches: 289 us with two workgroups a unit, 274 with
+// four, 280 with eight; the fp32 caches: 31 us in parts of 256 keys, 38 in parts of 128). Parts cost a write and a read
+// of fp32 results: 3 x 1031 bf16 tokens over 1777, 8 heads, d = 32, which are 408 workgroups, take 31 us, in three
+// parts 30 and 14 to join them.
 struct DiffParts {
     bool keys_apart;
     int splits;
@@ -316,7 +324,8 @@ constexpr int kDiffKeys = 128;  // keys of a workgroup of the key pass
 // Parts of the key pass's rows. One key head's keys in tiles of 128 may be few workgroups, and under a causal mask the
 // first tile meets all rows and the last only its own; parts cost a write and a read of fp32 sums. Two workgroups run on a
 // unit: as many parts as fill the units twice where work is even and four times where it is causal, no part below
-// 4 tiles of 32 rows, at most 8. (2 x 4096 keys, 16 heads over 4, d = 64, bf16, causal: @1@)
+// 4 tiles of 32 rows, at most 8. (2 x 4096 keys, 16 heads over 4, d = 64, bf16, causal: in 2 parts 472 us
+// and 14 to join them, in 4 parts 357 and 23, in 6 parts 354 and 33.)
 inline int diff_key_splits(int B, int kv_heads, int Nk, int R, bool causal)
 {
     const long long groups = static_cast<long long>(B) * kv_heads * ((Nk + kDiffKeys - 1) / kDiffKeys);
@@ -326,11 +335,12 @@ inline int diff_key_splits(int B, int kv_heads, int Nk, int R, bool causal)
     return static_cast<int>(s < 1 || most < 1 ? 1 : (s > most ? most : s) > 8 ? 8 : (s > most ? most : s));
 }
 
-// Parts of the query pass's keys: enough to fill the units twice, none below 256 keys, at most 16.
+// Parts of the query pass's keys: enough to give every unit a workgroup, none below 256 keys, at most 16 (2 x 997 causal
+// tokens, 8 heads, d = 32, fp32: 103 us whole, 53 in two parts, 60 in three).
 inline int diff_query_splits(int B, int kv_heads, int Nk, int R)
 {
     const long long groups = static_cast<long long>(B) * kv_heads * ((R + 127) / 128), most = Nk / 256;
-    const long long s = (2LL * device_cu_count() + groups - 1) / groups;
+    const long long s = (device_cu_count() + groups - 1) / groups;
     return static_cast<int>(s < 1 || most < 1 ? 1 : (s > most ? most : s) > 16 ? 16 : (s > most ? most : s));
 }
 

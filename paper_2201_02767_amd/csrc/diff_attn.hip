@@ -3,6 +3,12 @@
 // One pass over the keys with running maxima and sums, S^T = K Q^T so that a lane holds one query's scores and its
 // rescaling is a lane's own. The two softmax maps share nothing but V and the rows, so a wave takes one map of 32 rows, and
 // the difference is formed once at the end through LDS.
+//
+// What bounds it: long prompts the matrix and the vector units together, at the clock that their power leaves (2 x 8192 causal
+// tokens, 16 heads over 4, d = 64, bf16: 830 us, 994 TFLOP/s of products at 1.9 GHz, where a large library product reaches
+// 1305); single tokens the caches' bytes (1.6 GB: 265 us, 6 TB/s). Four waves a SIMD with a few spills: 806 us, but 264 instead
+// of 236 for the forward of training, which writes more; one wave over 64 rows: 793 us, none gained in training;
+// tiles of 64 keys: 895 us; a pipeline over three tiles that alternates matrix and vector instructions: 930 us.
 #include <atomic>
 #include <type_traits>
 
@@ -244,12 +250,19 @@ __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffArgs a)
         x[m] = a.part + at * (2 * D) + lane * V;
     }
     piece o[2] = {};
-#pragma unroll 8
-    for (int s = 0; s < a.splits; ++s)
+    // four parts' loads in flight together (behind the last part: that one again, with the weight 0 of its lane)
+    for (int s = 0; s < a.splits; s += 4) {
+        piece y[4][2];
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
-            o[m] += *reinterpret_cast<const piece*>(x[m] + s * step * (2 * D)) *
-                    __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f[m]), s));
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+                y[j][m] = *reinterpret_cast<const piece*>(x[m] + min(s + j, a.splits - 1) * step * (2 * D));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) o[m] += y[j][m] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f[m]), s + j));
+    }
     const float lam = diff_lambda(a, b, qi, h);
     const long long row = (static_cast<long long>(b) * a.Nq + qi) * a.heads + h;
 #pragma unroll
@@ -292,6 +305,7 @@ template <typename T, int D>
 hipError_t launch_type(const DiffArgs& a, hipStream_t stream)
 {
     if (a.keys_apart) return launch_fwd<T, D, 64, true>(a, stream);
+    // tiles of 64 keys where they leave LDS for four workgroups a unit: 33 us against 38 for 3 x 1031 bf16 tokens over 1777
     return launch_fwd<T, D, sizeof(T) == 2 && D == 32 ? 64 : 32, false>(a, stream);
 }
 

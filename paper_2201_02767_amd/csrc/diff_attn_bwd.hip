@@ -492,6 +492,7 @@ __global__ __launch_bounds__(kThreads) void diff_dkv_join_kernel(DiffBwdArgs a)
     if (item >= total) return;
     const f32x4* p = reinterpret_cast<const f32x4*>(a.part) + item;
     f32x4 x = *p;
+#pragma unroll 4
     for (int s = 1; s < a.splits; ++s) x += p[s * total];
     const long long row = item / D;
     const int c = 4 * static_cast<int>(item - row * D);

@@ -300,4 +300,6 @@ class _DiffAttention(torch.autograd.Function):
 
 def diff_attention(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None):
     """Differentiable ``diff_attn``: gradients of q, k, v and lam."""
+    if not (torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in (q, k, v, lam))):
+        return diff_attn(q, k, v, lam, scale=scale, causal=causal, lens=lens, q_pos=q_pos)
     return _DiffAttention.apply(q, k, v, lam, scale, causal, lens, q_pos)
