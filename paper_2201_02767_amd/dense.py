@@ -146,6 +146,8 @@ def _rotate(xs, freqs, pos, axes, interleaved, scale, start, inverse, inplace=Fa
         for t, y, s in zip(xs, ys, shapes)])
     _call("qta_rotary", x, ctypes.addressof(table), len(xs), B, N, d, 2 * freqs.numel(), axes,
           x.shape[2] if x.dim() == 5 else 0, interleaved, inverse, code, freqs.data_ptr(), at, pos_batch, start, scale)
+    if inplace:
+        torch.autograd.graph.increment_version(xs)      # (for what autograd may have kept of them)
     return ys
 
 

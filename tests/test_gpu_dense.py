@@ -232,6 +232,38 @@ def test_diff_attn_against_differences(dev):
             assert abs(num - ana) <= 1e-5 * float((g.double() * step).abs().sum()) + 1e-6, (i, num, ana)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_diff_attn_parts_of_ragged_caches(dev, dtype):
+    """Few rows over many keys, whose parts are joined: some elements have fewer keys than there are parts, one has none,
+    and a causal call whose first rows see nothing."""
+    lens = [0, 1, 300, 3000, 2049]
+    check(dev, *make(dev, 5, 1, 3000, 8, 2, 64, dtype, seed=51), lens=lens)
+    check(dev, *make(dev, 5, 3, 3000, 16, 2, 32, dtype, seed=52), lens=lens, causal=True, q_pos=[0, -1, 297, 2997, -5])
+    check(dev, *make(dev, 5, 1, 3000, 64, 1, 32, dtype, seed=53), lens=lens)            # 64 rows of one key head
+
+
+def test_diff_attn_rows_past_32_bits(dev):
+    """An output of more than 2^31 elements: its last rows are those of a call on these rows alone."""
+    N, heads, d = 270000, 64, 64
+    r = gen(54, dev)
+    q = torch.empty(1, N, 2 * heads, d, dtype=torch.bfloat16, device=dev)
+    q[:, -200:] = r(1, 200, 2 * heads, d).bfloat16()
+    q[:, :-200] = q[:, -1:]
+    k, v = r(1, 40, 2 * heads, d).bfloat16(), r(1, 40, heads, 2 * d).bfloat16()
+    lam = 0.5 + 0.1 * r(heads)
+    out = P.diff_attn(q, k, v, lam)
+    assert out.numel() > 2 ** 31
+    within("last rows", out[:, -200:], R.diff_attention(q[:, -200:], k, v, lam)["out"])
+    freqs = P.rotary_freqs(d, device=dev)
+    del out
+    turned = P.rotary(q, freqs, inplace=True)
+    torch.cuda.synchronize()
+    p = torch.arange(N - 200, N, device=dev)[None, :, None]
+    again = r(1, 200, 2 * heads, d).bfloat16()
+    q[:, -200:] = again
+    within("last positions", P.rotary(turned, freqs)[:, -200:], R.rotary(again, freqs, p))
+
+
 # ---- rotary positions ----
 
 ROTARY = [  # B, N, heads, k_heads, d, rot
@@ -434,6 +466,97 @@ def test_dense_calls_in_a_graph(dev):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, held))
+
+
+def test_dense_calls_with_parts_in_a_graph(dev):
+    """Calls whose keys, rows and query parts are joined from a workspace, replayed beside eager ones of the same shapes."""
+    q, k, v, lam, do = make(dev, 1, 40, 2600, 4, 1, 64, "bf16", seed=44)
+
+    def step():
+        out, kept = P.diff_attn(q, k, v, lam, keep=True)
+        return [out, P.diff_attn(q[:, :1], k, v, lam), *P.diff_attn_backward(q, k, v, lam, kept, do)]
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            held = step()
+        graphs.append((g, held))
+    r = gen(45, dev)
+    for _ in range(3):
+        for t in (q, k, v, do):
+            t.copy_(r(*t.shape))
+        want = step()
+        for g, held in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for _, held in graphs:
+            assert all(torch.equal(a, b) for a, b in zip(want, held))
+
+
+def test_dense_calls_on_two_streams_at_once(dev):
+    q, k, v, lam, do = make(dev, 2, 3, 6000, 8, 2, 64, "bf16", seed=46)
+    want = P.diff_attn(q, k, v, lam)
+    out, kept = P.diff_attn(q, k, v, lam, keep=True)
+    wantg = P.diff_attn_backward(q, k, v, lam, kept, do)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append((P.diff_attn(q, k, v, lam), *P.diff_attn_backward(q, k, v, lam, kept, do)))
+    torch.cuda.synchronize()
+    for g in got[0] + got[1]:
+        assert all(torch.equal(a, b) for a, b in zip(g, (want, *wantg)))
+
+
+# ---- autograd ----
+
+def test_diff_attention_autograd(dev):
+    """Gradients through autograd are those of the calls: for an expanded and a misaligned upstream gradient, with some
+    inputs that need none, for a map, and for a weight a token; none are kept where none are asked for."""
+    q, k, v, lam, do = make(dev, 2, 30, 50, 4, 2, 32, "bf16", seed=61, token_lam=True)
+    leaves = [t.clone().requires_grad_() for t in (q, k, v, lam)]
+    out, kept = P.diff_attn(q, k, v, lam, keep=True)
+    want = P.diff_attn_backward(q, k, v, lam, kept, do)
+    got = torch.autograd.grad(P.diff_attention(*leaves), leaves, do)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    off = torch.zeros(do.numel() + 1, dtype=do.dtype, device=dev)[1:].view(do.shape).copy_(do)
+    got = torch.autograd.grad(P.diff_attention(*leaves), leaves, off)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    ones = P.diff_attn_backward(q, k, v, lam, kept, torch.ones_like(do))
+    got = torch.autograd.grad(P.diff_attention(*leaves).sum(), leaves)
+    assert all(torch.equal(a, b) for a, b in zip(ones, got))
+    y = P.diff_attention(q, leaves[1], v, lam)
+    assert torch.equal(torch.autograd.grad(y, leaves[1], do)[0], want[1])
+    maps = [t.unflatten(1, (-1, 5)) for t in leaves]
+    got = torch.autograd.grad(P.diff_attention(*maps), leaves, do.unflatten(1, (-1, 5)))
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    with torch.no_grad():
+        assert not P.diff_attention(*leaves).requires_grad
+    assert not P.diff_attention(q, k, v, lam).requires_grad
+
+
+def test_turning_in_place_is_seen_by_autograd(dev):
+    x = torch.randn(1, 3, 2, 32, device=dev)
+    w = torch.ones(1, requires_grad=True, device=dev)
+    y = (x * w).sum()
+    P.rotary(x, P.rotary_freqs(32, device=dev), inplace=True)
+    with pytest.raises(RuntimeError):
+        y.backward()
+
+
+def test_gradients_of_gradients_are_refused(dev):
+    q, k, v, lam, do = make(dev, 1, 4, 4, 2, 1, 32, "f32", seed=62)
+    q.requires_grad_()
+    g, = torch.autograd.grad(P.diff_attention(q, k, v, lam), q, do.requires_grad_(), create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
 
 
 # ---- refusals of the binding ----
