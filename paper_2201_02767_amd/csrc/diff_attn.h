@@ -298,6 +298,7 @@ struct DiffBwdArgs {
     const void* dout;           // [B][Nq][heads][2d] contiguous
     // by rows of one key head, [B][kv_heads][kDiffStats][Rpad] fp32. With s the logits' scale, S the sign of lambda:
     // -lse_0 / s, -(lse_1 - log2 |lambda|) / s, -t_0, -S (t_0 - t_1), -S for the key pass; -lse_1 / s, t_0 - t_1, t_1
+    // (fp32 inputs: the first two and the sixth without the division)
     float* stats;
     int Rpad;                   // R rounded up to kDiffRowPad; rows behind R are zero
     void* dq;                   // [B][Nq][2 heads][d]

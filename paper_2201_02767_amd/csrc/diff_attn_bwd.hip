@@ -7,8 +7,8 @@
 // rows of every query head that shares them. D, and in the key pass V's weights, serve both maps, so here a wave
 // holds both. Each result is summed in one order: no atomics, the same bits every run.
 //
-// D starts from -t_0 instead of zero, and in the key pass, where a statistic is needed for every register, Q K^T from
-// -lse / scale: a weight is then one product and one power of two away. t_m comes from results whose weights were rounded;
+// D starts from -t_0 instead of zero, and in the key pass of bf16 inputs, where a statistic is needed for every register,
+// Q K^T from -lse / scale: a weight is then one product and one power of two away. t_m comes from results whose weights were rounded;
 // the rows of P_1 (D - t_1), which with the exact t_1 sum to zero, give what is missing, and dlambda is exact to fp32.
 #include <atomic>
 #include <type_traits>
@@ -29,6 +29,11 @@ __device__ __forceinline__ void store_dlambda(const DiffBwdArgs& a, int b, int i
     else if (a.f.lam_bf16) Storage<bf16>::store1(a.dlam, row * a.f.heads + h, x);
     else Storage<float>::store1(a.dlam, row * a.f.heads + h, x);
 }
+
+// Whether the key pass starts Q K^T from -lse / scale (bf16), or from zero as fp32 inputs need: the sum would be rounded at the
+// size of lse / scale (dK and dV of 4000 rows and 300 keys, d = 64: 1.2e-6 off, from zero 6.6e-7, a plain fp32 form 7e-7).
+template <typename T>
+__device__ __forceinline__ constexpr bool from_statistics() { return sizeof(T) == 2; }
 
 // ---- the rows' statistics ----
 
@@ -74,7 +79,7 @@ __global__ __launch_bounds__(kThreads) void diff_rows_kernel(DiffBwdArgs a)
         t1 += xchg_f32<16>(t1);
     }
     if (c != 0) return;
-    const float lam = diff_lambda(f, b, i, h), inv = -1.0f / f.scale;
+    const float lam = diff_lambda(f, b, i, h), inv = from_statistics<T>() ? -1.0f / f.scale : -1.0f;
     const float* const lse = f.lse + (static_cast<long long>(b) * f.heads + h) * 2 * f.Nq + i;
     const float l0 = lse[0], l1 = lse[f.Nq];
     const float nsign = lam < 0.f ? 1.0f : -1.0f;
@@ -130,7 +135,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
     const int qi = fast_div(r, f.div_G), h = g * G + r - qi * G, lim = range.limit(qi);
     const float* const st = a.stats + static_cast<size_t>(bh) * kDiffStats * a.Rpad + r;
     const size_t plane = a.Rpad;
-    const float nlse0 = st[0] * f.scale, nlse1 = st[5 * plane] * f.scale, nt0 = st[2 * plane], t01 = st[6 * plane], t1 = st[7 * plane];
+    const float unit = from_statistics<T>() ? f.scale : 1.0f;
+    const float nlse0 = st[0] * unit, nlse1 = st[5 * plane] * unit, nt0 = st[2 * plane], t01 = st[6 * plane], t1 = st[7 * plane];
     const float nlam = -diff_lambda(f, b, qi, h);
     float miss = 0.f;                       // sum of P_1 (D - t_1)
     Frag<T> qf[2][D / 16], of[D / 8];
@@ -401,20 +407,21 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
             float w[16];
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                f32x16 s = from(m);
+                f32x16 s = from_statistics<T>() ? from(m) : f32x16{};
 #pragma unroll
                 for (int c = 0; c < D / 16; ++c) s = mma(QT::row_frag(qrow, cur + m * kQ, 0, c), kf[m][c], s);
                 float ds[16];
 #pragma unroll
                 for (int e = 0; e < 16; e += 4) {
-                    f32x4 t{}, sign{};
+                    f32x4 t{}, sign{}, nlse{};
+                    if constexpr (!from_statistics<T>()) nlse = stat(m, e);
                     if (m == 1) {
                         t = stat(3, e);
                         sign = stat(4, e);
                     }
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float p = exp2_fast(s[e + j] * f.scale);
+                        const float p = exp2_fast(from_statistics<T>() ? s[e + j] * f.scale : fmaf(s[e + j], f.scale, nlse[j]));
                         ds[e + j] = p * (m == 0 ? dp[e + j] : fmaf(sign[j], dp[e + j], t[j]));
                         w[e + j] = m == 0 ? p : fmaf(sign[j], p, w[e + j]);
                     }
