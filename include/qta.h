@@ -12,6 +12,8 @@
  *   5. the per-level messages are combined: QuadTree-A sums partial messages over the disjoint
  *      regions Omega^l (Eqs. 2-4), QuadTree-B takes a weighted sum of per-level attention over
  *      the overlapping regions Gamma^l (Eqs. 5-6).
+ * Beside it, at the end of this file: rotary positions (qta_rotary) and dense differential attention (qta_diff_attn),
+ * whose shapes, supported sizes and outputs stand with them; what is said below on memory and errors holds for all calls.
  *
  * Conventions shared by every call
  *   - Level l = 0 is the finest level (the input map), l = L-1 the coarsest. Level l+1 has
