@@ -64,7 +64,7 @@ inline DiffParts diff_key_parts(int B, int kv_heads, int Nk, int R, bool bf16_in
     if (tiles >= (bf16_inputs ? cus : 2 * cus) && R > 32) return p;
     p.keys_apart = R <= 32;
     const long long work = groups * ((R + (p.keys_apart ? 31 : 63)) / (p.keys_apart ? 32 : 64));
-    const long long want = (4 * cus + work - 1) / work, most = Nk / 256;
+    const long long want = (4 * cus + work - 1) / work, most = bf16_inputs && Nk < 1024 ? 1 : Nk / 256;
     p.splits = static_cast<int>(most < 1 ? 1 : want < 1 ? 1 : want > most ? most : want);
     if (p.splits > 64) p.splits = 64;
     return p;

@@ -85,6 +85,11 @@ def _call(name, t, *args):
         _check(name, status)
 
 
+def _new(t):
+    """A contiguous tensor like t."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 # ------------------------------------------------------------------------------------------------
 # rotary positions
 # ------------------------------------------------------------------------------------------------
@@ -138,12 +143,13 @@ def _rotate(xs, freqs, pos, axes, interleaved, scale, start, inverse, inplace=Fa
             raise ValueError("a broadcast tensor cannot be turned in place")
         ys = xs
     else:
-        ys = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in xs]
-    if B == 0 or N == 0 or all(t.numel() == 0 for t in xs):
+        ys = [_new(t) for t in xs]
+    if B == 0 or N == 0 or d == 0:
         return ys
-    table = (RotaryTensor * len(xs))(*[
-        RotaryTensor(t.data_ptr(), y.data_ptr(), s[2], *s[4:], *(s[4:] if inplace else (N * s[2] * d, s[2] * d, d)))
-        for t, y, s in zip(xs, ys, shapes)])
+    table = (RotaryTensor * len(xs))()
+    for e, t, y, (_, _, heads, _, b, n, h) in zip(table, xs, ys, shapes):
+        row = heads * d
+        e.__init__(t.data_ptr(), y.data_ptr(), heads, b, n, h, *((b, n, h) if inplace else (N * row, row, d)))
     _call("qta_rotary", x, ctypes.addressof(table), len(xs), B, N, d, 2 * freqs.numel(), axes,
           x.shape[2] if x.dim() == 5 else 0, interleaved, inverse, code, freqs.data_ptr(), at, pos_batch, start, scale)
     if inplace:
@@ -175,9 +181,9 @@ def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.
     (``[.., N, 2]`` for two axes, N = H*W on a map); None: ``start`` + 0, 1, .. along a sequence, the coordinates of a map.
     ``interleaved``: pairs are neighbouring channels instead of the two halves of an axis. ``inverse``: turn back.
     ``inplace``: overwrite x and k (and return them); not differentiable."""
-    xs = [x] if k is None else [x, k]
+    xs = (x,) if k is None else (x, k)
     how = (axes, bool(interleaved), float(scale), int(start))
-    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in xs):
+    if torch.is_grad_enabled() and (getattr(x, "requires_grad", False) or getattr(k, "requires_grad", False)):
         if inplace:
             raise ValueError("in-place rotation of a tensor that requires gradients")
         if inverse:
@@ -272,7 +278,7 @@ def diff_attn_backward(q, k, v, lam, kept, dout, *, scale=None, causal=False, le
                            (lse, "kept", torch.float32, (args.B, args.heads, 2, args.Nq)), (dout, "dout", q.dtype, shape)):
         if t.dtype is not dtype or t.device != q.device or t.shape != s or not t.is_contiguous():
             raise ValueError(f"{n} must be contiguous {dtype} {tuple(s)} on {q.device}")
-    grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v, lam)]
+    grads = [_new(t) for t in (q, k, v, lam)]
     if args.Nk == 0 or dout.numel() == 0:
         return tuple(g.zero_() for g in grads)
     ws, nbytes = _workspace("qta_diff_attn_backward_workspace_bytes", args, q)
