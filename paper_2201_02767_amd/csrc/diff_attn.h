@@ -49,7 +49,8 @@ struct DiffArgs {
 // d = 32, fp32: 22 us, by rows 32). And where the rows do not give every unit a workgroup (fp32, whose products take 16
 // times as long: two), the keys come in parts that make four workgroups a unit, none below 256 keys (4800 fp32 tokens,
 // 4 heads, d = 32: 510 us whole, 381 in two parts, 327 in four; the long caches: 289 us with two workgroups a unit, 274 with
-// four, 280 with eight; the fp32 caches: 31 us in parts of 256 keys, 38 in parts of 128). Parts cost a write and a read
+// four, 280 with eight; the fp32 caches: 31 us in parts of 256 keys, 38 in parts of 128; below 1024 bf16 keys the second
+// launch costs more than it gives: 512 keys, 8 heads, d = 64, 12 us a call whole, 16 in two parts). Parts cost a write and a read
 // of fp32 results: 3 x 1031 bf16 tokens over 1777, 8 heads, d = 32, which are 408 workgroups, take 31 us, in three
 // parts 30 and 14 to join them.
 struct DiffParts {
@@ -141,7 +142,7 @@ __device__ __forceinline__ Frag<T> global_frag(const void* base, long long elem)
     return f;
 }
 
-// Result rows 8s .. 8s + 7 (in the order above) as a fragment. bf16: rounded to nearest, 2^-9 of each value at
+// Result rows 8s .. 8s + 7 (in the order above) as a fragment. bf16: rounded to nearest, 2^-8 of each value at
 // most, once, as the matrix product asks; sums of weights are taken from the fp32 values.
 template <typename T>
 __device__ __forceinline__ Frag<T> pack_frag(const float* x)
@@ -186,8 +187,8 @@ struct Tile {
         else return ((r >> 2) & 1) << 3 | (r & 3) << 1 | ((r >> 3) & 1);
     }
 
-    // Brings `rows` rows in (a multiple of 64 / kChunks times the waves taking part), each wave its share, 1 KB an
-    // instruction straight to LDS: `off(r)` is the byte offset of row r in `map`.
+    // Brings `rows` rows in (a multiple of 64 / kChunks), each wave its share, 1 KB an instruction straight to LDS:
+    // `off(r)` is the byte offset of row r in `map`.
     template <typename Off>
     __device__ static __forceinline__ void stage(lds_byte* tile, __amdgpu_buffer_rsrc_t map, int rows, int wave, int waves,
                                                  int lane, Off off)

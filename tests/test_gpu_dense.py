@@ -129,6 +129,18 @@ def test_what_lies_behind_the_lengths_is_not_used(dev, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Nq", [3, 20, 70])
+def test_keys_that_no_causal_query_sees_are_not_used(dev, Nq, dtype):
+    """A cache without lengths: what lies behind the last query's position may be anything, also in the gradients."""
+    q, k, v, lam, do = make(dev, 2, Nq, 400, 4, 2, 32, dtype, seed=18)
+    rk, rv = k.clone(), v.clone()
+    at = [50, 301]
+    for b, p in enumerate(at):
+        k[b, p + Nq:], v[b, p + Nq:] = math.nan, -math.inf
+    check(dev, q, k, v, lam, do, causal=True, q_pos=at, ref_kv=(rk, rv))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_diff_attn_weights(dev, dtype):
     """lambda zero, negative and large; in both types; a negative zero length of nothing."""
     q, k, v, _, do = make(dev, 2, 33, 90, 4, 2, 32, dtype, seed=8)
