@@ -297,9 +297,8 @@ __device__ __forceinline__ float other_half(float x) { return xchg_f32<32>(x); }
 struct DiffBwdArgs {
     DiffArgs f;                 // maps and lse are the forward's (read)
     const void* dout;           // [B][Nq][heads][2d] contiguous
-    // by rows of one key head, [B][kv_heads][kDiffStats][Rpad] fp32. With s the logits' scale, S the sign of lambda:
-    // -lse_0 / s, -(lse_1 - log2 |lambda|) / s, -t_0, -S (t_0 - t_1), -S for the key pass; -lse_1 / s, t_0 - t_1, t_1
-    // (fp32 inputs: the first two and the sixth without the division)
+    // by rows of one key head, for the key pass: [B][kv_heads][kDiffStats][Rpad] fp32. With s the logits' scale, S the sign
+    // of lambda: -lse_0 / s, -(lse_1 - log2 |lambda|) / s (fp32 inputs: both without the division), -t_0, -S (t_0 - t_1), -S
     float* stats;
     int Rpad;                   // R rounded up to kDiffRowPad; rows behind R are zero
     void* dq;                   // [B][Nq][2 heads][d]
@@ -312,14 +311,15 @@ struct DiffBwdArgs {
     // the key pass in `splits` parts of the rows: fp32 [splits][B][Nk][kv_heads][4d] sums of dK_0, dK_1 and dV (splits > 1)
     int splits;
     float* part;
+    int key_groups;             // workgroups of the key pass that have keys; set by the launcher
     // the query pass in `q_splits` parts of the keys: fp32 [q_splits][B][kv_heads][R][2][d] sums of dQ_0 and dQ_1, and
-    // [..][R] those of P_1 (D - t_1) (q_splits > 1)
+    // [..][R] those of P_1 (D - t_1), the first part's plus t_1 (q_splits > 1)
     int q_splits;
     float* q_part;
     float* q_miss;
 };
 constexpr float kDiffLn2 = 0.693147180559945f;
-constexpr int kDiffStats = 8;
+constexpr int kDiffStats = 5;
 constexpr int kDiffRowPad = 64;
 constexpr int kDiffKeys = 128;  // keys of a workgroup of the key pass
 

@@ -3,9 +3,11 @@
 // With D = dO V^T, t_m = dO . O_m (O_m = P_m V) and the weights made again from the stored sums:
 //   dS_0 = P_0 (D - t_0),   dS_1 = -lambda P_1 (D - t_1),   dlambda = -t_1
 //   dQ_m = scale dS_m K_m,  dK_m = scale dS_m^T Q_m,        dV = (P_0 - lambda P_1)^T dO
-// Launches: the rows' statistics; dQ, a wave taking 32 rows through the keys; dK and dV, a wave taking 32 keys through the
-// rows of every query head that shares them. D, and in the key pass V's weights, serve both maps, so here a wave
-// holds both. Each result is summed in one order: no atomics, the same bits every run.
+// Two passes: dQ, a wave taking 32 rows through the keys, which also leaves the rows' statistics for dK and dV, a wave
+// taking 32 keys through the rows of every query head that shares them. D, and in the key pass V's weights, serve both
+// maps, so here a wave holds both. Each result is summed in one order: no atomics, the same bits every run.
+// The query pass has dO at hand for t_m, and a launch before it for the statistics has to read dO again: 28 us of 4096 rows,
+// 2 x 16 heads of d = 64 in bf16, 19 in the query pass. Sums of dlambda by head run beside the keys for a launch of 4.5 us.
 //
 // D starts from -t_0 instead of zero, and in the key pass of bf16 inputs, where a statistic is needed for every register,
 // Q K^T from -lse / scale: a weight is then one product and one power of two away. t_m comes from results whose weights were rounded;
@@ -35,81 +37,33 @@ __device__ __forceinline__ void store_dlambda(const DiffBwdArgs& a, int b, int i
 template <typename T>
 __device__ __forceinline__ constexpr bool from_statistics() { return sizeof(T) == 2; }
 
-// ---- the rows' statistics ----
+__device__ __forceinline__ float frag_elem(const Frag<bf16>& f, int j) { return static_cast<float>(f.v[j]); }
+__device__ __forceinline__ float frag_elem(const Frag<float>& f, int j) { return f.v[j]; }
 
-// A row (b, i, h) takes 2D / V lanes of one 16-byte chunk each.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void diff_rows_kernel(DiffBwdArgs a)
+// A weight for each head: its rows' gradients summed by one workgroup.
+__device__ __forceinline__ void sum_dlambda(const DiffBwdArgs& a, int head, float* part)
 {
-    constexpr int V = 16 / static_cast<int>(sizeof(T)), LPR = 2 * D / V;
-    const DiffArgs& f = a.f;
-    const int G = f.heads / f.kv_heads;
-    const long long item = (static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / LPR;
-    const int c = threadIdx.x % LPR;
-    const long long per = a.Rpad, total = per * f.B * f.kv_heads;
-    if (item >= total) return;
-    const int bh = static_cast<int>(item / per), r = static_cast<int>(item - bh * per);
-    float* const st = a.stats + static_cast<size_t>(bh) * kDiffStats * a.Rpad + r;
-    if (r >= f.R) {
-        if (c == 0)
+    const long long n = static_cast<long long>(a.f.B) * a.f.Nq;
+    const float* const p = a.dlam_rows + head * n;
+    float s[4] = {};
+    long long i = threadIdx.x;
+    for (; i + 3 * kThreads < n; i += 4 * kThreads)
 #pragma unroll
-            for (int p = 0; p < kDiffStats; ++p) st[static_cast<size_t>(p) * a.Rpad] = 0.f;
-        return;
-    }
-    const int b = bh / f.kv_heads, i = fast_div(r, f.div_G), h = (bh - b * f.kv_heads) * G + r - i * G;
-    const long long row = (static_cast<long long>(b) * f.Nq + i) * f.heads + h;
-    const uint4* const go = reinterpret_cast<const uint4*>(a.dout) + row * LPR + c;
-    const f32x4* const o = reinterpret_cast<const f32x4*>(f.maps + row * (4 * D) + c * V);
-    float x[V];
-    Storage<T>::unpack(*go, x);
-    float t0 = 0.f, t1 = 0.f;
-#pragma unroll
-    for (int j = 0; j < V; j += 4) {
-        const f32x4 y = o[j / 4], z = o[(2 * D + j) / 4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            t0 = fmaf(x[j + k], y[k], t0);
-            t1 = fmaf(x[j + k], z[k], t1);
-        }
-    }
-    t0 = group_sum<LPR < 16 ? LPR : 16>(t0);
-    t1 = group_sum<LPR < 16 ? LPR : 16>(t1);
-    if constexpr (LPR == 32) {
-        t0 += xchg_f32<16>(t0);
-        t1 += xchg_f32<16>(t1);
-    }
-    if (c != 0) return;
-    const float lam = diff_lambda(f, b, i, h), inv = from_statistics<T>() ? -1.0f / f.scale : -1.0f;
-    const float* const lse = f.lse + (static_cast<long long>(b) * f.heads + h) * 2 * f.Nq + i;
-    const float l0 = lse[0], l1 = lse[f.Nq];
-    const float nsign = lam < 0.f ? 1.0f : -1.0f;
-    const float x_[kDiffStats] = {l0 * inv, (l1 - __builtin_amdgcn_logf(fabsf(lam))) * inv, -t0, nsign * (t0 - t1), nsign,
-                                  l1 * inv, t0 - t1, t1};
-#pragma unroll
-    for (int p = 0; p < kDiffStats; ++p) st[static_cast<size_t>(p) * a.Rpad] = x_[p];
-}
-
-// A weight for each head: its rows' gradients summed, one workgroup a head.
-__global__ __launch_bounds__(1024) void diff_lambda_kernel(const float* rows, long long n, void* dlam, bool lam_bf16)
-{
-    __shared__ float part[16];
-    const float* const p = rows + blockIdx.x * n;
-    float s = 0.f;
-    for (long long i = threadIdx.x; i < n; i += 1024) s += p[i];
-    s = wave_sum_fast(s);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+        for (int j = 0; j < 4; ++j) s[j] += p[i + j * kThreads];
+    for (; i < n; i += kThreads) s[0] += p[i];
+    const float t = wave_sum_fast((s[0] + s[1]) + (s[2] + s[3]));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = t;
     __syncthreads();
     if (threadIdx.x != 0) return;
-    float t = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) t += part[i];
-    if (lam_bf16) Storage<bf16>::store1(dlam, blockIdx.x, t);
-    else Storage<float>::store1(dlam, blockIdx.x, t);
+    const float x = (part[0] + part[1]) + (part[2] + part[3]);
+    if (a.f.lam_bf16) Storage<bf16>::store1(a.dlam, head, x);
+    else Storage<float>::store1(a.dlam, head, x);
 }
 
 // ---- dQ ----
 
-// With `q_splits` > 1 a workgroup takes one part of its rows' keys and writes fp32 sums to `q_part` and `q_miss`.
+// With `q_splits` > 1 a workgroup takes one part of its rows' keys and writes fp32 sums to `q_part` and `q_miss` (the first
+// part's with t_1).
 template <typename T, int D, int BN>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kernel(DiffBwdArgs a)
 {
@@ -133,11 +87,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
 
     const int rr = row0 + wave * 32 + (lane & 31), r = min(rr, f.R - 1);
     const int qi = fast_div(r, f.div_G), h = g * G + r - qi * G, lim = range.limit(qi);
-    const float* const st = a.stats + static_cast<size_t>(bh) * kDiffStats * a.Rpad + r;
-    const size_t plane = a.Rpad;
-    const float unit = from_statistics<T>() ? f.scale : 1.0f;
-    const float nlse0 = st[0] * unit, nlse1 = st[5 * plane] * unit, nt0 = st[2 * plane], t01 = st[6 * plane], t1 = st[7 * plane];
-    const float nlam = -diff_lambda(f, b, qi, h);
     float miss = 0.f;                       // sum of P_1 (D - t_1)
     Frag<T> qf[2][D / 16], of[D / 8];
 #pragma unroll
@@ -148,6 +97,34 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
     const long long orow = ((static_cast<long long>(b) * f.Nq + qi) * f.heads + h) * (2 * D);
 #pragma unroll
     for (int s = 0; s < D / 8; ++s) of[s] = global_frag<T>(a.dout, orow + 16 * s + 8 * half);
+    // t_m, of this lane's half of the channels and then of both; the first part's workgroups leave what the key pass needs
+    float t0 = 0.f, t1 = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 8; ++s) {
+        const f32x4* const o = reinterpret_cast<const f32x4*>(f.maps + 2 * orow + 16 * s + 8 * half);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const f32x4 y = o[j], z = o[2 * D / 4 + j];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                t0 = fmaf(frag_elem(of[s], 4 * j + k), y[k], t0);
+                t1 = fmaf(frag_elem(of[s], 4 * j + k), z[k], t1);
+            }
+        }
+    }
+    t0 += other_half(t0);
+    t1 += other_half(t1);
+    const float lam = diff_lambda(f, b, qi, h), nlam = -lam, nt0 = -t0, t01 = t0 - t1;
+    const float* const lse = f.lse + (static_cast<long long>(b) * f.heads + h) * 2 * f.Nq + qi;
+    const float nlse0 = -lse[0], nlse1 = -lse[f.Nq];
+    if (split == 0 && half == 0 && rr < a.Rpad) {
+        const bool row = rr < f.R;
+        const float unit = from_statistics<T>() ? 1.0f / f.scale : 1.0f, nsign = lam < 0.f ? 1.0f : -1.0f;
+        const float x[kDiffStats] = {nlse0 * unit, (nlse1 + __builtin_amdgcn_logf(fabsf(lam))) * unit, nt0, nsign * t01, nsign};
+        float* const st = a.stats + static_cast<size_t>(bh) * kDiffStats * a.Rpad + rr;
+#pragma unroll
+        for (int p = 0; p < kDiffStats; ++p) st[static_cast<size_t>(p) * a.Rpad] = row ? x[p] : 0.f;
+    }
     f32x16 acc[2][D / 32];
 #pragma unroll
     for (int m = 0; m < 2; ++m)
@@ -235,7 +212,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
     if (rr >= f.R) return;
     if (a.q_splits > 1) {
         const long long at = (static_cast<long long>(split) * f.B * f.kv_heads + bh) * f.R + r;
-        if (half == 0) a.q_miss[at] = miss;
+        if (half == 0) a.q_miss[at] = split == 0 ? t1 + miss : miss;
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -276,7 +253,7 @@ __global__ __launch_bounds__(kThreads) void diff_dq_join_kernel(DiffBwdArgs a)
     store4<T>(a.dq, ((static_cast<long long>(b) * f.Nq + i) * f.heads + h) * (2 * D) + c, x[0] * a.grad_scale, x[1] * a.grad_scale,
               x[2] * a.grad_scale, x[3] * a.grad_scale);
     if (c != 0) return;
-    float miss = a.stats[(static_cast<size_t>(bh) * kDiffStats + 7) * a.Rpad + r];
+    float miss = 0.f;
     for (int s = 0; s < a.q_splits; ++s) miss += a.q_miss[s * rows + at];
     store_dlambda(a, b, i, h, -miss);
 }
@@ -298,8 +275,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
     const DiffArgs& f = a.f;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+    if (static_cast<int>(blockIdx.x) >= a.key_groups) {             // behind the key tiles: lambda's gradients, a head each
+        sum_dlambda(a, static_cast<int>(blockIdx.x) - a.key_groups, reinterpret_cast<float*>(lds_raw));
+        return;
+    }
     const int tiles_n = (f.Nk + BN - 1) / BN;
-    const int logical = xcd_remap(blockIdx.x, gridDim.x);
+    const int logical = xcd_remap(blockIdx.x, a.key_groups);
     const int bh = logical / (tiles_n * a.splits), rest = logical - bh * tiles_n * a.splits;
     const int tile = rest / a.splits, split = rest - tile * a.splits;      // the keys that most rows see first
     const int b = bh / f.kv_heads, g = bh - b * f.kv_heads, G = f.heads / f.kv_heads;
@@ -363,7 +344,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
             OT::stage(at + 2 * kQ, omap, BM, wave, 4, lane, ooff);
             // five statistics of the 32 rows, 128 bytes each (lanes behind the fifth repeat it)
             if (wave == 0) {
-                const int p = min(lane >> 3, 4);
+                const int p = min(lane >> 3, kDiffStats - 1);
                 tiles::load_lds16(smap, (static_cast<uint32_t>(p) * a.Rpad + r0 + 4 * (lane & 7)) * 4u, 0, at + 2 * kQ + kO);
             }
         };
@@ -508,20 +489,20 @@ __global__ __launch_bounds__(kThreads) void diff_dkv_join_kernel(DiffBwdArgs a)
 }
 
 template <typename T, int D>
-hipError_t launch_bwd(const DiffBwdArgs& a, hipStream_t stream)
+hipError_t launch_bwd(const DiffBwdArgs& args, hipStream_t stream)
 {
     static std::atomic<unsigned long long> configured_q{0}, configured_k{0};
     constexpr int ES = static_cast<int>(sizeof(T)), BN = 32;
+    DiffBwdArgs a = args;
     const long long bh = static_cast<long long>(a.f.B) * a.f.kv_heads;
-    constexpr int lpr = 2 * D * ES / 16;
-    const long long rblocks = (bh * a.Rpad * lpr + kThreads - 1) / kThreads;
-    const long long qblocks = (a.f.R + 127) / 128 * bh * a.q_splits, kblocks = (a.f.Nk + kDiffKeys - 1) / kDiffKeys * bh * a.splits;
-    if (rblocks > 0x7FFFFFFFLL || qblocks > 0x7FFFFFFFLL || kblocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    const long long qblocks = (a.f.R + 127) / 128 * bh * a.q_splits;
+    const long long kblocks = (a.f.Nk + kDiffKeys - 1) / kDiffKeys * bh * a.splits, heads = a.lam_heads ? a.f.heads : 0;
+    if (qblocks > 0x7FFFFFFFLL || kblocks + heads > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    a.key_groups = static_cast<int>(kblocks);
     hipError_t e = set_max_lds_once(reinterpret_cast<const void*>(&diff_dq_kernel<T, D, BN>), configured_q);
     if (e != hipSuccess) return e;
     e = set_max_lds_once(reinterpret_cast<const void*>(&diff_dkv_kernel<T, D>), configured_k);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((diff_rows_kernel<T, D>), dim3(static_cast<unsigned>(rblocks)), dim3(kThreads), 0, stream, a);
     hipLaunchKernelGGL((diff_dq_kernel<T, D, BN>), dim3(static_cast<unsigned>(qblocks)), dim3(kThreads), 2 * BN * 4 * D * ES,
                        stream, a);
     if (a.q_splits > 1) {
@@ -529,10 +510,7 @@ hipError_t launch_bwd(const DiffBwdArgs& a, hipStream_t stream)
         hipLaunchKernelGGL((diff_dq_join_kernel<T, D>), dim3(static_cast<unsigned>((items + kThreads - 1) / kThreads)),
                            dim3(kThreads), 0, stream, a);
     }
-    if (a.lam_heads)
-        hipLaunchKernelGGL(diff_lambda_kernel, dim3(static_cast<unsigned>(a.f.heads)), dim3(1024), 0, stream, a.dlam_rows,
-                           static_cast<long long>(a.f.B) * a.f.Nq, a.dlam, a.f.lam_bf16);
-    hipLaunchKernelGGL((diff_dkv_kernel<T, D>), dim3(static_cast<unsigned>(kblocks)), dim3(kThreads),
+    hipLaunchKernelGGL((diff_dkv_kernel<T, D>), dim3(static_cast<unsigned>(kblocks + heads)), dim3(kThreads),
                        2 * (32 * 4 * D * ES + 1024) + kDiffKeys * 2 * D * ES, stream, a);
     if (a.splits > 1) {
         const long long items = static_cast<long long>(a.f.B) * a.f.Nk * a.f.kv_heads * D;
