@@ -114,7 +114,8 @@ def rotary_freqs(rot, *, theta=10000.0, axes=1, factor=1.0, trained=None, low=1.
     return f.repeat(axes).to(device) if device is not None else f.repeat(axes)
 
 
-def _rotate(xs, freqs, pos, axes, interleaved, scale, start, inverse, inplace=False):
+def _rotary_args(xs, freqs, pos, axes, interleaved, scale, start):
+    """A call's arguments, checked: sizes and strides of the tensors, and the rest but for pointers and the direction."""
     x = xs[0]
     shapes = [_tokens(t, n, x) for t, n in zip(xs, ("x", "k"))]
     B, N, _, d = shapes[0][:4]
@@ -129,46 +130,51 @@ def _rotate(xs, freqs, pos, axes, interleaved, scale, start, inverse, inplace=Fa
         raise TypeError("freqs must be a tensor")
     if freqs.dtype is not torch.float64 or freqs.device != x.device or freqs.dim() != 1 or not freqs.is_contiguous():
         raise ValueError(f"freqs must be a contiguous torch.float64 vector on {x.device}")
-    at, pos_batch = None, 0
+    pos_batch = 0
     if pos is not None:
         if start != 0:
             raise ValueError("start goes with positions that are counted, not with given ones")
-        at = _int32(pos, "pos", x, *(((N,), (B, N)) if axes == 1 else ((N, 2), (B, N, 2))))
+        _int32(pos, "pos", x, *(((N,), (B, N)) if axes == 1 else ((N, 2), (B, N, 2))))
         pos_batch = N * axes if pos.dim() > axes else 0
     elif axes == 2 and x.dim() != 5:
         raise ValueError("two axes need a map or given positions")
-    if inplace:
-        # (a broadcast axis has all its entries in one place)
-        if any(n > 1 and s == 0 for t in xs for n, s in zip(t.shape, t.stride())):
-            raise ValueError("a broadcast tensor cannot be turned in place")
-        ys = xs
-    else:
-        ys = [_new(t) for t in xs]
+    return shapes, (B, N, d, 2 * freqs.numel(), axes, x.shape[2] if x.dim() == 5 else 0, interleaved), code, \
+        (pos_batch, start, scale)
+
+
+def _turn(xs, ys, freqs, pos, args, inverse, x_dense=False, y_dense=True):
+    """The launch. ``x_dense``, ``y_dense``: xs or ys are contiguous, whatever strides the checked tensors had."""
+    shapes, sizes, code, rest = args
+    B, N, d = sizes[:3]
     if B == 0 or N == 0 or d == 0:
-        return ys
+        return
     table = (RotaryTensor * len(xs))()
-    for e, t, y, (_, _, heads, _, b, n, h) in zip(table, xs, ys, shapes):
-        row = heads * d
-        e.__init__(t.data_ptr(), y.data_ptr(), heads, b, n, h, *((b, n, h) if inplace else (N * row, row, d)))
-    _call("qta_rotary", x, ctypes.addressof(table), len(xs), B, N, d, 2 * freqs.numel(), axes,
-          x.shape[2] if x.dim() == 5 else 0, interleaved, inverse, code, freqs.data_ptr(), at, pos_batch, start, scale)
-    if inplace:
-        torch.autograd.graph.increment_version(xs)      # (for what autograd may have kept of them)
-    return ys
+    for e, t, y, (_, _, heads, _, *st) in zip(table, xs, ys, shapes):
+        dense = (N * heads * d, heads * d, d)
+        e.__init__(t.data_ptr(), y.data_ptr(), heads, *(dense if x_dense else st), *(dense if y_dense else st))
+    _call("qta_rotary", xs[0], ctypes.addressof(table), len(xs), *sizes, inverse, code, freqs.data_ptr(),
+          None if pos is None else pos.data_ptr(), *rest)
 
 
 class _Rotary(torch.autograd.Function):
     @staticmethod
     def forward(ctx, freqs, pos, how, *xs):
-        ctx.how = how
-        ctx.save_for_backward(freqs, *([] if pos is None else [pos]))
-        return tuple(_rotate(xs, freqs, pos, *how, False))
+        ctx.args = _rotary_args(xs, freqs, pos, *how)
+        ctx.save_for_backward(freqs, pos)
+        ys = tuple(_new(t) for t in xs)
+        _turn(xs, ys, freqs, pos, ctx.args, False)
+        return ys
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, *dys):
-        freqs, pos = (*ctx.saved_tensors, None)[:2]
-        return (None, None, None, *_rotate([dy.contiguous() for dy in dys], freqs, pos, *ctx.how, True))
+        # autograd's thread runs Python two to three times slower than the caller's: no checks here, the engine has
+        # brought the gradients to the shapes, type and device of the outputs
+        freqs, pos = ctx.saved_tensors
+        dys = [dy.contiguous() for dy in dys]
+        dxs = [torch.empty_like(dy) for dy in dys]
+        _turn(dys, dxs, freqs, pos, ctx.args, True, x_dense=True)
+        return (None, None, None, *dxs)
 
 
 def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.0, start=0, inverse=False, inplace=False):
@@ -190,7 +196,14 @@ def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.
             raise ValueError("inverse is for tensors that do not require gradients")
         ys = _Rotary.apply(freqs, pos, how, *xs)
     else:
-        ys = _rotate(xs, freqs, pos, *how, bool(inverse), bool(inplace))
+        args = _rotary_args(xs, freqs, pos, *how)
+        # (a broadcast axis has all its entries in one place)
+        if inplace and any(n > 1 and s == 0 for t in xs for n, s in zip(t.shape, t.stride())):
+            raise ValueError("a broadcast tensor cannot be turned in place")
+        ys = xs if inplace else [_new(t) for t in xs]
+        _turn(xs, ys, freqs, pos, args, bool(inverse), y_dense=not inplace)
+        if inplace:
+            torch.autograd.graph.increment_version(xs)      # (for what autograd may have kept of them)
     return ys[0] if k is None else (ys[0], ys[1])
 
 

@@ -373,6 +373,35 @@ def test_rotary_gradient(dev, dtype):
     within("ones", g, R.rotary(torch.ones_like(x), freqs, p, scale=0.7, inverse=True))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_of_views_with_moved_saved_tensors(dev, dtype):
+    """Inputs and upstream gradients of any strides, and what is kept for the backward pass brought back at new addresses."""
+    r = gen(31, dev)
+    x = r(2, 3, 3, 4, 32).to(DT[dtype]).permute(0, 2, 3, 1, 4).requires_grad_()            # a map, heads before tokens
+    k = r(1, 3, 4, 2, 32).to(DT[dtype]).expand(2, 3, 4, 2, 32).requires_grad_()            # a broadcast axis
+    v, lam = r(2, 3, 4, 1, 64).to(DT[dtype]).requires_grad_(), r(1).requires_grad_()
+    q = r(2, 3, 4, 2, 32).to(DT[dtype]).requires_grad_()
+    freqs = P.rotary_freqs(32, axes=2, device=dev)
+    dy = r(2, 4, 3, 3, 32).to(DT[dtype]).transpose(1, 2)
+    dz = r(2, 3, 4, 1, 32).to(DT[dtype]).expand(2, 3, 4, 2, 32)
+    dout = r(2, 4, 3, 1, 64).to(DT[dtype]).transpose(1, 2)
+    grads = []
+    for moved in (False, True):
+        copy = (lambda t: t.clone()) if moved else (lambda t: t)
+        with torch.autograd.graph.saved_tensors_hooks(copy, copy):
+            y, z = P.rotary(x, freqs, k=k)
+            out = P.diff_attention(q, k, v, lam)
+        for _ in range(2):
+            grads.append(torch.autograd.grad((y, z), (x, k), (dy, dz), retain_graph=True)
+                         + torch.autograd.grad(out, (q, k, v, lam), dout, retain_graph=True))
+    i = torch.arange(12, device=dev)
+    p = torch.stack((i // 4, i % 4), -1)[None]
+    for g, d_ in zip(grads[0], (dy, dz)):
+        within("gradient", g.flatten(1, 2), R.rotary(d_.flatten(1, 2), freqs, p, inverse=True))
+    for other in grads[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(grads[0], other))
+
+
 # ---- together, as they are used ----
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
