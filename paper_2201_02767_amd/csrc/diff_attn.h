@@ -11,6 +11,8 @@
 #ifndef QTA_DIFF_ATTN_H
 #define QTA_DIFF_ATTN_H
 
+#include <algorithm>
+
 #include "bf16_tiles.h"
 #include "qta_internal.h"
 
@@ -326,24 +328,29 @@ constexpr int kDiffKeys = 128;  // keys of a workgroup of the key pass
 // Parts of the key pass's rows. One key head's keys in tiles of 128 may be few workgroups, and under a causal mask the
 // first tile meets all rows and the last only its own; parts cost a write and a read of fp32 sums. Two workgroups run on a
 // unit: as many parts as fill the units twice where work is even and four times where it is causal, no part below
-// 4 tiles of 32 rows, at most 8. (2 x 4096 keys, 16 heads over 4, d = 64, bf16, causal: in 2 parts 472 us
-// and 14 to join them, in 4 parts 357 and 23, in 6 parts 354 and 33.)
+// 4 tiles of 32 rows. (2 x 4096 keys, 16 heads over 4, d = 64, bf16, causal: in 2 parts 472 us and 14 to join them, in 4
+// parts 357 and 23, in 6 parts 354 and 33.) Past eight parts the sums weigh more: half as many workgroups and no part below
+// 8 tiles. (A training step, bf16, d = 64, 8 heads over 1: 7591 queries of 232 keys 579 us in 8 parts, 175 in 128 and 184 in
+// 64; 2048 causal tokens 240 in 8, 178 in 32, 186 in 64.)
+constexpr int kDiffEvenParts = 8;
 inline int diff_key_splits(int B, int kv_heads, int Nk, int R, bool causal)
 {
     const long long groups = static_cast<long long>(B) * kv_heads * ((Nk + kDiffKeys - 1) / kDiffKeys);
     const long long want = static_cast<long long>(device_cu_count()) * (causal ? 4 : 2);
-    const long long most = R / 128;
-    const long long s = (want + groups - 1) / groups;
-    return static_cast<int>(s < 1 || most < 1 ? 1 : (s > most ? most : s) > 8 ? 8 : (s > most ? most : s));
+    long long s = std::min<long long>((want + groups - 1) / groups, R / 128);
+    if (s > kDiffEvenParts)
+        s = std::max<long long>(kDiffEvenParts, std::min<long long>((want / 2 + groups - 1) / groups, R / 256));
+    return static_cast<int>(std::max(s, 1LL));
 }
 
-// Parts of the query pass's keys: enough to give every unit a workgroup, none below 256 keys, at most 16 (2 x 997 causal
-// tokens, 8 heads, d = 32, fp32: 103 us whole, 53 in two parts, 60 in three).
+// Parts of the query pass's keys: enough to give every unit a workgroup, none below 256 keys, at most 64 (2 x 997 causal
+// tokens, 8 heads, d = 32, fp32: 103 us whole, 53 in two parts, 60 in three; a training step of 100 queries, 4 heads over 1,
+// and 16000 keys, d = 32, fp32: 243 us with at most 16 parts, 177 with 62).
 inline int diff_query_splits(int B, int kv_heads, int Nk, int R)
 {
-    const long long groups = static_cast<long long>(B) * kv_heads * ((R + 127) / 128), most = Nk / 256;
-    const long long s = (device_cu_count() + groups - 1) / groups;
-    return static_cast<int>(s < 1 || most < 1 ? 1 : (s > most ? most : s) > 16 ? 16 : (s > most ? most : s));
+    const long long groups = static_cast<long long>(B) * kv_heads * ((R + 127) / 128);
+    const long long s = std::min<long long>((device_cu_count() + groups - 1) / groups, Nk / 256);
+    return static_cast<int>(std::clamp(s, 1LL, 64LL));
 }
 
 hipError_t launch_diff_attn(const DiffArgs& a, int d, bool use_bf16, hipStream_t stream);

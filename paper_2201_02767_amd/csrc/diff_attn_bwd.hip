@@ -471,17 +471,31 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
     }
 }
 
-// The parts' sums, in their order: four channels of one key row a thread.
-template <typename T, int D>
+// The parts' sums, in their order: four channels of one key by SLICES threads, each adding a run of the parts.
+template <typename T, int D, int SLICES>
 __global__ __launch_bounds__(kThreads) void diff_dkv_join_kernel(DiffBwdArgs a)
 {
-    const long long item = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
+    constexpr int ITEMS = kThreads / SLICES;
+    __shared__ f32x4 sums[SLICES == 1 ? 1 : kThreads];
+    const int in = threadIdx.x % ITEMS, slice = threadIdx.x / ITEMS;
+    const long long item = static_cast<long long>(blockIdx.x) * ITEMS + in;
     const long long total = static_cast<long long>(a.f.B) * a.f.Nk * a.f.kv_heads * D;
-    if (item >= total) return;
-    const f32x4* p = reinterpret_cast<const f32x4*>(a.part) + item;
-    f32x4 x = *p;
+    const int first = a.splits * slice / SLICES, end = a.splits * (slice + 1) / SLICES;     // (never empty)
+    f32x4 x{};
+    if (item < total) {
+        const f32x4* const p = reinterpret_cast<const f32x4*>(a.part) + item;
+        x = p[first * total];
 #pragma unroll 4
-    for (int s = 1; s < a.splits; ++s) x += p[s * total];
+        for (int s = first + 1; s < end; ++s) x += p[s * total];
+    }
+    if constexpr (SLICES > 1) {
+        sums[threadIdx.x] = x;
+        __syncthreads();
+        if (slice != 0) return;
+#pragma unroll
+        for (int s = 1; s < SLICES; ++s) x += sums[s * ITEMS + in];
+    }
+    if (item >= total) return;
     const long long row = item / D;
     const int c = 4 * static_cast<int>(item - row * D);
     if (c < 2 * D) store4<T>(a.dk, row * (2 * D) + c, x[0] * a.grad_scale, x[1] * a.grad_scale, x[2] * a.grad_scale, x[3] * a.grad_scale);
@@ -514,8 +528,10 @@ hipError_t launch_bwd(const DiffBwdArgs& args, hipStream_t stream)
                        2 * (32 * 4 * D * ES + 1024) + kDiffKeys * 2 * D * ES, stream, a);
     if (a.splits > 1) {
         const long long items = static_cast<long long>(a.f.B) * a.f.Nk * a.f.kv_heads * D;
-        hipLaunchKernelGGL((diff_dkv_join_kernel<T, D>), dim3(static_cast<unsigned>((items + kThreads - 1) / kThreads)),
-                           dim3(kThreads), 0, stream, a);
+        const int slices = a.splits > kDiffEvenParts ? 8 : 1;           // many parts are of few keys
+        const dim3 grid(static_cast<unsigned>((items * slices + kThreads - 1) / kThreads));
+        if (slices > 1) hipLaunchKernelGGL((diff_dkv_join_kernel<T, D, 8>), grid, dim3(kThreads), 0, stream, a);
+        else hipLaunchKernelGGL((diff_dkv_join_kernel<T, D, 1>), grid, dim3(kThreads), 0, stream, a);
     }
     return hipGetLastError();
 }

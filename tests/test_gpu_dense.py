@@ -254,6 +254,16 @@ def test_diff_attn_parts_of_ragged_caches(dev, dtype):
     check(dev, *make(dev, 5, 1, 3000, 64, 1, 32, dtype, seed=53), lens=lens)            # 64 rows of one key head
 
 
+@pytest.mark.parametrize("d", [32, 64])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_diff_attn_many_parts(dev, d, dtype):
+    """Many rows over few keys and few rows over many: both gradient passes in tens of parts, some without a key to see."""
+    check(dev, *make(dev, 2, 700, 130, 8, 1, d, dtype, seed=61), lens=[130, 3])
+    check(dev, *make(dev, 1, 700, 1100, 8, 1, d, dtype, seed=62), causal=True, lens=[1001], q_pos=[-90])
+    check(dev, *make(dev, 1, 3, 6000, 2, 1, d, dtype, seed=63, token_lam=True))
+    check(dev, *make(dev, 2, 3, 6000, 2, 1, d, dtype, seed=64), lens=[6000, 900], causal=True)
+
+
 def test_diff_attn_rows_past_32_bits(dev):
     """An output of more than 2^31 elements: its last rows are those of a call on these rows alone."""
     N, heads, d = 270000, 64, 64
