@@ -254,17 +254,7 @@ def _workspace(name, args, like):
     return (torch.empty(n, dtype=torch.uint8, device=like.device), n) if n > 256 else (None, 0)
 
 
-def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, keep=False):
-    """Differential attention, ``softmax(scale q0 k0^T) v - lam softmax(scale q1 k1^T) v`` for every head, the maps of
-    head i being q's heads 2i and 2i + 1. q ``[B, Nq, 2*heads, d]``, k ``[B, Nk, 2*kv_heads, d]``, v
-    ``[B, Nk, kv_heads, 2*d]`` (or maps ``[B, H, W, ..]``), d 32 or 64, heads a multiple of kv_heads; ``lam`` ``[heads]``
-    or one for every token ``[B, Nq, heads]``, fp32 or q's type. Returns ``[B, Nq, heads, 2*d]``.
-
-    ``lens`` (int32 ``[B]``): keys of each batch element; what lies behind them is never used, so k and v may be the
-    whole of a cache. ``causal``: query i sees the keys up to position ``q_pos[b] + i`` (int32 ``[B]``; None: the
-    queries are the last Nq of Nk tokens). A row that sees no key gives 0. ``scale``: None for 1/sqrt(d).
-    ``keep``: also return what ``diff_attn_backward`` needs."""
-    args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
+def _diff_forward(args, shape, q, keep):
     out = torch.empty(shape, dtype=q.dtype, device=q.device)
     maps = lse = None
     if keep:
@@ -279,6 +269,31 @@ def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, 
         ws, nbytes = _workspace("qta_diff_attn_workspace_bytes", args, q)
         _call("qta_diff_attn", q, ctypes.byref(args), out.data_ptr(), maps.data_ptr() if keep else None,
               lse.data_ptr() if keep else None, None if ws is None else ws.data_ptr(), nbytes)
+    return out, maps, lse
+
+
+def _diff_backward(args, q, k, v, lam, maps, lse, dout):
+    grads = [_new(t) for t in (q, k, v, lam)]
+    if args.Nk == 0 or dout.numel() == 0:
+        return tuple(g.zero_() for g in grads)
+    ws, nbytes = _workspace("qta_diff_attn_backward_workspace_bytes", args, q)
+    _call("qta_diff_attn_backward", q, ctypes.byref(args), maps.data_ptr(), lse.data_ptr(), dout.data_ptr(),
+          *[g.data_ptr() for g in grads], lam.dim() == 1, ws.data_ptr(), nbytes)
+    return tuple(grads)
+
+
+def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, keep=False):
+    """Differential attention, ``softmax(scale q0 k0^T) v - lam softmax(scale q1 k1^T) v`` for every head, the maps of
+    head i being q's heads 2i and 2i + 1. q ``[B, Nq, 2*heads, d]``, k ``[B, Nk, 2*kv_heads, d]``, v
+    ``[B, Nk, kv_heads, 2*d]`` (or maps ``[B, H, W, ..]``), d 32 or 64, heads a multiple of kv_heads; ``lam`` ``[heads]``
+    or one for every token ``[B, Nq, heads]``, fp32 or q's type. Returns ``[B, Nq, heads, 2*d]``.
+
+    ``lens`` (int32 ``[B]``): keys of each batch element; what lies behind them is never used, so k and v may be the
+    whole of a cache. ``causal``: query i sees the keys up to position ``q_pos[b] + i`` (int32 ``[B]``; None: the
+    queries are the last Nq of Nk tokens). A row that sees no key gives 0. ``scale``: None for 1/sqrt(d).
+    ``keep``: also return what ``diff_attn_backward`` needs."""
+    args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
+    out, maps, lse = _diff_forward(args, shape, q, keep)
     return (out, (maps, lse)) if keep else out
 
 
@@ -291,20 +306,15 @@ def diff_attn_backward(q, k, v, lam, kept, dout, *, scale=None, causal=False, le
                            (lse, "kept", torch.float32, (args.B, args.heads, 2, args.Nq)), (dout, "dout", q.dtype, shape)):
         if t.dtype is not dtype or t.device != q.device or t.shape != s or not t.is_contiguous():
             raise ValueError(f"{n} must be contiguous {dtype} {tuple(s)} on {q.device}")
-    grads = [_new(t) for t in (q, k, v, lam)]
-    if args.Nk == 0 or dout.numel() == 0:
-        return tuple(g.zero_() for g in grads)
-    ws, nbytes = _workspace("qta_diff_attn_backward_workspace_bytes", args, q)
-    _call("qta_diff_attn_backward", q, ctypes.byref(args), maps.data_ptr(), lse.data_ptr(), dout.data_ptr(),
-          *[g.data_ptr() for g in grads], lam.dim() == 1, ws.data_ptr(), nbytes)
-    return tuple(grads)
+    return _diff_backward(args, q, k, v, lam, maps, lse, dout)
 
 
 class _DiffAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, lam, scale, causal, lens, q_pos):
-        out, (maps, lse) = diff_attn(q, k, v, lam, scale=scale, causal=causal, lens=lens, q_pos=q_pos, keep=True)
-        ctx.how = (scale, causal)
+        ctx.args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
+        out, maps, lse = _diff_forward(ctx.args, shape, q, True)
+        ctx.strides, ctx.how = (q.stride(), k.stride(), v.stride(), lam.stride()), (scale, causal)
         ctx.save_for_backward(q, k, v, lam, maps, lse, lens, q_pos)
         return out
 
@@ -315,8 +325,15 @@ class _DiffAttention(torch.autograd.Function):
         dout = dout.contiguous()
         if dout.data_ptr() % 16:
             dout = dout.clone()
-        return (*diff_attn_backward(q, k, v, lam, (maps, lse), dout, scale=ctx.how[0], causal=ctx.how[1], lens=lens,
-                                    q_pos=q_pos), None, None, None, None)
+        # the forward's checks hold as long as what was kept came back as it was laid out, at whatever address
+        if (q.stride(), k.stride(), v.stride(), lam.stride()) == ctx.strides:
+            args = DiffAttnArgs.from_buffer_copy(ctx.args)
+            args.q, args.k, args.v, args.lam = q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr()
+            args.lens = None if lens is None else lens.data_ptr()
+            args.q_pos = None if q_pos is None else q_pos.data_ptr()
+        else:
+            args, _ = _diff_args(q, k, v, lam, *ctx.how, lens, q_pos)
+        return (*_diff_backward(args, q, k, v, lam, maps, lse, dout), None, None, None, None)
 
 
 def diff_attention(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None):

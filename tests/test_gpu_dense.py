@@ -400,10 +400,11 @@ def test_gradients_of_views_with_moved_saved_tensors(dev, dtype):
         copy = (lambda t: t.clone()) if moved else (lambda t: t)
         with torch.autograd.graph.saved_tensors_hooks(copy, copy):
             y, z = P.rotary(x, freqs, k=k)
-            out = P.diff_attention(q, k, v, lam)
+            out, dense = P.diff_attention(q, k, v, lam), P.diff_attention(q, k.contiguous(), v, lam)
         for _ in range(2):
             grads.append(torch.autograd.grad((y, z), (x, k), (dy, dz), retain_graph=True)
-                         + torch.autograd.grad(out, (q, k, v, lam), dout, retain_graph=True))
+                         + torch.autograd.grad(out, (q, k, v, lam), dout, retain_graph=True)
+                         + torch.autograd.grad(dense, (q, k, v, lam), dout, retain_graph=True))
     i = torch.arange(12, device=dev)
     p = torch.stack((i // 4, i % 4), -1)[None]
     for g, d_ in zip(grads[0], (dy, dz)):
