@@ -122,6 +122,20 @@ BwdLayout bwd_layout(const qta_diff_attn_args* a, bool lam_heads)
     return L;
 }
 
+// Whether every launch of a call is one that HIP takes.
+bool fwd_fits(const qta_diff_attn_args* a, const FwdLayout& L)
+{
+    const long long groups = static_cast<long long>(a->B) * a->kv_heads, R = static_cast<long long>(a->Nq) * (a->heads / a->kv_heads);
+    return diff_fwd_blocks(groups, R, L.parts) <= kDiffMaxBlocks && (L.parts.splits == 1 || diff_join_blocks(groups, R) <= kDiffMaxBlocks);
+}
+bool bwd_fits(const qta_diff_attn_args* a, const BwdLayout& L)
+{
+    const long long groups = static_cast<long long>(a->B) * a->kv_heads, R = static_cast<long long>(a->Nq) * (a->heads / a->kv_heads);
+    return diff_dq_blocks(groups, R, L.q_splits) <= kDiffMaxBlocks && diff_dkv_blocks(groups, a->Nk, L.splits) + a->heads <= kDiffMaxBlocks &&
+           (L.q_splits == 1 || diff_dq_join_blocks(groups, R, a->d) <= kDiffMaxBlocks) &&
+           (L.splits == 1 || diff_dkv_join_blocks(groups, a->Nk, a->d, L.splits) <= kDiffMaxBlocks);
+}
+
 }  // namespace
 
 extern "C" {
@@ -129,8 +143,9 @@ extern "C" {
 size_t qta_diff_attn_workspace_bytes(const qta_diff_attn_args* args)
 {
     if (check_diff(args, true) != QTA_OK) return 0;
-    const size_t n = fwd_layout(args).total;
-    return n < kAlign ? kAlign : n;
+    const FwdLayout L = fwd_layout(args);
+    if (!fwd_fits(args, L)) return 0;
+    return L.total < kAlign ? kAlign : L.total;
 }
 
 qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, float* maps, float* lse, void* workspace,
@@ -140,6 +155,7 @@ qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, float* maps,
     if (st != QTA_OK) return st;
     if (!out || !aligned(out, 16) || (maps != nullptr) != (lse != nullptr) || !aligned(maps, 16) || !aligned(lse, 4)) return QTA_ERR_INVALID;
     const FwdLayout L = fwd_layout(args);
+    if (!fwd_fits(args, L)) return QTA_ERR_UNSUPPORTED;
     if (L.total > 0) {
         if (workspace_bytes < L.total) return QTA_ERR_WORKSPACE;
         if (!workspace || !aligned(workspace, kAlign)) return QTA_ERR_INVALID;
@@ -157,7 +173,9 @@ qta_status qta_diff_attn(const qta_diff_attn_args* args, void* out, float* maps,
 
 size_t qta_diff_attn_backward_workspace_bytes(const qta_diff_attn_args* args)
 {
-    return check_diff(args, true) == QTA_OK ? bwd_layout(args, true).total : 0;
+    if (check_diff(args, true) != QTA_OK) return 0;
+    const BwdLayout L = bwd_layout(args, true);
+    return bwd_fits(args, L) ? L.total : 0;
 }
 
 qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const float* maps, const float* lse, const void* dout,
@@ -170,6 +188,7 @@ qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const float* m
         if (!p || !aligned(p, 16)) return QTA_ERR_INVALID;
     if (!lse || !dlam || !workspace || !aligned(workspace, 256)) return QTA_ERR_INVALID;
     const BwdLayout L = bwd_layout(args, dlam_heads != 0);
+    if (!bwd_fits(args, L)) return QTA_ERR_UNSUPPORTED;
     if (workspace_bytes < L.total) return QTA_ERR_WORKSPACE;
     DiffBwdArgs a{};
     a.f = make_args(args);

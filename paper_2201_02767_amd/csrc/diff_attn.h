@@ -353,6 +353,31 @@ inline int diff_query_splits(int B, int kv_heads, int Nk, int R)
     return static_cast<int>(std::clamp(s, 1LL, 64LL));
 }
 
+// Workgroups of the launches, as the launchers make them and the entry points check them beforehand: HIP takes fewer than
+// 2^32 threads a launch, which is 2^24 workgroups.
+constexpr int kDiffThreads = 256;
+constexpr long long kDiffMaxBlocks = (1LL << 32) / kDiffThreads - 1;
+inline long long diff_fwd_blocks(long long groups, long long R, const DiffParts& p)
+{
+    const int rows = p.keys_apart ? 32 : 64;
+    return (R + rows - 1) / rows * groups * p.splits;
+}
+inline long long diff_join_blocks(long long groups, long long R)       // a wave a row
+{
+    return (groups * R + kDiffThreads / kWave - 1) / (kDiffThreads / kWave);
+}
+inline long long diff_dq_blocks(long long groups, long long R, int q_splits) { return (R + 127) / 128 * groups * q_splits; }
+inline long long diff_dq_join_blocks(long long groups, long long R, int d)
+{
+    return (groups * R * (d / 2) + kDiffThreads - 1) / kDiffThreads;
+}
+inline long long diff_dkv_blocks(long long groups, long long Nk, int splits) { return (Nk + kDiffKeys - 1) / kDiffKeys * groups * splits; }
+inline int diff_dkv_slices(int splits) { return splits > kDiffEvenParts ? 8 : 1; }             // many parts are of few keys
+inline long long diff_dkv_join_blocks(long long groups, long long Nk, int d, int splits)
+{
+    return (groups * Nk * d * diff_dkv_slices(splits) + kDiffThreads - 1) / kDiffThreads;
+}
+
 hipError_t launch_diff_attn(const DiffArgs& a, int d, bool use_bf16, hipStream_t stream);
 hipError_t launch_diff_bwd(const DiffBwdArgs& a, int d, bool use_bf16, hipStream_t stream);
 

@@ -19,7 +19,7 @@ namespace {
 
 using namespace diff;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kDiffThreads;
 
 // Maxima lag: a row's running maximum is raised only when a tile exceeds it by 2^8 or more, so that most tiles rescale
 // nothing. Weights then go up to 2^8, which costs neither fp32 sums nor bf16 weights any of their bits.
@@ -284,7 +284,6 @@ template <typename T, int D, int BN, bool KEYS>
 hipError_t launch_fwd(const DiffArgs& a, hipStream_t stream)
 {
     static std::atomic<unsigned long long> configured{0};
-    constexpr int BM = KEYS ? 32 : 64;
     constexpr int stage = BN * 4 * D * static_cast<int>(sizeof(T));
     constexpr int boxes = 2 * (2 * D / 32 * 16 + 2) * 64 * 4;
     constexpr int lds = 2 * stage > boxes ? 2 * stage : boxes;
@@ -292,12 +291,11 @@ hipError_t launch_fwd(const DiffArgs& a, hipStream_t stream)
     const hipError_t e = set_max_lds_once(fn, configured);
     if (e != hipSuccess) return e;
     const long long groups = static_cast<long long>(a.B) * a.kv_heads;
-    const long long blocks = (a.R + BM - 1) / BM * groups * a.splits;
-    const long long join = (groups * a.R + kThreads / kWave - 1) / (kThreads / kWave);
-    if (blocks > 0x7FFFFFFFLL || join > 0x7FFFFFFFLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((diff_fwd_kernel<T, D, BN, KEYS>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), lds, stream, a);
+    const dim3 grid(static_cast<unsigned>(diff_fwd_blocks(groups, a.R, {KEYS, a.splits})));
+    hipLaunchKernelGGL((diff_fwd_kernel<T, D, BN, KEYS>), grid, dim3(kThreads), lds, stream, a);
     if (a.splits > 1)
-        hipLaunchKernelGGL((diff_join_kernel<T, D>), dim3(static_cast<unsigned>(join)), dim3(kThreads), 0, stream, a);
+        hipLaunchKernelGGL((diff_join_kernel<T, D>), dim3(static_cast<unsigned>(diff_join_blocks(groups, a.R))), dim3(kThreads), 0,
+                           stream, a);
     return hipGetLastError();
 }
 

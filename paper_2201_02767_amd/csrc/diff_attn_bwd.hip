@@ -22,7 +22,7 @@ namespace {
 
 using namespace diff;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kDiffThreads;
 
 __device__ __forceinline__ void store_dlambda(const DiffBwdArgs& a, int b, int i, int h, float x)
 {
@@ -509,9 +509,8 @@ hipError_t launch_bwd(const DiffBwdArgs& args, hipStream_t stream)
     constexpr int ES = static_cast<int>(sizeof(T)), BN = 32;
     DiffBwdArgs a = args;
     const long long bh = static_cast<long long>(a.f.B) * a.f.kv_heads;
-    const long long qblocks = (a.f.R + 127) / 128 * bh * a.q_splits;
-    const long long kblocks = (a.f.Nk + kDiffKeys - 1) / kDiffKeys * bh * a.splits, heads = a.lam_heads ? a.f.heads : 0;
-    if (qblocks > 0x7FFFFFFFLL || kblocks + heads > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    const long long qblocks = diff_dq_blocks(bh, a.f.R, a.q_splits), kblocks = diff_dkv_blocks(bh, a.f.Nk, a.splits);
+    const long long heads = a.lam_heads ? a.f.heads : 0;
     a.key_groups = static_cast<int>(kblocks);
     hipError_t e = set_max_lds_once(reinterpret_cast<const void*>(&diff_dq_kernel<T, D, BN>), configured_q);
     if (e != hipSuccess) return e;
@@ -519,18 +518,14 @@ hipError_t launch_bwd(const DiffBwdArgs& args, hipStream_t stream)
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((diff_dq_kernel<T, D, BN>), dim3(static_cast<unsigned>(qblocks)), dim3(kThreads), 2 * BN * 4 * D * ES,
                        stream, a);
-    if (a.q_splits > 1) {
-        const long long items = bh * a.f.R * (D / 2);
-        hipLaunchKernelGGL((diff_dq_join_kernel<T, D>), dim3(static_cast<unsigned>((items + kThreads - 1) / kThreads)),
+    if (a.q_splits > 1)
+        hipLaunchKernelGGL((diff_dq_join_kernel<T, D>), dim3(static_cast<unsigned>(diff_dq_join_blocks(bh, a.f.R, D))),
                            dim3(kThreads), 0, stream, a);
-    }
     hipLaunchKernelGGL((diff_dkv_kernel<T, D>), dim3(static_cast<unsigned>(kblocks + heads)), dim3(kThreads),
                        2 * (32 * 4 * D * ES + 1024) + kDiffKeys * 2 * D * ES, stream, a);
     if (a.splits > 1) {
-        const long long items = static_cast<long long>(a.f.B) * a.f.Nk * a.f.kv_heads * D;
-        const int slices = a.splits > kDiffEvenParts ? 8 : 1;           // many parts are of few keys
-        const dim3 grid(static_cast<unsigned>((items * slices + kThreads - 1) / kThreads));
-        if (slices > 1) hipLaunchKernelGGL((diff_dkv_join_kernel<T, D, 8>), grid, dim3(kThreads), 0, stream, a);
+        const dim3 grid(static_cast<unsigned>(diff_dkv_join_blocks(bh, a.f.Nk, D, a.splits)));
+        if (diff_dkv_slices(a.splits) > 1) hipLaunchKernelGGL((diff_dkv_join_kernel<T, D, 8>), grid, dim3(kThreads), 0, stream, a);
         else hipLaunchKernelGGL((diff_dkv_join_kernel<T, D, 1>), grid, dim3(kThreads), 0, stream, a);
     }
     return hipGetLastError();

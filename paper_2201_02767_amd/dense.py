@@ -278,7 +278,7 @@ def _diff_backward(args, q, k, v, lam, maps, lse, dout):
         return tuple(g.zero_() for g in grads)
     ws, nbytes = _workspace("qta_diff_attn_backward_workspace_bytes", args, q)
     _call("qta_diff_attn_backward", q, ctypes.byref(args), maps.data_ptr(), lse.data_ptr(), dout.data_ptr(),
-          *[g.data_ptr() for g in grads], lam.dim() == 1, ws.data_ptr(), nbytes)
+          *[g.data_ptr() for g in grads], lam.dim() == 1, None if ws is None else ws.data_ptr(), nbytes)
     return tuple(grads)
 
 
