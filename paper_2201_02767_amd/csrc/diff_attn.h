@@ -399,6 +399,7 @@ struct RotaryArgs {
     float scale;
     FastDiv div_N, div_W, div_pairs, div_items, div_heads;      // set by the launcher
     int items, tokens;          // items of a head, tokens of a workgroup; set by the launcher
+    long long first;            // token of the launch's first workgroup; set by the launcher
 };
 hipError_t launch_rotary(const RotaryArgs& a, bool use_bf16, hipStream_t stream);
 

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
     constexpr int U = INTER && V == 1 ? 2 : V;             // elements of a turned piece
     extern __shared__ __align__(16) float2 turn[];         // [tokens][rot / 2] (cos, sin) times m
     const int pairs = a.rot / 2, per = pairs / a.axes;     // pairs of all axes, of one
-    const long long first = static_cast<long long>(blockIdx.x) * a.tokens;
+    const long long first = a.first + static_cast<long long>(blockIdx.x) * a.tokens;
     const int tokens = static_cast<int>(min(static_cast<long long>(a.tokens), static_cast<long long>(a.B) * a.N - first));
     for (int i = threadIdx.x; i < tokens * pairs; i += kThreads) {
         const int t = fast_div(i, a.div_pairs), p = i - t * pairs;
@@ -150,8 +150,13 @@ hipError_t launch(const RotaryArgs& a, hipStream_t stream)
     p.div_items = make_fastdiv(p.items);
     p.div_heads = make_fastdiv(heads);
     const long long blocks = (tokens + p.tokens - 1) / p.tokens;
-    hipLaunchKernelGGL((rotary_kernel<T, V, INTER>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads),
-                       static_cast<size_t>(p.tokens) * pairs * sizeof(float2), stream, p);
+    // HIP takes fewer than 2^32 threads a launch
+    constexpr long long most = (1LL << 32) / kThreads - 1;
+    for (long long at = 0; at < blocks; at += most) {
+        p.first = at * p.tokens;
+        hipLaunchKernelGGL((rotary_kernel<T, V, INTER>), dim3(static_cast<unsigned>(std::min(most, blocks - at))), dim3(kThreads),
+                           static_cast<size_t>(p.tokens) * pairs * sizeof(float2), stream, p);
+    }
     return hipGetLastError();
 }
 

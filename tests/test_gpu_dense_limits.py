@@ -1,0 +1,24 @@
+"""Rotary positions and differential attention on the GPU at the border of what they take: the largest sizes, calls that are
+refused, and what lies in places that nothing may use. Values against tests/dense_ref.py, as in test_gpu_dense.py."""
+import pytest
+import torch
+
+import paper_2201_02767_amd as P
+from tests import dense_ref as R
+from tests.test_gpu_dense import announce, dev, gen, within  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def test_rotary_of_more_workgroups_than_a_launch_takes(dev):
+    """A token a workgroup, and more tokens than the 2^24 - 1 workgroups of 256 threads that one launch can have: around that
+    border, and at the end."""
+    N, d, rot = (1 << 24) + 300, 514, 4
+    announce(f"rotary {N} x {d}")
+    x = gen(71, dev)(1, 1, 1, d).bfloat16()
+    freqs = P.rotary_freqs(rot, device=dev)
+    y = P.rotary(x.expand(1, N, 1, d), freqs)
+    for at in (0, (1 << 24) - 50, N - 100):
+        p = torch.arange(at, at + 100, device=dev)[None, :, None]
+        within(f"tokens from {at} on", y[:, at:at + 100], R.rotary(x.expand(1, 100, 1, d), freqs, p))
+        assert torch.equal(y[:, at:at + 100, :, rot:], x[..., rot:].expand(1, 100, 1, d - rot))
