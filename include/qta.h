@@ -373,7 +373,7 @@ qta_status qta_finest_attn(const void* q0, const void* k0, const void* v0,
  *   interleaved within an axis of S channels pair j is (2j, 2j+1); 0: (j, j + S/2).
  *   freqs       device fp64 [rot/2], radians a position step, axis by axis. Angles are taken in fp64.
  *   pos         device int32 [B][N][axes], pos_batch elements between batch elements (0: the same for all); or NULL:
- *               start + n for axes = 1, and (n / width, n % width) for axes = 2, N a multiple of width.
+ *               start + n for axes = 1, and (n / width, n % width) for axes = 2, N a multiple of width and start 0.
  *   inverse     nonzero: angles negated. scale is kept, so this is the gradient: dx from dy with the same arguments.
  */
 #define QTA_MAX_ROTARY_D 4096

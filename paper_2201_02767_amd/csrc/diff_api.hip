@@ -219,7 +219,7 @@ qta_status qta_rotary(const qta_rotary_tensor* tensors, int count, int B, int N,
 {
     if (!tensors || count < 1 || count > 2 || !freqs || !aligned(freqs, 8) || !aligned(pos, 4) || !dtype_ok(dtype)) return QTA_ERR_INVALID;
     if (B <= 0 || N <= 0 || d <= 0 || rot <= 0 || rot > d || (axes != 1 && axes != 2) || rot % (2 * axes) != 0) return QTA_ERR_INVALID;
-    if (axes == 2 && !pos && (width <= 0 || N % width != 0)) return QTA_ERR_INVALID;
+    if (axes == 2 && !pos && (width <= 0 || N % width != 0 || start != 0)) return QTA_ERR_INVALID;
     if (pos_batch < 0) return QTA_ERR_INVALID;
     if (!pos && axes == 1 && (start > INT32_MAX - N || start < INT32_MIN + 1)) return QTA_ERR_INVALID;
     if (d > QTA_MAX_ROTARY_D || static_cast<int64_t>(B) * N > 0x7FFFFFFFLL) return QTA_ERR_UNSUPPORTED;

@@ -14,6 +14,8 @@ from torch._C import _cuda_getCurrentRawStream as _raw_stream      # (torch.cuda
 
 from .qta import _DTYPES, _SIGS, _check, _dtype_code, _scale, lib
 
+_INT_MAX = 2 ** 31 - 1
+
 _P, _I, _F, _L = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_int64
 
 
@@ -58,6 +60,8 @@ def _tokens(t, name, like=None):
         N, token = shape[1] * shape[2], st[2] if shape[2] > 1 else st[1]
         if shape[1] > 1 and shape[2] > 1 and st[1] != shape[2] * st[2]:
             raise ValueError(f"the rows of the map {name} must follow each other at one distance")
+    if t.numel() > _INT_MAX and max(shape[0], N, *shape[-2:]) > _INT_MAX:       # (ctypes would wrap them)
+        raise ValueError(f"{name} has shape {tuple(shape)}: sizes are below 2^31")
     # (the stride of an axis of one entry is never taken, and may be anything)
     return (shape[0], N, shape[-2], shape[-1], st[0] if shape[0] > 1 else 0, token if N > 1 else 0,
             st[-2] if shape[-2] > 1 else 0)
@@ -117,6 +121,8 @@ def rotary_freqs(rot, *, theta=10000.0, axes=1, factor=1.0, trained=None, low=1.
 def _rotary_args(xs, freqs, pos, axes, interleaved, scale, start):
     """A call's arguments, checked: sizes and strides of the tensors, and the rest but for pointers and the direction."""
     x = xs[0]
+    if not -_INT_MAX <= start <= _INT_MAX:              # (and start + N as well: the library's check)
+        raise ValueError(f"start must be below 2^31, got {start}")
     shapes = [_tokens(t, n, x) for t, n in zip(xs, ("x", "k"))]
     B, N, _, d = shapes[0][:4]
     for t, s in zip(xs[1:], shapes[1:]):
@@ -136,8 +142,11 @@ def _rotary_args(xs, freqs, pos, axes, interleaved, scale, start):
             raise ValueError("start goes with positions that are counted, not with given ones")
         _int32(pos, "pos", x, *(((N,), (B, N)) if axes == 1 else ((N, 2), (B, N, 2))))
         pos_batch = N * axes if pos.dim() > axes else 0
-    elif axes == 2 and x.dim() != 5:
-        raise ValueError("two axes need a map or given positions")
+    elif axes == 2:
+        if x.dim() != 5:
+            raise ValueError("two axes need a map or given positions")
+        if start != 0:
+            raise ValueError("start goes with the positions of a sequence, not with rows and columns")
     return shapes, (B, N, d, 2 * freqs.numel(), axes, x.shape[2] if x.dim() == 5 else 0, interleaved), code, \
         (pos_batch, start, scale)
 
@@ -184,7 +193,8 @@ def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.
 
     ``axes``: 1, or 2 for row and column positions, the first half of the turned channels going by the row and the rest by
     the column (the default for maps, ``[B, H, W, heads, d]``). ``pos``: int32 positions ``[N]`` or ``[B, N]``
-    (``[.., N, 2]`` for two axes, N = H*W on a map); None: ``start`` + 0, 1, .. along a sequence, the coordinates of a map.
+    (``[.., N, 2]`` for two axes, N = H*W on a map); None: ``start`` + 0, 1, .. (below 2^31) along the tokens for one axis, the coordinates of a map
+    for two.
     ``interleaved``: pairs are neighbouring channels instead of the two halves of an axis. ``inverse``: turn back.
     ``inplace``: overwrite x and k (and return them); not differentiable."""
     xs = (x,) if k is None else (x, k)

@@ -22,3 +22,14 @@ def test_rotary_of_more_workgroups_than_a_launch_takes(dev):
         p = torch.arange(at, at + 100, device=dev)[None, :, None]
         within(f"tokens from {at} on", y[:, at:at + 100], R.rotary(x.expand(1, 100, 1, d), freqs, p))
         assert torch.equal(y[:, at:at + 100, :, rot:], x[..., rot:].expand(1, 100, 1, d - rot))
+
+
+def test_rotary_positions_that_are_refused(dev):
+    x, f = torch.zeros(1, 3, 4, 2, 32, device=dev), P.rotary_freqs(32, axes=2, device=dev)
+    for start in (1, 2 ** 32 + 5):
+        with pytest.raises(ValueError, match="start"):
+            P.rotary(x, f, start=start)                     # rows and columns have no start
+    assert P.rotary(x, f, axes=1, start=5).shape == x.shape
+    wide = torch.zeros(1, 1, 1, 32, device=dev).expand(1, 2 ** 32 + 12, 1, 32)
+    with pytest.raises(ValueError, match="2\\^31"):
+        P.rotary(wide, P.rotary_freqs(32, device=dev))
