@@ -366,7 +366,8 @@ qta_status qta_finest_attn(const void* q0, const void* k0, const void* v0,
  *               contiguous, aligned to their type (16-byte aligned tensors whose strides are multiples of 16 bytes, with
  *               every half of an axis (half layout) or all turned channels (interleaved), and the rest, multiples of 16
  *               bytes, take 16-byte accesses, others single elements). y may be x itself (in place, same strides);
- *               otherwise they must not overlap. Strides of y must place no two elements together.
+ *               otherwise they must not overlap. Strides of y must place no two elements together, and of two tensors
+ *               neither's y may overlap the other's x or y (they may share x).
  *   rot, axes   the first rot <= d channels turn, the others are copied. axes = 1: by the token's position; axes = 2:
  *               the first rot/2 of them by its first position (row), the others by its second (column). rot is a multiple
  *               of 2 axes; d <= QTA_MAX_ROTARY_D.

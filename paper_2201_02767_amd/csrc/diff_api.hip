@@ -236,6 +236,8 @@ qta_status qta_rotary(const qta_rotary_tensor* tensors, int count, int B, int N,
         heads += t.heads;
     }
     if (heads > (1 << 16)) return QTA_ERR_UNSUPPORTED;
+    // what one tensor's threads write is neither written nor read by the other's (further overlaps are the caller's to avoid)
+    if (count == 2 && (tensors[0].y == tensors[1].y || tensors[0].y == tensors[1].x || tensors[0].x == tensors[1].y)) return QTA_ERR_INVALID;
     a.B = B;
     a.N = N;
     a.d = d;

@@ -165,6 +165,71 @@ def _turn(xs, ys, freqs, pos, args, inverse, x_dense=False, y_dense=True):
           None if pos is None else pos.data_ptr(), *rest)
 
 
+def _extent(axes, run):
+    """Elements from the first to behind the last of runs that lie at the axes (stride, entries), where no two runs meet as
+    each axis steps over all that is inside it; None where an axis does not."""
+    for stride, n in sorted(axes):
+        if stride < run:
+            return None
+        run += stride * (n - 1)
+    return run
+
+
+def _apart(xs, shapes):
+    """Whether no two heads of the tokens of one or two tensors (and their ``_tokens``) share an element. (In place each is
+    read and written by threads of its own.)"""
+    size, at = xs[0].element_size(), [t.data_ptr() for t in xs]
+    lo, hi = (0, 1) if at[0] <= at[-1] else (1, 0)
+    gap = (at[-1] - at[0]) * (hi - lo)
+    # tokens, and heads within them, one after the other: the usual layouts, quickly
+    spans = []
+    for B, N, heads, d, b, n, h in shapes:
+        token = (heads - 1) * h + d
+        row = (N - 1) * n + token
+        if (heads > 1 and h < d) or (N > 1 and n < token) or (B > 1 and b < row):
+            break
+        spans.append((token, (B - 1) * b + row))
+    else:
+        if len(xs) == 1 or gap >= spans[lo][1] * size:
+            return True
+        B, N, _, _, b, n, _ = shapes[0]
+        both = gap + spans[hi][0] * size                # a token of both, side by side
+        if (b, n) == shapes[1][4:6] and gap >= spans[lo][0] * size and (N == 1 or n * size >= both) \
+                and (B == 1 or b * size >= (N - 1) * n * size + both):
+            return True
+    if any(0 in s[:4] for s in shapes):                 # (no element, or a call that is refused)
+        return True
+    return _apart_anyhow(at, [[a for a in zip(s[4:], s[:3]) if a[1] > 1] for s in shapes], shapes[0][3], size)
+
+
+def _apart_anyhow(at, axes, d, size):
+    """The same from addresses, axes (stride, entries) and the length of a head, for strides of any order."""
+    if any(s == 0 for a in axes for s, _ in a):
+        return False
+    spans = [_extent(a, d) for a in axes]
+    if None not in spans:
+        if len(at) == 1:
+            return True
+        lo, hi = (0, 1) if at[0] <= at[1] else (1, 0)
+        gap = at[hi] - at[lo]
+        if gap >= spans[lo] * size:
+            return True
+        # side by side inside the axes on which both step alike
+        alike = sorted((a for a in axes[0] if a in axes[1]), reverse=True)
+        for n in range(1, len(alike) + 1):
+            inside = [_extent([a for a in x if a not in alike[:n]], d) for x in axes]
+            if gap >= inside[lo] * size and _extent(alike[:n], -(-gap // size) + inside[hi]) is not None:
+                return True
+    # every head's place
+    places = []
+    for p, x in zip(at, axes):
+        p = torch.full((1,), p, dtype=torch.int64)
+        for s, n in x:
+            p = (p[:, None] + torch.arange(n, dtype=torch.int64) * (s * size)).flatten()
+        places.append(p)
+    return bool((torch.cat(places).sort().values.diff() >= d * size).all())
+
+
 class _Rotary(torch.autograd.Function):
     @staticmethod
     def forward(ctx, freqs, pos, how, *xs):
@@ -196,7 +261,7 @@ def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.
     (``[.., N, 2]`` for two axes, N = H*W on a map); None: ``start`` + 0, 1, .. (below 2^31) along the tokens for one axis, the coordinates of a map
     for two.
     ``interleaved``: pairs are neighbouring channels instead of the two halves of an axis. ``inverse``: turn back.
-    ``inplace``: overwrite x and k (and return them); not differentiable."""
+    ``inplace``: overwrite x and k, which must not overlap, and return them; not differentiable."""
     xs = (x,) if k is None else (x, k)
     how = (axes, bool(interleaved), float(scale), int(start))
     if torch.is_grad_enabled() and (getattr(x, "requires_grad", False) or getattr(k, "requires_grad", False)):
@@ -207,9 +272,8 @@ def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.
         ys = _Rotary.apply(freqs, pos, how, *xs)
     else:
         args = _rotary_args(xs, freqs, pos, *how)
-        # (a broadcast axis has all its entries in one place)
-        if inplace and any(n > 1 and s == 0 for t in xs for n, s in zip(t.shape, t.stride())):
-            raise ValueError("a broadcast tensor cannot be turned in place")
+        if inplace and not _apart(xs, args[0]):
+            raise ValueError("in place, no two heads may share memory: a broadcast or overlapping tensor, or x and k that overlap")
         ys = xs if inplace else [_new(t) for t in xs]
         _turn(xs, ys, freqs, pos, args, bool(inverse), y_dense=not inplace)
         if inplace:

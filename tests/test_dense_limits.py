@@ -1,13 +1,15 @@
 """Sizes and arguments at the border of what rotary positions and differential attention take, on the host: what is past it
 is refused before anything reaches a device."""
 import ctypes
+import random
 
 import pytest
 import torch
 
 import paper_2201_02767_amd as P
 from paper_2201_02767_amd import dense
-from tests.test_dense_abi import INVALID, UNSUPPORTED, backward, diff_args, forward, rotary
+from paper_2201_02767_amd.dense import RotaryTensor
+from tests.test_dense_abi import FAKE, INVALID, UNSUPPORTED, backward, diff_args, forward, rotary
 
 BLOCKS = 1 << 24        # of 256 threads: 2^32 threads, the first count that HIP does not take
 
@@ -77,3 +79,65 @@ def test_sizes_past_32_bits(shape, monkeypatch):
     with pytest.raises(ValueError, match="2\\^31"):
         dense._tokens(Shaped(shape, (0,) * (len(shape) - 1) + (1,)), "x")
     assert dense._tokens(Shaped((3, 2 ** 30, 4, 32), (0, 0, 0, 1)), "x")[:4] == (3, 2 ** 30, 4, 32)
+
+
+# ---- in place: a head is read and written by threads of its own ----
+
+def brute_apart(xs):
+    """Every element's place, counted."""
+    seen = set()
+    for t in xs:
+        for e in torch.ones(t.shape).nonzero().tolist():
+            at = t.data_ptr() + t.element_size() * sum(i * s for i, s in zip(e, t.stride()))
+            if at in seen:
+                return False
+            seen.add(at)
+    return True
+
+
+def apart(xs, monkeypatch):
+    with monkeypatch.context() as m:
+        m.setattr(torch.Tensor, "is_cuda", True)
+        shapes = [dense._tokens(t, "x") for t in xs]
+    return dense._apart(xs, shapes)
+
+
+def test_overlaps_of_what_is_turned_in_place(monkeypatch):
+    fused = torch.zeros(2, 11, 7, 8)
+    heads_first = torch.zeros(2, 9, 5, 8).transpose(1, 2)
+    pairs = torch.zeros(2, 5, 3, 2, 8)
+    sound = [(fused,), (fused[:, :, :4], fused[:, :, 4:]), (fused[:, :, 5:], fused[:, :, :5]), (fused[:1], fused[1:]),
+             (fused[:, :6], fused[:, 5:][:, 1:]), (heads_first[:, :, :6], heads_first[:, :, 6:]),
+             (pairs[..., 0, :], pairs[..., 1, :]), (pairs[:, :, :2, 0], pairs[..., 1, :]), (fused, fused.clone()),
+             (torch.zeros(40).as_strided((1, 2, 3, 2), (0, 6, 4, 1)),), (fused[:0], fused[:0]), (fused[:, :, ::2], fused[:, :, 1::2])]
+    together = [(fused, fused), (fused[:, :, :4], fused[:, :, 3:]), (fused[:, :, 4:], fused[:, :, :5]), (fused[:, :10], fused[:, 1:]),
+                (fused[:, :1].expand(-1, 11, -1, -1),), (pairs[..., 0, :], pairs[:, :, 1:, 0]),
+                (torch.zeros(99).as_strided((1, 6, 2, 8), (0, 8, 8, 1)),)]
+    for xs in sound:
+        assert brute_apart(xs) and apart(xs, monkeypatch), [(t.shape, t.stride(), t.storage_offset()) for t in xs]
+    for xs in together:
+        assert not brute_apart(xs) and not apart(xs, monkeypatch), [(t.shape, t.stride(), t.storage_offset()) for t in xs]
+
+
+def test_overlaps_of_any_strides(monkeypatch):
+    """Against every element's place, for tensors of one store at random places."""
+    rng, store, found = random.Random(3), torch.zeros(4000), [0, 0]
+    for _ in range(3000):
+        B, N, d = rng.randint(1, 3), rng.randint(1, 4), rng.choice([2, 4])
+        alike = (rng.randint(0, 60), rng.choice([0, 1, 4, 8, 12, 16, 24, 48]))
+        xs = []
+        for _ in range(rng.choice([1, 2, 2])):
+            lead = alike if rng.random() < 0.7 else (rng.randint(0, 60), rng.randint(0, 24))
+            xs.append(store.as_strided((B, N, rng.randint(1, 3), d), (*lead, rng.choice([2, 4, 4, 8, 12, 50]), 1), rng.randint(0, 99)))
+        want = brute_apart(xs)
+        found[want] += 1
+        assert apart(xs, monkeypatch) == want, [(t.shape, t.stride(), t.storage_offset()) for t in xs]
+    assert min(found) > 300
+
+
+def test_two_tensors_that_write_one_place():
+    e = dict(heads=4, x_batch=1536, x_token=128, x_head=32, y_batch=1536, y_token=128, y_head=32)
+    at = lambda i: FAKE + i * 65536
+    for x0, y0, x1, y1 in ((0, 0, 0, 0), (0, 1, 2, 1), (0, 0, 0, 1), (0, 1, 1, 2), (0, 1, 2, 0)):
+        table = (RotaryTensor * 2)(RotaryTensor(x=at(x0), y=at(y0), **e), RotaryTensor(x=at(x1), y=at(y1), **e))
+        assert P.lib().qta_rotary(ctypes.addressof(table), 2, 2, 12, 32, 32, 1, 0, 0, 0, 0, FAKE, None, 0, 0, 1.0, None) == INVALID

@@ -33,3 +33,19 @@ def test_rotary_positions_that_are_refused(dev):
     wide = torch.zeros(1, 1, 1, 32, device=dev).expand(1, 2 ** 32 + 12, 1, 32)
     with pytest.raises(ValueError, match="2\\^31"):
         P.rotary(wide, P.rotary_freqs(32, device=dev))
+
+
+def test_in_place_tensors_that_overlap(dev):
+    """Refused; parts that lie apart are turned."""
+    fused = gen(72, dev)(2, 11, 7, 64)
+    f = P.rotary_freqs(64, device=dev)
+    before = fused.clone()
+    for x, k in ((fused, fused), (fused[:, :, :4], fused[:, :, 3:]), (fused[:, :10], fused[:, 1:])):
+        with pytest.raises(ValueError, match="share memory"):
+            P.rotary(x, f, k=k, inplace=True)
+    with pytest.raises(ValueError, match="share memory"):
+        P.rotary(fused.as_strided((1, 9, 2, 64), (0, 64, 64, 1)), f, inplace=True)
+    assert torch.equal(fused, before)
+    want = P.rotary(fused[:, :, 1::2], f), P.rotary(fused[:, :, ::2], f)
+    P.rotary(fused[:, :, 1::2], f, k=fused[:, :, ::2], inplace=True)
+    assert torch.equal(fused[:, :, 1::2], want[0]) and torch.equal(fused[:, :, ::2], want[1])
