@@ -254,7 +254,8 @@ class _Rotary(torch.autograd.Function):
 def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.0, start=0, inverse=False, inplace=False):
     """Rotary positions: the first ``rot = 2 * len(freqs)`` channels of every head turned pair by pair by
     position * freqs (fp64, radians; see ``rotary_freqs``), times ``scale``; the other channels are copied. Returns a new
-    tensor, or with ``k`` (the same tokens, its own number of heads) a pair of them from one launch. Differentiable.
+    tensor, or with ``k`` (the same tokens, its own number of heads) a pair of them from one launch. Differentiable in x and k
+    (reverse mode); frequencies that require gradients are refused.
 
     ``axes``: 1, or 2 for row and column positions, the first half of the turned channels going by the row and the rest by
     the column (the default for maps, ``[B, H, W, heads, d]``). ``pos``: int32 positions ``[N]`` or ``[B, N]``
@@ -264,7 +265,10 @@ def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.
     ``inplace``: overwrite x and k, which must not overlap, and return them; not differentiable."""
     xs = (x,) if k is None else (x, k)
     how = (axes, bool(interleaved), float(scale), int(start))
-    if torch.is_grad_enabled() and (getattr(x, "requires_grad", False) or getattr(k, "requires_grad", False)):
+    grad = torch.is_grad_enabled()
+    if grad and getattr(freqs, "requires_grad", False):
+        raise ValueError("freqs gets no gradient: detach it")
+    if grad and (getattr(x, "requires_grad", False) or getattr(k, "requires_grad", False)):
         if inplace:
             raise ValueError("in-place rotation of a tensor that requires gradients")
         if inverse:

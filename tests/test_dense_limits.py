@@ -141,3 +141,14 @@ def test_two_tensors_that_write_one_place():
     for x0, y0, x1, y1 in ((0, 0, 0, 0), (0, 1, 2, 1), (0, 0, 0, 1), (0, 1, 1, 2), (0, 1, 2, 0)):
         table = (RotaryTensor * 2)(RotaryTensor(x=at(x0), y=at(y0), **e), RotaryTensor(x=at(x1), y=at(y1), **e))
         assert P.lib().qta_rotary(ctypes.addressof(table), 2, 2, 12, 32, 32, 1, 0, 0, 0, 0, FAKE, None, 0, 0, 1.0, None) == INVALID
+
+
+# ---- derivatives that there are none of ----
+
+@pytest.mark.parametrize("leaf", [False, True])
+def test_frequencies_that_require_gradients(leaf):
+    x, f = torch.zeros(1, 4, 4, 32, requires_grad=leaf), P.rotary_freqs(32).requires_grad_()
+    with pytest.raises(ValueError, match="freqs"):
+        P.rotary(x, f)
+    with torch.no_grad(), pytest.raises(ValueError, match="GPU"):       # taken, but for the place of x
+        P.rotary(x, f)

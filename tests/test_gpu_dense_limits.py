@@ -49,3 +49,13 @@ def test_in_place_tensors_that_overlap(dev):
     want = P.rotary(fused[:, :, 1::2], f), P.rotary(fused[:, :, ::2], f)
     P.rotary(fused[:, :, 1::2], f, k=fused[:, :, ::2], inplace=True)
     assert torch.equal(fused[:, :, 1::2], want[0]) and torch.equal(fused[:, :, ::2], want[1])
+
+
+def test_frequencies_that_require_gradients(dev):
+    x, f = gen(73, dev)(1, 4, 2, 32), P.rotary_freqs(32, device=dev)
+    want = P.rotary(x, f)
+    for t in (x, x.clone().requires_grad_()):
+        with pytest.raises(ValueError, match="freqs"):
+            P.rotary(t, f.clone().requires_grad_())
+    with torch.no_grad():
+        assert torch.equal(P.rotary(x, f.clone().requires_grad_()), want)
