@@ -10,6 +10,7 @@ import ctypes
 import math
 
 import torch
+from torch.autograd import forward_ad
 from torch._C import _cuda_getCurrentRawStream as _raw_stream      # (torch.cuda.current_stream: 2 us a call)
 
 from .qta import _DTYPES, _SIGS, _check, _dtype_code, _scale, lib
@@ -87,6 +88,13 @@ def _call(name, t, *args):
             status = getattr(lib(), name)(*args, _raw_stream(dev))
     if status:
         _check(name, status)
+
+
+def _no_tangents(*tensors):
+    """Refuses dual tensors, whose derivative a result of the library's would not carry on."""
+    if getattr(forward_ad, "_current_level", 0) >= 0 and any(      # (outside every dual level none is dual: 0.1 us a call)
+            isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise NotImplementedError("rotary positions and differential attention have no forward-mode derivatives")
 
 
 def _new(t):
@@ -265,6 +273,7 @@ def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.
     ``inplace``: overwrite x and k, which must not overlap, and return them; not differentiable."""
     xs = (x,) if k is None else (x, k)
     how = (axes, bool(interleaved), float(scale), int(start))
+    _no_tangents(x, k, freqs)
     grad = torch.is_grad_enabled()
     if grad and getattr(freqs, "requires_grad", False):
         raise ValueError("freqs gets no gradient: detach it")
@@ -415,7 +424,8 @@ class _DiffAttention(torch.autograd.Function):
 
 
 def diff_attention(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None):
-    """Differentiable ``diff_attn``: gradients of q, k, v and lam."""
+    """Differentiable ``diff_attn`` (reverse mode): gradients of q, k, v and lam."""
+    _no_tangents(q, k, v, lam)
     if not (torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in (q, k, v, lam))):
         return diff_attn(q, k, v, lam, scale=scale, causal=causal, lens=lens, q_pos=q_pos)
     return _DiffAttention.apply(q, k, v, lam, scale, causal, lens, q_pos)

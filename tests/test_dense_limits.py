@@ -5,6 +5,7 @@ import random
 
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 import paper_2201_02767_amd as P
 from paper_2201_02767_amd import dense
@@ -152,3 +153,24 @@ def test_frequencies_that_require_gradients(leaf):
         P.rotary(x, f)
     with torch.no_grad(), pytest.raises(ValueError, match="GPU"):       # taken, but for the place of x
         P.rotary(x, f)
+
+
+@pytest.mark.parametrize("leaf", [False, True])
+def test_forward_mode_derivatives(leaf):
+    """Refused wherever the dual tensor comes in, with gradients on or off."""
+    def refused(call, *tensors, **more):
+        for i in range(len(tensors)):
+            args = [forward_ad.make_dual(t, torch.ones_like(t)) if j == i else t for j, t in enumerate(tensors)]
+            for mode in (torch.enable_grad, torch.no_grad):
+                with mode(), pytest.raises(NotImplementedError, match="forward-mode"):
+                    call(*args, **more)
+
+    x = torch.zeros(1, 4, 4, 32, requires_grad=leaf)
+    with forward_ad.dual_level():
+        refused(P.rotary, x, P.rotary_freqs(32))
+        refused(lambda a, b: P.rotary(a, P.rotary_freqs(32), k=b), x, x)
+        refused(P.rotary, x.detach(), P.rotary_freqs(32), inverse=True)
+        refused(P.rotary, x.detach(), P.rotary_freqs(32), inplace=True)
+        refused(P.diff_attention, x, x, torch.zeros(1, 4, 2, 64), torch.zeros(2))
+        with pytest.raises(ValueError, match="GPU"):                        # no dual tensor: taken, but for their place
+            P.rotary(x.detach(), P.rotary_freqs(32))

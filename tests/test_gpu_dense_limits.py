@@ -2,10 +2,11 @@
 refused, and what lies in places that nothing may use. Values against tests/dense_ref.py, as in test_gpu_dense.py."""
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 import paper_2201_02767_amd as P
 from tests import dense_ref as R
-from tests.test_gpu_dense import announce, dev, gen, within  # noqa: F401
+from tests.test_gpu_dense import announce, dev, gen, make, within  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -59,3 +60,14 @@ def test_frequencies_that_require_gradients(dev):
             P.rotary(t, f.clone().requires_grad_())
     with torch.no_grad():
         assert torch.equal(P.rotary(x, f.clone().requires_grad_()), want)
+
+
+def test_forward_mode_derivatives(dev):
+    q, k, v, lam, _ = make(dev, 1, 5, 6, 2, 1, 32, "f32")
+    f = P.rotary_freqs(32, device=dev)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(q, torch.ones_like(q))
+        for call in (lambda: P.rotary(dual, f), lambda: P.rotary(dual, f, inverse=True), lambda: P.diff_attention(dual, k, v, lam)):
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                call()
+        assert torch.equal(P.diff_attention(q, k, v, lam), P.diff_attn(q, k, v, lam))
