@@ -11,7 +11,6 @@ import math
 
 import torch
 from torch.autograd import forward_ad
-from torch._C import _cuda_getCurrentRawStream as _raw_stream      # (torch.cuda.current_stream: 2 us a call)
 
 from .qta import _DTYPES, _SIGS, _check, _dtype_code, _scale, lib
 
@@ -76,6 +75,11 @@ def _int32(t, name, like, *shapes):
     if t.shape not in shapes:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {' or '.join(str(s) for s in shapes)}")
     return t.data_ptr()
+
+
+def _raw_stream(dev):
+    """The current stream (torch.cuda.current_stream: 2 us a call). A torch without GPUs does not have the name."""
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 def _call(name, t, *args):

@@ -2,6 +2,8 @@
 is refused before anything reaches a device."""
 import ctypes
 import random
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -174,3 +176,13 @@ def test_forward_mode_derivatives(leaf):
         refused(P.diff_attention, x, x, torch.zeros(1, 4, 2, 64), torch.zeros(2))
         with pytest.raises(ValueError, match="GPU"):                        # no dual tensor: taken, but for their place
             P.rotary(x.detach(), P.rotary_freqs(32))
+
+
+def test_import_without_a_gpu_build_of_torch():
+    """Such a torch does not have the names of its GPU side."""
+    code = ("import torch\n"
+            "for n in [n for n in vars(torch._C) if n.startswith('_cuda_getCurrent')]: delattr(torch._C, n)\n"
+            "import paper_2201_02767_amd as P\n"
+            "assert P.level_dims(8, 8, 2) and P.rotary_freqs(8).numel() == 4")
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr
