@@ -30,6 +30,7 @@ qta_status check_diff(const qta_diff_attn_args* a, bool shapes_only)
     if (!(a->lam_dtype == QTA_F32 || (a->lam_dtype == QTA_BF16 && a->dtype == QTA_BF16))) return QTA_ERR_INVALID;
     if (!a->q || !a->k || !a->v || !a->lam) return QTA_ERR_INVALID;
     if (!aligned(a->q, 16) || !aligned(a->k, 16) || !aligned(a->v, 16)) return QTA_ERR_INVALID;
+    if (!aligned(a->lam, dtype_size(a->lam_dtype)) || !aligned(a->lens, 4) || !aligned(a->q_pos, 4)) return QTA_ERR_INVALID;
     const int size = dtype_size(a->dtype), piece = 16 / size;
     const int64_t tokens[9] = {a->q_batch, a->q_token, a->q_head, a->k_batch, a->k_token, a->k_head, a->v_batch, a->v_token, a->v_head};
     for (const int64_t s : tokens)
@@ -186,7 +187,8 @@ qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const float* m
     if (st != QTA_OK) return st;
     for (const void* p : {static_cast<const void*>(maps), dout, static_cast<const void*>(dq), static_cast<const void*>(dk), static_cast<const void*>(dv)})
         if (!p || !aligned(p, 16)) return QTA_ERR_INVALID;
-    if (!lse || !dlam || !workspace || !aligned(workspace, 256)) return QTA_ERR_INVALID;
+    if (!lse || !aligned(lse, 4) || !dlam || !aligned(dlam, dtype_size(args->lam_dtype))) return QTA_ERR_INVALID;
+    if (!workspace || !aligned(workspace, kAlign)) return QTA_ERR_INVALID;
     const BwdLayout L = bwd_layout(args, dlam_heads != 0);
     if (!bwd_fits(args, L)) return QTA_ERR_UNSUPPORTED;
     if (workspace_bytes < L.total) return QTA_ERR_WORKSPACE;

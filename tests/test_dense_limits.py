@@ -1,6 +1,7 @@
 """Sizes and arguments at the border of what rotary positions and differential attention take, on the host: what is past it
 is refused before anything reaches a device."""
 import ctypes
+import os
 import random
 import subprocess
 import sys
@@ -12,8 +13,9 @@ from torch.autograd import forward_ad
 import paper_2201_02767_amd as P
 from paper_2201_02767_amd import dense
 from paper_2201_02767_amd.dense import RotaryTensor
-from tests.test_dense_abi import FAKE, INVALID, UNSUPPORTED, backward, diff_args, forward, rotary
+from tests.test_dense_abi import BF16, FAKE, INVALID, UNSUPPORTED, WORKSPACE, backward, diff_args, forward, rotary
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 BLOCKS = 1 << 24        # of 256 threads: 2^32 threads, the first count that HIP does not take
 
 
@@ -184,5 +186,16 @@ def test_import_without_a_gpu_build_of_torch():
             "for n in [n for n in vars(torch._C) if n.startswith('_cuda_getCurrent')]: delattr(torch._C, n)\n"
             "import paper_2201_02767_amd as P\n"
             "assert P.level_dims(8, 8, 2) and P.rotary_freqs(8).numel() == 4")
-    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=ROOT)
     assert r.returncode == 0, r.stderr
+
+
+def test_alignment_of_the_small_arguments():
+    """Every pointer by its type."""
+    for n in ("lam", "lens", "q_pos"):
+        assert forward(causal=1, **{n: FAKE + 2}) == INVALID, n
+    half = dict(dtype=BF16, lam_dtype=BF16)
+    assert forward(lam=FAKE + 1, **half) == INVALID
+    assert backward(nbytes=16, kw=dict(half, lam=FAKE + 2), dlam=FAKE + 2) == WORKSPACE       # as far as that is checked
+    for kw, n, off in (({}, "dlam", 2), (half, "dlam", 1), ({}, "lse", 2)):
+        assert backward(nbytes=16, kw=kw, **{n: FAKE + off}) == INVALID, n
