@@ -398,7 +398,7 @@ qta_status qta_rotary(const qta_rotary_tensor* tensors, int count, int B, int N,
  *               channels contiguous, pointers 16-byte aligned, strides multiples of 16 bytes (0: broadcast).
  *   lam         lambda by strides: 0 for the batch and the token where a head has one weight. fp32, or bf16 with bf16 inputs.
  *   d           32 or 64; heads a multiple of kv_heads.
- *   scale       of the logits; <= 0: 1/sqrt(d).
+ *   scale       of the logits, 2^-96 .. 2^96; <= 0: 1/sqrt(d).
  *   alignment   of lam, lens, q_pos, lse and dlam: their type's.
  *   lens        device int32 [B] or NULL: element b's keys are [0, lens[b]) (clamped to [0, Nk]). What lies behind them is
  *               never used, whatever it holds.

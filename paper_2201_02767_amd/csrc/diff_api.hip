@@ -36,6 +36,8 @@ qta_status check_diff(const qta_diff_attn_args* a, bool shapes_only)
     for (const int64_t s : tokens)
         if (s < 0 || s % piece != 0) return QTA_ERR_INVALID;
     if (a->lam_batch < 0 || a->lam_token < 0 || a->lam_head < 0) return QTA_ERR_INVALID;
+    // (the backward starts logits from the sums' logarithms over the scale)
+    if (!(a->scale <= 0.f) && !(a->scale >= 0x1p-96f && a->scale <= 0x1p96f)) return QTA_ERR_INVALID;
     // inside one tile (at most 128 keys, or the rows of 65 queries) offsets are 31 bits
     const int64_t lim = (static_cast<int64_t>(1) << 30) / size;
     if (a->k_token > lim / 128 || a->v_token > lim / 128 || a->q_token > lim / 80 || a->q_head > lim / (2 * a->heads + 2)) return QTA_ERR_UNSUPPORTED;

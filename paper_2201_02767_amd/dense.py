@@ -327,6 +327,8 @@ def _diff_args(q, k, v, lam, scale, causal, lens, q_pos):
         raise ValueError(f"lam has shape {tuple(lam.shape)}, expected {(heads,)} or {(*q.shape[:-2], heads)}")
     if q_pos is not None and not causal:
         raise ValueError("q_pos goes with causal=True")
+    if scale is not None and not 2.0 ** -96 <= scale <= 2.0 ** 96:         # (zero and below mean 1/sqrt(d) to the library)
+        raise ValueError(f"scale must be positive, from 2^-96 to 2^96, got {scale}")
     args = DiffAttnArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(), B, heads, kv, Nq, Nk, d, code,
                         _DTYPES[lam.dtype], qb, qn, qh, kb, kn, kh, vb, vn, vh, lb, ln, lh,
                         None if lens is None else _int32(lens, "lens", q, (B,)),
@@ -381,7 +383,7 @@ def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, 
 
     ``lens`` (int32 ``[B]``): keys of each batch element; what lies behind them is never used, so k and v may be the
     whole of a cache. ``causal``: query i sees the keys up to position ``q_pos[b] + i`` (int32 ``[B]``; None: the
-    queries are the last Nq of Nk tokens). A row that sees no key gives 0. ``scale``: None for 1/sqrt(d).
+    queries are the last Nq of Nk tokens). A row that sees no key gives 0. ``scale``: positive, or None for 1/sqrt(d).
     ``keep``: also return what ``diff_attn_backward`` needs."""
     args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
     out, maps, lse = _diff_forward(args, shape, q, keep)

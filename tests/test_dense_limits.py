@@ -1,6 +1,7 @@
 """Sizes and arguments at the border of what rotary positions and differential attention take, on the host: what is past it
 is refused before anything reaches a device."""
 import ctypes
+import math
 import os
 import random
 import subprocess
@@ -199,3 +200,11 @@ def test_alignment_of_the_small_arguments():
     assert backward(nbytes=16, kw=dict(half, lam=FAKE + 2), dlam=FAKE + 2) == WORKSPACE       # as far as that is checked
     for kw, n, off in (({}, "dlam", 2), (half, "dlam", 1), ({}, "lse", 2)):
         assert backward(nbytes=16, kw=kw, **{n: FAKE + off}) == INVALID, n
+
+
+def test_scales_of_the_library():
+    for scale in (math.nan, math.inf, 2.0 ** 97, 2.0 ** -97, 1e-45):
+        assert forward(scale=scale) == INVALID, scale
+        assert backward(nbytes=16, kw=dict(scale=scale)) == INVALID, scale
+    for scale in (0.0, -1.0, -math.inf, 2.0 ** 96, 2.0 ** -96):
+        assert backward(nbytes=16, kw=dict(scale=scale)) == WORKSPACE, scale      # as far as that is checked

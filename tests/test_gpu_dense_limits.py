@@ -1,12 +1,14 @@
 """Rotary positions and differential attention on the GPU at the border of what they take: the largest sizes, calls that are
 refused, and what lies in places that nothing may use. Values against tests/dense_ref.py, as in test_gpu_dense.py."""
+import math
+
 import pytest
 import torch
 from torch.autograd import forward_ad
 
 import paper_2201_02767_amd as P
 from tests import dense_ref as R
-from tests.test_gpu_dense import announce, dev, gen, make, within  # noqa: F401
+from tests.test_gpu_dense import announce, check, dev, gen, make, within  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +73,21 @@ def test_forward_mode_derivatives(dev):
             with pytest.raises(NotImplementedError, match="forward-mode"):
                 call()
         assert torch.equal(P.diff_attention(q, k, v, lam), P.diff_attn(q, k, v, lam))
+
+
+def test_scales_that_are_refused(dev):
+    """None alone stands for 1/sqrt(d): a scale of zero or below, or one that is no number, is no other name of it."""
+    q, k, v, lam, do = make(dev, 1, 5, 6, 2, 1, 32, "f32")
+    _, kept = P.diff_attn(q, k, v, lam, keep=True)
+    for scale in (0.0, -0.5, math.nan, math.inf, 1e-45, 1e-60, 1e39):
+        for call in (lambda: P.diff_attn(q, k, v, lam, scale=scale), lambda: P.diff_attention(q.clone().requires_grad_(), k, v, lam, scale=scale),
+                     lambda: P.diff_attn_backward(q, k, v, lam, kept, do, scale=scale)):
+            with pytest.raises(ValueError, match="scale"):
+                call()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_small_and_large_scales(dev, dtype):
+    args = make(dev, 1, 40, 300, 2, 1, 32, dtype, seed=74)
+    for scale in (2.0 ** -96, 1e-12, 3.0):
+        check(dev, *args, scale=scale)
