@@ -297,14 +297,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
 
     // rows that see any of these keys: from the first query at or behind k0 on; this workgroup's tiles of them
     const int i0 = range.causal ? min(max(0, k0 - range.pos), f.Nq) : 0;
-    const int rbeg = (k0 < range.len ? i0 * G : f.R) / BM * BM;
-    const int all = k0 < range.len ? (f.R - rbeg + BM - 1) / BM : 0;
+    const bool seen = k0 < range.len && i0 < f.Nq;
+    const int rbeg = seen ? i0 * G / BM * BM : 0, all = seen ? (f.R - rbeg + BM - 1) / BM : 0;
     const int t0 = static_cast<int>(static_cast<long long>(all) * split / a.splits);
     const int t1 = static_cast<int>(static_cast<long long>(all) * (split + 1) / a.splits);
 
     if (t0 < t1) {
-        // (keys behind the element's last are read as that one; their weights are masked)
-        const int last = range.len - 1;
+        // (keys behind the last that any query sees are read as that one; their weights are masked)
+        const int last = range.limit(f.Nq - 1) - 1;
         const auto vmap = tiles::map_resource(byte_at(f.v, b * f.vb + k0 * f.vn + g * f.vh, ES));
         OT::stage(vt, vmap, BN, wave, 4, lane,
                   [&](int r) { return static_cast<uint32_t>(min(r, last - k0)) * (static_cast<uint32_t>(f.vn) * ES); });

@@ -208,3 +208,9 @@ def test_scales_of_the_library():
         assert backward(nbytes=16, kw=dict(scale=scale)) == INVALID, scale
     for scale in (0.0, -1.0, -math.inf, 2.0 ** 96, 2.0 ** -96):
         assert backward(nbytes=16, kw=dict(scale=scale)) == WORKSPACE, scale      # as far as that is checked
+
+
+def test_sources_that_may_see_a_nan():
+    """A weight of the backward overflows where its row does not see the key: compiled for NaNs."""
+    from paper_2201_02767_amd import build
+    assert "diff_attn_bwd.hip" not in build.NO_NAN_SOURCES
