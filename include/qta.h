@@ -405,7 +405,7 @@ qta_status qta_rotary(const qta_rotary_tensor* tensors, int count, int B, int N,
  *   causal      nonzero: query i of element b sees the keys up to q_pos[b] + i (device int32 [B]); q_pos NULL: Nk - Nq + i.
  * Sizes      fewer than 2^24 workgroups a launch: B kv_heads ceil(R / 64) (R = Nq heads / kv_heads rows, at most 2^26) and, in
  *             the backward, B kv_heads ceil(Nk / 128) + heads; Nk at most 2^28. What is past that is QTA_ERR_UNSUPPORTED.
- * A row that sees no key gives 0, and has and gives no gradient.
+ * A row that sees no key gives 0, and has and gives no gradient, whatever its q, dout and own lambda hold.
  * Sums, maxima and the softmax are fp32. With bf16 inputs the weights are rounded to bf16 for the products with V, and
  * results once at the end.
  */

@@ -78,6 +78,8 @@ struct DiffRange {
     int len, pos;
     bool causal;
     __device__ __forceinline__ int limit(int i) const { return causal ? max(0, min(len, pos + i + 1)) : len; }
+    // the query that query i is read as: itself, or, where it sees no key and may hold anything, the first that does
+    __device__ __forceinline__ int read_as(int i, int Nq) const { return causal ? max(i, min(-pos, Nq - 1)) : i; }
 };
 __device__ __forceinline__ DiffRange diff_range(const DiffArgs& a, int b)
 {

@@ -55,8 +55,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (KEYS ? 2 : 3) : 1) void
     const int rr = row0 + rb * 32 + (lane & 31), r = min(rr, a.R - 1);
     const int qi = fast_div(r, a.div_G), h = g * G + r - qi * G, lim = range.limit(qi);
     Frag<T> qf[D / 16];
+    const long long qat = range.read_as(qi, a.Nq);
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) qf[s] = global_frag<T>(a.q, b * a.qb + qi * a.qn + (2 * h + map) * a.qh + 16 * s + 8 * half);
+    for (int s = 0; s < D / 16; ++s) qf[s] = global_frag<T>(a.q, b * a.qb + qat * a.qn + (2 * h + map) * a.qh + 16 * s + 8 * half);
     f32x16 acc[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) acc[c] = f32x16{};
@@ -200,7 +201,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? (KEYS ? 2 : 3) : 1) void
             sum > 0.f ? mx + __builtin_amdgcn_logf(sum) : -INFINITY;
     __syncthreads();
     if (map == 1 || kb == 1 || rr >= a.R) return;
-    const float lam = diff_lambda(a, b, qi, h);
+    const float lam = sum > 0.f ? diff_lambda(a, b, qi, h) : 0.f;      // (a row without a key: whatever its weight is)
     T* const out = static_cast<T*>(a.out) + row * (2 * D) + 4 * half;
     float* const maps = a.maps + row * (4 * D) + 4 * half;
 #pragma unroll
@@ -263,7 +264,7 @@ __global__ __launch_bounds__(kThreads) void diff_join_kernel(DiffArgs a)
 #pragma unroll
             for (int m = 0; m < 2; ++m) o[m] += y[j][m] * __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f[m]), s + j));
     }
-    const float lam = diff_lambda(a, b, qi, h);
+    const float lam = sum[1] > 0.f ? diff_lambda(a, b, qi, h) : 0.f;
     const long long row = (static_cast<long long>(b) * a.Nq + qi) * a.heads + h;
 #pragma unroll
     for (int v = 0; v < V; ++v) {

@@ -87,14 +87,15 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
 
     const int rr = row0 + wave * 32 + (lane & 31), r = min(rr, f.R - 1);
     const int qi = fast_div(r, f.div_G), h = g * G + r - qi * G, lim = range.limit(qi);
+    const long long qat = range.read_as(qi, f.Nq);
     float miss = 0.f;                       // sum of P_1 (D - t_1)
     Frag<T> qf[2][D / 16], of[D / 8];
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int s = 0; s < D / 16; ++s)
-            qf[m][s] = global_frag<T>(f.q, b * f.qb + qi * f.qn + (2 * h + m) * f.qh + 16 * s + 8 * half);
-    const long long orow = ((static_cast<long long>(b) * f.Nq + qi) * f.heads + h) * (2 * D);
+            qf[m][s] = global_frag<T>(f.q, b * f.qb + qat * f.qn + (2 * h + m) * f.qh + 16 * s + 8 * half);
+    const long long orow = ((static_cast<long long>(b) * f.Nq + qat) * f.heads + h) * (2 * D);
 #pragma unroll
     for (int s = 0; s < D / 8; ++s) of[s] = global_frag<T>(a.dout, orow + 16 * s + 8 * half);
     // t_m, of this lane's half of the channels and then of both; the first part's workgroups leave what the key pass needs
@@ -114,11 +115,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dq_kern
     }
     t0 += other_half(t0);
     t1 += other_half(t1);
-    const float lam = diff_lambda(f, b, qi, h), nlam = -lam, nt0 = -t0, t01 = t0 - t1;
+    if (lim == 0) t0 = t1 = 0.f;            // (an element without a key has no row to read instead)
+    const float lam = lim > 0 ? diff_lambda(f, b, qi, h) : 0.f, nlam = -lam, nt0 = -t0, t01 = t0 - t1;
     const float* const lse = f.lse + (static_cast<long long>(b) * f.heads + h) * 2 * f.Nq + qi;
     const float nlse0 = -lse[0], nlse1 = -lse[f.Nq];
     if (split == 0 && half == 0 && rr < a.Rpad) {
-        const bool row = rr < f.R;
+        const bool row = rr < f.R && lim > 0;
         const float unit = from_statistics<T>() ? 1.0f / f.scale : 1.0f, nsign = lam < 0.f ? 1.0f : -1.0f;
         const float x[kDiffStats] = {nlse0 * unit, (nlse1 + __builtin_amdgcn_logf(fabsf(lam))) * unit, nt0, nsign * t01, nsign};
         float* const st = a.stats + static_cast<size_t>(bh) * kDiffStats * a.Rpad + rr;
@@ -322,8 +324,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void diff_dkv_ker
             const auto qmap0 = tiles::map_resource(byte_at(f.q, b * f.qb + i_first * f.qn + (2 * g * G) * f.qh, ES));
             const auto omap = tiles::map_resource(
                 byte_at(a.dout, ((static_cast<long long>(b) * f.Nq + i_first) * f.heads + g * G) * (2 * D), ES));
+            // (rows before the first that sees any of these keys are read as that one: they may hold anything)
             auto place = [&](int r, int* i, int* hh) {
-                const int x = min(r0 + r, f.R - 1);
+                const int x = min(max(r0 + r, i0 * G), f.R - 1);
                 *i = fast_div(x, f.div_G);
                 *hh = x - *i * G;
                 *i -= i_first;

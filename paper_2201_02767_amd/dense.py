@@ -383,7 +383,7 @@ def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, 
 
     ``lens`` (int32 ``[B]``): keys of each batch element; what lies behind them is never used, so k and v may be the
     whole of a cache. ``causal``: query i sees the keys up to position ``q_pos[b] + i`` (int32 ``[B]``; None: the
-    queries are the last Nq of Nk tokens). A row that sees no key gives 0. ``scale``: positive, or None for 1/sqrt(d).
+    queries are the last Nq of Nk tokens). A row that sees no key gives 0, whatever it holds. ``scale``: positive, or None for 1/sqrt(d).
     ``keep``: also return what ``diff_attn_backward`` needs."""
     args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
     out, maps, lse = _diff_forward(args, shape, q, keep)

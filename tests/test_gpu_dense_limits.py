@@ -91,3 +91,33 @@ def test_small_and_large_scales(dev, dtype):
     args = make(dev, 1, 40, 300, 2, 1, 32, dtype, seed=74)
     for scale in (2.0 ** -96, 1e-12, 3.0):
         check(dev, *args, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 64])
+def test_rows_that_see_no_key_may_hold_anything(dev, d, dtype):
+    """Queries before the first key (left padding) and those of elements without keys: NaN and infinities in their q, dout and
+    weight give zeros and reach no gradient, whether keys and rows are taken whole or in parts."""
+    for shape, lens, pos in (((4, 70, 90, 4, 2), [90, 50, 0, 90], [-40, -69, 3, -200]), ((3, 40, 2600, 4, 2), [2600, 31, 0], [-33, -9, 0]),
+                             ((3, 700, 130, 8, 1), [130, 9, 0], [-590, -699, 0]), ((3, 1, 700, 4, 1), [700, 0, 650], [-1, 0, 699])):
+        q, k, v, lam, do = make(dev, *shape, d, dtype, seed=75, token_lam=True)
+        rows = [t.clone() for t in (q, lam, do)]
+        for b, (n, p) in enumerate(zip(lens, pos)):
+            empty = shape[1] if n == 0 else min(max(-p, 0), shape[1])
+            for t, x in ((q, math.nan), (lam, math.inf), (do, -math.inf)):
+                t[b, :empty] = x
+                t[b, :empty // 2] = math.nan
+        announce(f"rows without a key {shape} {d} {dtype}")
+        how = dict(causal=True, lens=torch.tensor(lens, dtype=torch.int32, device=dev), q_pos=torch.tensor(pos, dtype=torch.int32, device=dev))
+        ref = R.diff_attention(rows[0], k, v, rows[1], dout=rows[2], causal=True, lens=lens, q_pos=pos)
+        out, kept = P.diff_attn(q, k, v, lam, keep=True, **how)
+        got = (P.diff_attn(q, k, v, lam, **how), out, *P.diff_attn_backward(q, k, v, lam, kept, do, **how))
+        torch.cuda.synchronize()
+        for n, t in zip(("out", "out", "dq", "dk", "dv", "dlam"), got):
+            within(n, t, ref[n])
+        # one weight a head: no sum over the rows takes them in
+        one = rows[1][0, -1].clone()
+        ref = R.diff_attention(rows[0], k, v, one, dout=rows[2], causal=True, lens=lens, q_pos=pos)
+        _, kept = P.diff_attn(q, k, v, one, keep=True, **how)
+        for n, t in zip(("dq", "dk", "dv", "dlam"), P.diff_attn_backward(q, k, v, one, kept, do, **how)):
+            within(n, t, ref[n])
