@@ -121,3 +121,37 @@ def test_rows_that_see_no_key_may_hold_anything(dev, d, dtype):
         _, kept = P.diff_attn(q, k, v, one, keep=True, **how)
         for n, t in zip(("dq", "dk", "dv", "dlam"), P.diff_attn_backward(q, k, v, one, kept, do, **how)):
             within(n, t, ref[n])
+
+
+def test_in_place_past_32_bits(dev):
+    """More than 2^31 elements turned where they lie: tokens at the start, around element 2^31 and at the end."""
+    N, heads, d = 270000, 128, 64
+    announce(f"in place {N} x {heads} x {d}")
+    x = gen(76, dev)(1, 100, heads, d).bfloat16().repeat(1, N // 100, 1, 1)
+    assert x.numel() > 2 ** 31
+    freqs, places = P.rotary_freqs(d, device=dev), (0, 2 ** 31 // (heads * d) - 50, N - 100)
+    before = [x[:, at:at + 100].clone() for at in places]
+    y = P.rotary(x, freqs, inplace=True)
+    assert y.data_ptr() == x.data_ptr()
+    for at, t in zip(places, before):
+        within(f"tokens from {at} on", x[:, at:at + 100], R.rotary(t, freqs, torch.arange(at, at + 100, device=dev)[None, :, None]))
+
+
+def test_gradients_past_32_bits(dev):
+    """dQ, dout and the kept maps of more than 2^31 elements. Only the last rows have an upstream gradient, so that every
+    gradient is that of a call on these rows alone, and zero elsewhere."""
+    N, heads, d, last = 270000, 64, 64, 200
+    announce(f"gradients {N} x {heads} x {d}")
+    r = gen(77, dev)
+    q = r(1, 100, 2 * heads, d).bfloat16().repeat(1, N // 100, 1, 1)
+    k, v, lam = r(1, 40, 2 * heads, d).bfloat16(), r(1, 40, heads, 2 * d).bfloat16(), 0.5 + 0.1 * r(heads)
+    do = torch.zeros(1, N, heads, 2 * d, dtype=torch.bfloat16, device=dev)
+    do[:, -last:] = r(1, last, heads, 2 * d).bfloat16()
+    out, kept = P.diff_attn(q, k, v, lam, keep=True)
+    dq, dk, dv, dlam = P.diff_attn_backward(q, k, v, lam, kept, do)
+    torch.cuda.synchronize()
+    assert dq.numel() > 2 ** 31 and out.numel() > 2 ** 31
+    ref = R.diff_attention(q[:, -last:], k, v, lam, dout=do[:, -last:])
+    for n, t in (("out", out[:, -last:]), ("dq", dq[:, -last:]), ("dk", dk), ("dv", dv), ("dlam", dlam)):
+        within(n, t, ref[n])
+    assert not bool((dq[:, :-last] != 0).any())
