@@ -1,6 +1,7 @@
 """Rotary positions and differential attention on the GPU at the border of what they take: the largest sizes, calls that are
 refused, and what lies in places that nothing may use. Values against tests/dense_ref.py, as in test_gpu_dense.py."""
 import math
+import sys
 
 import pytest
 import torch
@@ -155,3 +156,22 @@ def test_gradients_past_32_bits(dev):
     for n, t in (("out", out[:, -last:]), ("dq", dq[:, -last:]), ("dk", dk), ("dv", dv), ("dlam", dlam)):
         within(n, t, ref[n])
     assert not bool((dq[:, :-last] != 0).any())
+
+
+@pytest.mark.parametrize("d", [32, 64])
+@pytest.mark.parametrize("shape", [(2, 300, 300, 4, 2), (2, 3, 3000, 4, 2), (1, 700, 130, 8, 1)], ids=lambda s: "x".join(map(str, s)))
+def test_fp32_keeps_its_bits(dev, shape, d):
+    """The root mean square of the errors, where the bounds element by element are worst cases that leave room for products
+    of far fewer bits. With f = 2^-24 and independent roundings of 0.4 f of the value each: a logit of d products is off by
+    0.4 f sqrt(d) of its size 1.3, 4 f at d = 64; its exponent, below 16, by 2^-21 / sqrt(3) ln 2 = 3.2 f; D = dO V^T, of 2d
+    products, by 0.4 f sqrt(2d) = 4.5 f; a sum of N terms by 0.28 f sqrt(N), 15 f for the 3000 of a row in one piece. Together
+    sqrt(16 + 10 + 20 + 225) f = 17 f of a result at most, and twice that is the limit. Products of 16 bits of mantissa are
+    off by 2^-17 = 128 f."""
+    q, k, v, lam, do = make(dev, *shape, d, "f32", seed=78, token_lam=True)
+    announce(f"fp32 bits {shape} {d}")
+    ref = R.diff_attention(q, k, v, lam, dout=do)
+    out, kept = P.diff_attn(q, k, v, lam, keep=True)
+    for n, t in zip(("out", "dq", "dk", "dv", "dlam"), (out, *P.diff_attn_backward(q, k, v, lam, kept, do))):
+        off = float((t.double() - ref[n][0]).square().mean().sqrt() / ref[n][0].square().mean().sqrt()) * 2 ** 24
+        print(f"{n}: {off:.1f} f", file=sys.stderr)
+        assert off <= 34.0, (n, off)
