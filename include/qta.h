@@ -406,8 +406,8 @@ qta_status qta_rotary(const qta_rotary_tensor* tensors, int count, int B, int N,
  * Sizes      fewer than 2^24 workgroups a launch: B kv_heads ceil(R / 64) (R = Nq heads / kv_heads rows, at most 2^26) and, in
  *             the backward, B kv_heads ceil(Nk / 128) + heads; Nk at most 2^28. What is past that is QTA_ERR_UNSUPPORTED.
  * A row that sees no key gives 0, and has and gives no gradient, whatever its q, dout and own lambda hold.
- * Sums, maxima and the softmax are fp32. With bf16 inputs the weights are rounded to bf16 for the products with V, and
- * results once at the end.
+ * Sums, maxima and the softmax are fp32. With bf16 inputs the weights are rounded to bf16 for the products with V (in
+ * calls of up to 32 rows R to two bf16 terms, 16 bits), and results once at the end.
  */
 typedef struct {
     const void* q;

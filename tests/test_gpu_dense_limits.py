@@ -175,3 +175,16 @@ def test_fp32_keeps_its_bits(dev, shape, d):
         off = float((t.double() - ref[n][0]).square().mean().sqrt() / ref[n][0].square().mean().sqrt()) * 2 ** 24
         print(f"{n}: {off:.1f} f", file=sys.stderr)
         assert off <= 34.0, (n, off)
+
+
+@pytest.mark.parametrize("d", [32, 64])
+@pytest.mark.parametrize("shape", [(4, 1, 512, 8, 8), (2, 1, 5000, 16, 4), (3, 5, 1025, 8, 2)], ids=lambda s: "x".join(map(str, s)))
+def test_bf16_tokens_are_rounded_once(dev, shape, d):
+    """A token or a few over a cache, bf16: off by the rounding of the result, and by 2^-17 of the weights, whose two bf16
+    terms hold 16 bits: (2^-8)^2 more of its square, and 100 times that where the two maps cancel to a tenth, 0.2%."""
+    q, k, v, lam, _ = make(dev, *shape, d, "bf16", seed=79)
+    announce(f"bf16 tokens {shape} {d}")
+    ref = R.diff_attention(q, k, v, lam)["out"][0]
+    off = float((P.diff_attn(q, k, v, lam).double() - ref).square().mean().sqrt() / (ref.bfloat16().double() - ref).square().mean().sqrt())
+    print(f"{off:.3f} of the rounding", file=sys.stderr)
+    assert off <= 1.02
