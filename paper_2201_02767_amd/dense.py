@@ -235,9 +235,9 @@ def _apart_anyhow(at, axes, d, size):
     # every head's place
     places = []
     for p, x in zip(at, axes):
-        p = torch.full((1,), p, dtype=torch.int64)
+        p = torch.full((1,), p, dtype=torch.int64, device="cpu")
         for s, n in x:
-            p = (p[:, None] + torch.arange(n, dtype=torch.int64) * (s * size)).flatten()
+            p = (p[:, None] + torch.arange(n, dtype=torch.int64, device="cpu") * (s * size)).flatten()
         places.append(p)
     return bool((torch.cat(places).sort().values.diff() >= d * size).all())
 

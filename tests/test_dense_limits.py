@@ -214,3 +214,12 @@ def test_sources_that_may_see_a_nan():
     """A weight of the backward overflows where its row does not see the key: compiled for NaNs."""
     from paper_2201_02767_amd import build
     assert "diff_attn_bwd.hip" not in build.NO_NAN_SOURCES
+
+
+def test_overlaps_under_a_default_device(monkeypatch):
+    """Places are counted on the host, whatever device new tensors go to."""
+    store = torch.zeros(60)
+    for stride, want in (((0, 3, 2, 1), False), ((0, 6, 4, 1), True)):
+        x = store.as_strided((1, 2, 3, 2), stride)
+        with torch.device("meta"):
+            assert apart((x,), monkeypatch) == want
