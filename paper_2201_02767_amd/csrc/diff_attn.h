@@ -47,7 +47,7 @@ struct DiffArgs {
 
 // How a forward's keys are split. Up to 32 rows of a key head (a token or a few, of all the query heads that share it): the
 // waves of a workgroup take halves of each key tile, since half of them would find no rows (16 tokens over caches of 16384
-// to 32768 keys, 32 heads over 8, d = 64, bf16: 265 us, by rows 292; 8 x 5 tokens over 4097 keys, 16 heads over 4,
+// to 32768 keys, 32 heads over 8, d = 64, bf16: 270 us, by rows 292; 8 x 5 tokens over 4097 keys, 16 heads over 4,
 // d = 32, fp32: 22 us, by rows 32). And where the rows do not give every unit a workgroup (fp32, whose products take 16
 // times as long: two), the keys come in parts that make four workgroups a unit, none below 256 keys (4800 fp32 tokens,
 // 4 heads, d = 32: 510 us whole, 381 in two parts, 327 in four; the long caches: 289 us with two workgroups a unit, 274 with

@@ -5,10 +5,11 @@
 // the difference is formed once at the end through LDS.
 //
 // What bounds it: long prompts the matrix and the vector units together, at the clock that their power leaves (2 x 8192 causal
-// tokens, 16 heads over 4, d = 64, bf16: 830 us, 994 TFLOP/s of products at 1.9 GHz, where a large library product reaches
-// 1305); single tokens the caches' bytes (1.6 GB: 265 us, 6 TB/s). Four waves a SIMD with a few spills: 806 us, but 264 instead
-// of 236 for the forward of training, which writes more; one wave over 64 rows: 793 us, none gained in training;
-// tiles of 64 keys: 895 us; a pipeline over three tiles that alternates matrix and vector instructions: 930 us.
+// tokens, 16 heads over 4, d = 64, bf16: 792 to 819 us, 1007 to 1041 TFLOP/s of products at 1.9 GHz, where a large library
+// product reaches 1305); single tokens the caches' bytes (1.6 GB: 270 us, 6 TB/s). Tried beside 830 us for prompts on one
+// card: four waves a SIMD with a few spills 806 us, but 264 instead of 236 for the forward of training, which writes more; one
+// wave over 64 rows 793 us, none gained in training; tiles of 64 keys 895 us; a pipeline over three tiles that alternates
+// matrix and vector instructions 930 us.
 #include <atomic>
 #include <type_traits>
 

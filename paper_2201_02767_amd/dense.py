@@ -2,7 +2,8 @@
 
 Argument marshalling only, like ``qta.py``. Tokens come as sequences ``[B, N, heads, d]`` or as maps
 ``[B, H, W, heads, d]`` (fp32 or bf16, on a GPU); views are taken as they are as long as the channels of a head are
-contiguous and, on a map, its rows follow each other at one distance.
+contiguous and, on a map, its rows follow each other at one distance. Attention also needs tensors that start on 16 bytes
+with all strides multiples of 16 bytes; rotary positions take any.
 """
 from __future__ import annotations
 
