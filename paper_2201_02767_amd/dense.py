@@ -272,8 +272,8 @@ def rotary(x, freqs, *, k=None, pos=None, axes=None, interleaved=False, scale=1.
 
     ``axes``: 1, or 2 for row and column positions, the first half of the turned channels going by the row and the rest by
     the column (the default for maps, ``[B, H, W, heads, d]``). ``pos``: int32 positions ``[N]`` or ``[B, N]``
-    (``[.., N, 2]`` for two axes, N = H*W on a map); None: ``start`` + 0, 1, .. (below 2^31) along the tokens for one axis, the coordinates of a map
-    for two.
+    (``[.., N, 2]`` for two axes, N = H*W on a map); None: ``start`` + 0, 1, .. (below 2^31) along the tokens for one axis,
+    the coordinates of a map for two.
     ``interleaved``: pairs are neighbouring channels instead of the two halves of an axis. ``inverse``: turn back.
     ``inplace``: overwrite x and k, which must not overlap, and return them; not differentiable."""
     xs = (x,) if k is None else (x, k)
@@ -384,8 +384,8 @@ def diff_attn(q, k, v, lam, *, scale=None, causal=False, lens=None, q_pos=None, 
 
     ``lens`` (int32 ``[B]``): keys of each batch element; what lies behind them is never used, so k and v may be the
     whole of a cache. ``causal``: query i sees the keys up to position ``q_pos[b] + i`` (int32 ``[B]``; None: the
-    queries are the last Nq of Nk tokens). A row that sees no key gives 0, whatever it holds. ``scale``: positive, or None for 1/sqrt(d).
-    ``keep``: also return what ``diff_attn_backward`` needs."""
+    queries are the last Nq of Nk tokens). A row that sees no key gives 0, whatever it holds. ``scale``: positive, or None
+    for 1/sqrt(d). ``keep``: also return what ``diff_attn_backward`` needs."""
     args, shape = _diff_args(q, k, v, lam, scale, causal, lens, q_pos)
     out, maps, lse = _diff_forward(args, shape, q, keep)
     return (out, (maps, lse)) if keep else out
