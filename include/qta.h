@@ -453,6 +453,67 @@ qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const float* m
                                   void* dq, void* dk, void* dv, void* dlam, int dlam_heads, void* workspace,
                                   size_t workspace_bytes, void* stream);
 
+/* ---- linear attention with a decay, and group norm ---- */
+
+/*
+ * Linear attention with a decay for each head. Each head carries a state, a dk x dv matrix, from token to token,
+ *   S_t = exp(g) S_{t-1} + k_t v_t^T,   o_t = scale * S_t^T q_t,   g = log_decay[head],
+ * that is o_t = scale * (sum over s <= t of exp(g (t - s)) (q_t . k_s) v_s + exp(g (t + 1)) S^T q_t) with S the state before
+ * the first token.
+ *   q, k        [B][N][heads][dk], v [B][N][heads][dv] dtype, by strides in elements; channels contiguous, pointers 16-byte
+ *               aligned, strides multiples of 16 bytes (0: broadcast).
+ *   log_decay   device fp32 [heads], natural logarithms of the decays: <= 0 (-inf: nothing is remembered). A positive one grows;
+ *               results are then right as long as they are finite. Beyond +-11356 it counts as that.
+ *   state       fp32 [B][heads][dk][dv] contiguous, 16-byte aligned, or NULL for zeros.
+ *   dk, dv      32, 64 or 128 each.
+ *   scale       2^-64 .. 2^64; <= 0: 1/sqrt(dk).
+ *   lens        device int32 [B] or NULL: element b's tokens are [0, lens[b]) (clamped to [0, N]). What lies behind them is never
+ *               used, whatever it holds; its results are zeros.
+ * Tokens before the lengths are finite: a tile computes the places that the order of time masks and leaves them out by a weight
+ * of zero. Sums and states are fp32. With bf16 inputs the state and the weighted scores are taken into products as two bf16
+ * terms (16 bits), what is added to the state as three (24 bits), and results are rounded once.
+ */
+typedef struct {
+    const void* q;
+    const void* k;
+    const void* v;
+    const float* log_decay;
+    const float* state;
+    int B, heads, N, dk, dv;
+    qta_dtype dtype;
+    int64_t q_batch, q_token, q_head;
+    int64_t k_batch, k_token, k_head;
+    int64_t v_batch, v_token, v_head;
+    const int32_t* lens;
+    float scale;
+} qta_decay_attn_args;
+
+/*
+ * qta_decay_attn - the forward.
+ *   out         [B][N][heads][dv] dtype, contiguous, 16-byte aligned, overwritten.
+ *   state_out   fp32 [B][heads][dk][dv], 16-byte aligned: the state behind the last token (lens[b] = 0: the state before).
+ *               NULL: not asked for. It may be `state` itself; otherwise the two must not overlap.
+ *   workspace   qta_decay_attn_workspace_bytes bytes (at least 256 for valid shapes, 0 otherwise), 256-byte aligned, in which long
+ *               calls put the states of their parts; may be NULL where 256 are asked for. Need not be preserved or cleared; calls
+ *               that may run at the same time need one each.
+ */
+size_t qta_decay_attn_workspace_bytes(const qta_decay_attn_args* args);
+qta_status qta_decay_attn(const qta_decay_attn_args* args, void* out, float* state_out, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * qta_decay_attn_backward - gradients for dout = dLoss/dout and dstate_out = dLoss/dstate_out (NULL: zeros).
+ *   dout        [B][N][heads][dv] dtype, contiguous; never used behind the lengths.
+ *   dstate_out  fp32 [B][heads][dk][dv], contiguous.
+ *   dq, dk, dv  dtype, contiguous in the shapes of q, k and v, overwritten (behind the lengths with zeros). For inputs broadcast
+ *               by a zero stride the gradient comes in the full shape.
+ *   dstate      fp32 [B][heads][dk][dv], overwritten; NULL: not asked for. Not dstate_out itself.
+ * All 16-byte aligned. log_decay gets no gradient. Sums are made in a fixed order: runs are identical.
+ */
+size_t qta_decay_attn_backward_workspace_bytes(const qta_decay_attn_args* args);
+qta_status qta_decay_attn_backward(const qta_decay_attn_args* args, const void* dout, const float* dstate_out, void* dq,
+                                   void* dk, void* dv, float* dstate, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,98 @@
+// Linear attention with a decay: argument blocks and the rules by which its work is divided.
+//
+//   S_t = exp(g) S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t
+//
+// Over a chunk of C tokens behind a state S (i, j = 0 .. C-1 within the chunk):
+//   o_i = f exp(g (i + 1 - e)) S^T q_i + scale sum over j <= i of exp(g (i - j)) (q_i . k_j) v_j
+//   S  <- exp(g C) S + u sum over j of exp(g (C - 1 - j + e)) k_j v_j^T
+// with e = 0, f = scale, u = 1 in the forward. The gradients are the same sums. With R the loss's gradient with respect to the state,
+//   dq_t = scale S_t do_t:                  the forward with (do, v, k) for (q, k, v) and S transposed;
+//   dv_s = R_s^T k_s, dk_s = R_s v_s,       R_s = exp(g) R_{s+1} + scale q_s do_s^T: with time running back, (k, q, do) and
+//                                           (v, do, q), and e = 1, f = 1, u = scale, since R starts as the gradient of the last state.
+// So one kernel serves all four; a role says what is read as q, k and v, and which way.
+#ifndef QTA_DECAY_ATTN_H
+#define QTA_DECAY_ATTN_H
+
+#include <algorithm>
+
+#include "diff_attn.h"
+
+namespace qta {
+
+struct DecayRole {
+    const void *q, *k, *v;                                      // [B][N][heads][.] by strides in elements
+    long long qb, qn, qh, kb, kn, kh, vb, vn, vh;
+    void* out;                  // [B][N][heads][DV] contiguous
+    const float* state;         // before the first token, or (with several segments) before each segment; NULL: zeros
+    int s_row, s_col;           // its strides (a transposed state has s_row = 1)
+    float* last;                // the state behind the last token, laid out like `state`, from calls of one segment; or NULL
+    bool back;                  // time runs back: e = 1
+    float f, u;                 // see above
+};
+
+struct DecayArgs {
+    DecayRole role[3];
+    int roles, B, heads, N;
+    int segs, seg;              // a (batch, head)'s tokens in `segs` segments of `seg` tokens
+    FastDiv div_segs, div_heads;
+    const float* log_decay;
+    const int32_t* lens;
+    float scale;
+    float* part;                // fp32 [roles][B][heads][segs][DK][DV]: what each segment adds to the state, then the states before them
+};
+
+// The scan over segments: part[r] becomes the states before each segment, and last[r] the one behind the last.
+struct DecayScanArgs {
+    float* part;
+    const float* state[2];      // before the first token, NULL: zeros
+    float* last[2];             // may be state itself; NULL: not asked for
+    int B, heads, N, segs, seg, cells;      // cells: dk * dv
+    const float* log_decay;
+    const int32_t* lens;
+};
+
+struct DecayStepArgs {
+    const void *q, *k, *v;
+    long long qb, qn, qh, kb, kn, kh, vb, vn, vh;
+    void* out;
+    const float* state;         // NULL: zeros
+    float* last;                // NULL: not asked for
+    int B, heads, N;
+    FastDiv div_heads;
+    const float* log_decay;
+    const int32_t* lens;
+    float scale;
+};
+
+// Calls of up to this many tokens go token by token through states that stay in registers.
+constexpr int kDecayStepTokens = 16;
+
+// Tokens of a chunk: as many as LDS holds twice.
+constexpr int decay_chunk(bool bf16_inputs) { return bf16_inputs ? 64 : 32; }
+
+// Segments of a call.
+struct DecaySegments {
+    int segs, seg;
+};
+inline DecaySegments decay_segments(int B, int heads, int N, int roles, bool bf16_inputs)
+{
+    const long long chunk = decay_chunk(bf16_inputs), rows = static_cast<long long>(B) * heads * roles;
+    const long long want = 4LL * device_cu_count();
+    const long long most = (N + 4 * chunk - 1) / (4 * chunk);
+    const long long segs = std::max(1LL, std::min(most, (want + rows - 1) / rows));
+    const long long seg = ((N + segs - 1) / segs + chunk - 1) / chunk * chunk;
+    return {static_cast<int>((N + seg - 1) / seg), static_cast<int>(seg)};
+}
+
+constexpr long long kDecayMaxBlocks = (1LL << 32) / 256 - 1;
+
+hipError_t launch_decay_step(const DecayStepArgs& a, int dk, int dv, bool use_bf16, hipStream_t stream);
+// What the segments add to the states (roles' k and v).
+hipError_t launch_decay_states(const DecayArgs& a, int dk, int dv, bool use_bf16, hipStream_t stream);
+hipError_t launch_decay_scan(const DecayScanArgs& a, int roles, hipStream_t stream);
+// The results of a's roles; dk, dv are the sizes as the roles read them.
+hipError_t launch_decay_chunks(const DecayArgs& a, int dk, int dv, bool use_bf16, hipStream_t stream);
+
+}  // namespace qta
+
+#endif

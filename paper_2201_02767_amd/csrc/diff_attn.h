@@ -217,15 +217,18 @@ struct Tile {
         const int r = lane & 31;
         return static_cast<uint32_t>(r * kRow + (((lane >> 5) * parts) ^ swz(r)) * 16);
     }
-    __device__ static __forceinline__ uint32_t col_base(int lane)
+    // (`swapped`: lane l gets column 32 ct + (l & 31 with bits 2 and 3 exchanged). A result whose rows are these columns, packed by
+    // eight, is then a fragment in the natural order of row_frag.)
+    __device__ static __forceinline__ uint32_t col_base(int lane, bool swapped = false)
     {
         const int h = lane >> 5;
         if constexpr (sizeof(T) == 2) {
             // 16 lanes read 4 rows x 32 bytes, 8 bytes each, and receive one column of the four rows each
-            const int i = lane & 15, r = 4 * h + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
-            return static_cast<uint32_t>(r * kRow + (c ^ swz(r)) * 16 + (i & 1) * 8);
+            const int i = lane & 15, r = 4 * h + (i >> 2), hi = (i >> 1) & 1, lo = i & 1;
+            const int c = 2 * ((lane >> 4) & 1) + (swapped ? lo : hi);
+            return static_cast<uint32_t>(r * kRow + (c ^ swz(r)) * 16 + (swapped ? hi : lo) * 8);
         } else {
-            const int col = lane & 31;
+            const int l = lane & 31, col = swapped ? (l & 19) | (l & 4) << 1 | (l & 8) >> 1 : l;
             return static_cast<uint32_t>(4 * h * kRow + ((col >> 2) ^ swz(4 * h)) * 16 + (col & 3) * 4);
         }
     }

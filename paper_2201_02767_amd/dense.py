@@ -99,7 +99,7 @@ def _no_tangents(*tensors):
     """Refuses dual tensors, whose derivative a result of the library's would not carry on."""
     if getattr(forward_ad, "_current_level", 0) >= 0 and any(      # (outside every dual level none is dual: 0.1 us a call)
             isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
-        raise NotImplementedError("rotary positions and differential attention have no forward-mode derivatives")
+        raise NotImplementedError("rotary positions, differential and decay attention and group norm have no forward-mode derivatives")
 
 
 def _new(t):
