@@ -514,6 +514,51 @@ size_t qta_decay_attn_backward_workspace_bytes(const qta_decay_attn_args* args);
 qta_status qta_decay_attn_backward(const qta_decay_attn_args* args, const void* dout, const float* dstate_out, void* dq,
                                    void* dk, void* dv, float* dstate, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Group norm with an activation, channels last. The C channels of a token are `groups` groups of C / groups neighbours; with mean and
+ * var (its values' mean squared distance from it) of a group over the N tokens of a batch element, or over one token with per_token,
+ *   y = act(w * (x - mean) / sqrt(var + eps) + b).
+ *   x           [B][N][C] dtype by strides in elements, channels contiguous, aligned to its type (16-byte aligned tensors whose strides
+ *               and C are multiples of 16 bytes take 16-byte accesses, others narrower ones).
+ *   weight, bias  [C] contiguous, fp32 or (with bf16 x) bf16, aligned to their type; each may be NULL (1 and 0).
+ *   groups      divides C; B * N and C at most 2^30 and 2^20, B * C at most 2^30.
+ *   eps         at least 0 (a group of equal values is then 0 times infinity).
+ * Statistics and sums are fp32, differences from the mean, in a fixed order: runs are identical. Results are rounded once.
+ */
+typedef enum { QTA_ACT_NONE = 0, QTA_ACT_RELU = 1, QTA_ACT_SILU = 2, QTA_ACT_GELU = 3 } qta_act;    /* GELU by the error function */
+typedef struct {
+    const void* x;
+    const void* weight;
+    const void* bias;
+    int B, N, C, groups;
+    qta_dtype dtype, param_dtype;
+    int64_t x_batch, x_token;
+    int per_token;
+    qta_act act;
+    float eps;
+} qta_group_norm_args;
+
+/*
+ * qta_group_norm - the forward.
+ *   y           [B][N][C] dtype, contiguous, aligned as x. Not x itself.
+ *   stats       for qta_group_norm_backward: fp32 [B][groups][2], mean and 1 / sqrt(var + eps), 8-byte aligned. NULL for inference, and
+ *               not used with per_token.
+ *   workspace   qta_group_norm_workspace_bytes bytes (at least 256 for valid shapes, 0 otherwise), 256-byte aligned; may be NULL where 256
+ *               are asked for. Need not be preserved or cleared; calls that may run at the same time need one each.
+ */
+size_t qta_group_norm_workspace_bytes(const qta_group_norm_args* args);
+qta_status qta_group_norm(const qta_group_norm_args* args, void* y, float* stats, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * qta_group_norm_backward - gradients for dy = dLoss/dy, contiguous, aligned as x; stats are the forward's (not used with per_token).
+ *   dx          [B][N][C] dtype, contiguous, overwritten.
+ *   dweight, dbias  [C] param_dtype, overwritten; each may be NULL. (With weight NULL they are those of weights of 1 and 0.)
+ */
+size_t qta_group_norm_backward_workspace_bytes(const qta_group_norm_args* args);
+qta_status qta_group_norm_backward(const qta_group_norm_args* args, const float* stats, const void* dy, void* dx, void* dweight,
+                                   void* dbias, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif
