@@ -29,33 +29,41 @@ struct NormArgs {
     void* dbias;
     float* part;                // see NormPlan
     // set by the launchers from the plan
-    int cols, rows, slabs, blocks, parts, entries;
+    int cols, rows, slabs, slab, blocks, parts, entries;
+    unsigned own;               // workgroups of the launch that have tokens
     int lanes, sums;            // (per token) lanes of a group; workgroups' sums in part
-    FastDiv div_N, div_P;
+    int rows_lanes;             // lanes that share the rows of a channel
+    float* group_part;
+    FastDiv div_N, div_slabs, div_rows, div_entry;
 };
 
-// Maps: a workgroup of kNormThreads threads takes a block of `cols` vector columns, `rows` tokens at a time, of one slab of the tokens of
+// Maps take two launches that each go over them (bound by memory: 8 maps of 200 x 336 x 256 bf16, 275 MB each, SiLU: 45 us to read x, 103 to
+// read it and write y, 101 to read x and dy, 157 to read them and write dx, 5.2 to 6.1 TB/s, where a large copy makes 5.1). The second
+// goes through every slab from its end, where the memory's cache still holds what the first read last, and stores go past the caches (with
+// ordinary stores, whose lines the next kernel's reads push out, and upwards: 71, 95, 150 and 164 us).
+// Batch elements one after the other, which would fit the caches, fill the card too badly: 467 us for these 407.
+//
+// A workgroup of kNormThreads threads takes a block of `cols` vector columns, `rows` tokens at a time, of one slab of the tokens of
 // a batch element. A thread's channels stay the same, and its sums over tokens stay in registers. Blocks hold whole groups, or
 // where a group is wider than a workgroup, a part of one (`parts` a group).
-constexpr int kNormThreads = 512;
+constexpr int kNormThreads = 1024;
 
 struct NormPlan {
     bool tokens;                // every token by itself: its groups in registers, or `wide`, a group a workgroup
     bool wide;
     int V;                      // elements of an access
-    int cols, rows, slabs, blocks, parts;
+    int cols, rows, slabs, slab, blocks, parts;      // slab: its tokens
     int lanes, pieces, grid;    // per token: lanes of a group, accesses of a lane, workgroups
-    // bytes of `part`: forward [B][slabs][groups * parts] (mean, sum of squared distances); backward [sums][C] (sum dz n, sum dz),
-    // sums = B * slabs, or per token `grid`
-    size_t fwd_bytes, bwd_bytes;
+    // of `part`: in the backward [sums][C] (sum dz n, sum dz), sums = B * slabs, or per token `grid`; then but per token
+    // [B][slabs][groups * parts] (forward: mean, sum of squared distances; backward: sum dn n, sum dn)
+    size_t channel_floats;
+    size_t bytes;
 };
 
 constexpr int kNormMaxPieces = 4;
 
-inline int norm_gcd(int a, int b) { return b ? norm_gcd(b, a % b) : a; }
-
 // `align`: elements that everything about x, y, dy and dx (addresses, strides) is a multiple of, a power of two up to 16 bytes.
-inline NormPlan norm_plan(int B, int N, int C, int groups, bool per_token, bool bf16_inputs, int align)
+inline NormPlan norm_plan(int B, int N, int C, int groups, bool per_token, bool bf16_inputs, int align, bool back)
 {
     NormPlan p{};
     const int P = C / groups;
@@ -76,13 +84,13 @@ inline NormPlan norm_plan(int B, int N, int C, int groups, bool per_token, bool 
         p.cols = p.wide ? 1 : std::min(groups, slots);              // groups of a workgroup
         p.rows = p.wide ? 1 : slots / p.cols;                       // tokens of a workgroup at a time
         p.blocks = (groups + p.cols - 1) / p.cols;
+        // four workgroups a unit, each with its own sums for the weights (16384 tokens of 16 x 128, bf16: forward and backward 29 and
+        // 42 us and 6 for the sums; with two 35, 49 and 4, with eight 30, 51 and 11)
         const long long tokens = (static_cast<long long>(B) * N + p.rows - 1) / p.rows;
         p.grid = static_cast<int>(std::min<long long>(tokens, std::max(1LL, 4LL * device_cu_count() / p.blocks)));
-        p.bwd_bytes = static_cast<size_t>(p.grid) * C * 2 * sizeof(float);
+        p.bytes = back ? static_cast<size_t>(p.grid) * C * 2 * sizeof(float) : 0;
         return p;
     }
-    const long long units = B;
-    const int tokens = N;
     p.parts = 1;
     p.V = align;
     while (C % p.V != 0) p.V /= 2;
@@ -104,10 +112,17 @@ inline NormPlan norm_plan(int B, int N, int C, int groups, bool per_token, bool 
         }
     }
     p.rows = kNormThreads / p.cols;
-    const long long want = 2LL * device_cu_count(), wide = units * p.blocks;
-    p.slabs = static_cast<int>(std::max(1LL, std::min<long long>((want + wide - 1) / wide, (tokens + 4 * p.rows - 1) / (4 * p.rows))));
-    p.fwd_bytes = static_cast<size_t>(units) * p.slabs * groups * p.parts * 2 * sizeof(float);
-    p.bwd_bytes = static_cast<size_t>(units) * p.slabs * C * 2 * sizeof(float);
+    // one workgroup a unit: half as many threads in twice as many, or two a unit, read more of the slabs' sums in all (2 x 19200 tokens
+    // of 256 channels, bf16: the second launch 16 us, 22 and 30). Where batch elements and blocks leave slabs uneven over
+    // the units, four times as many.
+    const long long want = device_cu_count(), wide = static_cast<long long>(B) * p.blocks;
+    const long long many = want / wide >= 8 ? want / wide : (4 * want + wide - 1) / wide;
+    const long long slabs = std::max(1LL, std::min<long long>(many, (N + 4 * p.rows - 1) / (4 * p.rows)));
+    p.slab = static_cast<int>((N + slabs - 1) / slabs);
+    p.slabs = (N + p.slab - 1) / p.slab;
+    const size_t sums = static_cast<size_t>(B) * p.slabs;
+    p.channel_floats = back ? sums * C * 2 : 0;
+    p.bytes = (p.channel_floats + sums * groups * p.parts * 2) * sizeof(float);
     return p;
 }
 

@@ -10,30 +10,42 @@ namespace {
 
 constexpr int kT = kNormThreads;
 
-// V elements at element e.
+
+// V elements as they lie in memory, and as numbers.
+template <typename T, int V>
+struct alignas(V * sizeof(T)) Piece {
+    T v[V];
+    __device__ __forceinline__ void unpack(float (&x)[V]) const
+    {
+        if constexpr (V * sizeof(T) == 16) {
+            Storage<T>::unpack(__builtin_bit_cast(uint4, *this), x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[i] = Storage<T>::load1(&v[i], 0);
+        }
+    }
+};
+template <typename T, int V>
+__device__ __forceinline__ Piece<T, V> piece_at(const void* base, long long e)
+{
+    return *reinterpret_cast<const Piece<T, V>*>(static_cast<const T*>(base) + e);
+}
 template <typename T, int V>
 __device__ __forceinline__ void load_piece(const void* base, long long e, float (&x)[V])
 {
-    if constexpr (V * sizeof(T) == 16) {
-        Storage<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(base) + e), x);
-    } else {
-        struct alignas(V * sizeof(T)) Raw { T v[V]; };
-        const Raw r = *reinterpret_cast<const Raw*>(static_cast<const T*>(base) + e);
-#pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = Storage<T>::load1(&r.v[i], 0);
-    }
+    piece_at<T, V>(base, e).unpack(x);
 }
 template <typename T, int V>
 __device__ __forceinline__ void store_piece(void* base, long long e, const float (&x)[V])
 {
     if constexpr (V * sizeof(T) == 16) {
-        *reinterpret_cast<uint4*>(static_cast<T*>(base) + e) = Storage<T>::pack(x);
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, Storage<T>::pack(x)), reinterpret_cast<u32x4*>(static_cast<T*>(base) + e));
     } else {
-        struct alignas(V * sizeof(T)) Raw { T v[V]; };
-        Raw r;
+        Piece<T, V> r;
 #pragma unroll
         for (int i = 0; i < V; ++i) Storage<T>::store1(&r.v[i], 0, x[i]);
-        *reinterpret_cast<Raw*>(static_cast<T*>(base) + e) = r;
+        *reinterpret_cast<Piece<T, V>*>(static_cast<T*>(base) + e) = r;
     }
 }
 
@@ -48,23 +60,43 @@ __device__ __forceinline__ void store_param(void* p, bool is_bf16, int c, float 
     else Storage<float>::store1(p, c, x);
 }
 
-__device__ __forceinline__ float sigmoid(float z) { return 1.f / (1.f + __expf(-z)); }
-__device__ __forceinline__ float activate(float z, int act)
-{
-    if (act == QTA_ACT_SILU) return z * sigmoid(z);
-    if (act == QTA_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    if (act == QTA_ACT_RELU) return z > 0.f ? z : z == z ? 0.f : z;
-    return z;
-}
-__device__ __forceinline__ float slope(float z, int act)
+__device__ __forceinline__ float sigmoid(float z) { return fast_rcp(1.f + __expf(-z)); }
+// n values' activations in place, and their slopes. (The choice stands outside the loop: a branch for every value would part the
+// instructions of different values.)
+template <int N>
+__device__ __forceinline__ void activate(float (&z)[N], int act)
 {
     if (act == QTA_ACT_SILU) {
-        const float s = sigmoid(z);
-        return s * (1.f + z * (1.f - s));
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] *= sigmoid(z[i]);
+    } else if (act == QTA_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = 0.5f * z[i] * (1.f + erff(z[i] * 0.70710678118654752f));
+    } else if (act == QTA_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = z[i] > 0.f ? z[i] : z[i] == z[i] ? 0.f : z[i];
     }
-    if (act == QTA_ACT_GELU) return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
-    if (act == QTA_ACT_RELU) return z > 0.f ? 1.f : z == z ? 0.f : z;
-    return 1.f;
+}
+template <int N>
+__device__ __forceinline__ void slope(float (&z)[N], int act)
+{
+    if (act == QTA_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float s = sigmoid(z[i]);
+            z[i] = s * (1.f + z[i] * (1.f - s));
+        }
+    } else if (act == QTA_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            z[i] = 0.5f * (1.f + erff(z[i] * 0.70710678118654752f)) + z[i] * __expf(-0.5f * z[i] * z[i]) * 0.39894228040143268f;
+    } else if (act == QTA_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = z[i] > 0.f ? 1.f : z[i] == z[i] ? 0.f : z[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = 1.f;
+    }
 }
 
 // Sum over `lanes` (a power of two up to 64) neighbouring lanes, in all of them.
@@ -95,7 +127,7 @@ __global__ __launch_bounds__(256) void norm_tokens_kernel(NormArgs a)
     const int lane = threadIdx.x & (a.lanes - 1), slot = threadIdx.x / a.lanes;
     const int block = blockIdx.y, row = slot / a.cols, g = block * a.cols + slot - row * a.cols;
     const bool mine = row < a.rows && g < a.groups;
-    const long long rows = static_cast<long long>(a.B) * a.N;
+    const int rows = a.B * a.N;
     const float inv = 1.f / a.P;
     float w[K][V], bias[K][V], dw[K][V] = {}, db[K][V] = {};
     bool on[K];
@@ -111,25 +143,36 @@ __global__ __launch_bounds__(256) void norm_tokens_kernel(NormArgs a)
             bias[k][i] = on[k] ? param(a.bias, a.param_bf16, at[k] + i, 0.f) : 0.f;
         }
     }
-    for (long long r0 = static_cast<long long>(blockIdx.x) * a.rows; r0 < rows; r0 += static_cast<long long>(gridDim.x) * a.rows) {
-        const long long t = r0 + row;
-        const bool here = mine && t < rows;
-        const int tt = static_cast<int>(here ? t : r0), b = fast_div(tt, a.div_N);
-        const long long from = b * a.xb + (tt - b * a.N) * a.xn, to = static_cast<long long>(tt) * a.C;
+    // (the next token's loads are in flight while one is worked on; rows behind the last are read as that)
+    Piece<T, V> px[K], py[K];
+    auto fetch = [&](int r0) {
+        const int t = min(r0 + (mine ? row : 0), rows - 1), b = fast_div(t, a.div_N);
+        const long long from = b * a.xb + (t - b * a.N) * a.xn, to = static_cast<long long>(t) * a.C;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            px[k] = piece_at<T, V>(a.x, from + at[k]);
+            if constexpr (BACK) py[k] = piece_at<T, V>(a.dy, to + at[k]);
+        }
+    };
+    const int step = gridDim.x * a.rows;
+    fetch(blockIdx.x * a.rows);
+    for (int r0 = blockIdx.x * a.rows; r0 < rows; r0 += step) {
+        const bool here = mine && r0 + row < rows;
+        const long long to = static_cast<long long>(r0 + row) * a.C;
         float x[K][V], dy[K][V];
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (on[k] && here) {
-                load_piece<T, V>(a.x, from + at[k], x[k]);
-                if constexpr (BACK) load_piece<T, V>(a.dy, to + at[k], dy[k]);
-            } else {
+            px[k].unpack(x[k]);
+            if constexpr (BACK) py[k].unpack(dy[k]);
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[k][i] = dy[k][i] = 0.f;
+            for (int i = 0; i < V; ++i) {
+                x[k][i] = on[k] && here ? x[k][i] : 0.f;
+                if constexpr (BACK) dy[k][i] = on[k] && here ? dy[k][i] : 0.f;
+                sum += x[k][i];
             }
-#pragma unroll
-            for (int i = 0; i < V; ++i) sum += x[k][i];
         }
+        if (r0 + step < rows) fetch(r0 + step);
         const float mean = team_sum(sum, a.lanes) * inv;
         float sq = 0.f;
 #pragma unroll
@@ -146,23 +189,31 @@ __global__ __launch_bounds__(256) void norm_tokens_kernel(NormArgs a)
             for (int k = 0; k < K; ++k) {
                 if (!on[k] || !here) continue;
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[k][i] = activate(x[k][i] * r * w[k][i] + bias[k][i], a.act);
+                for (int i = 0; i < V; ++i) x[k][i] = x[k][i] * r * w[k][i] + bias[k][i];
+                activate(x[k], a.act);
                 store_piece<T, V>(a.y, to + at[k], x[k]);
             }
         } else {
             float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-            for (int k = 0; k < K; ++k)
+            for (int k = 0; k < K; ++k) {
+                float z[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     x[k][i] *= r;
-                    const float dz = dy[k][i] * slope(x[k][i] * w[k][i] + bias[k][i], a.act);
+                    z[i] = x[k][i] * w[k][i] + bias[k][i];
+                }
+                slope(z, a.act);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float dz = dy[k][i] * z[i];
                     db[k][i] += dz;
                     dw[k][i] += dz * x[k][i];
                     dy[k][i] = dz * w[k][i];
                     s0 += dy[k][i];
                     s1 += dy[k][i] * x[k][i];
                 }
+            }
             s0 = team_sum(s0, a.lanes) * inv;
             s1 = team_sum(s1, a.lanes) * inv;
 #pragma unroll
@@ -246,10 +297,14 @@ __global__ __launch_bounds__(256) void norm_wide_kernel(NormArgs a)
             for (int c = c0; c < c1; c += 256 * V) {
                 load_piece<T, V>(a.x, from + c, x);
                 load_piece<T, V>(a.dy, to + c, dy);
+                float z[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    z[i] = (x[i] - mean) * r * param(a.weight, a.param_bf16, c + i, 1.f) + param(a.bias, a.param_bf16, c + i, 0.f);
+                slope(z, a.act);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float w = param(a.weight, a.param_bf16, c + i, 1.f), n = (x[i] - mean) * r;
-                    const float dz = dy[i] * slope(n * w + param(a.bias, a.param_bf16, c + i, 0.f), a.act);
+                    const float w = param(a.weight, a.param_bf16, c + i, 1.f), n = (x[i] - mean) * r, dz = dy[i] * z[i];
                     s0 += w * dz;
                     s1 += w * dz * n;
                 }
@@ -260,22 +315,25 @@ __global__ __launch_bounds__(256) void norm_wide_kernel(NormArgs a)
         for (int c = c0; c < c1; c += 256 * V) {
             load_piece<T, V>(a.x, from + c, x);
             if constexpr (BACK) load_piece<T, V>(a.dy, to + c, dy);
+            float z[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float w = param(a.weight, a.param_bf16, c + i, 1.f), n = (x[i] - mean) * r;
-                const float z = n * w + param(a.bias, a.param_bf16, c + i, 0.f);
-                if constexpr (BACK) {
-                    const float dz = dy[i] * slope(z, a.act);
+            for (int i = 0; i < V; ++i)
+                z[i] = (x[i] - mean) * r * param(a.weight, a.param_bf16, c + i, 1.f) + param(a.bias, a.param_bf16, c + i, 0.f);
+            if constexpr (BACK) {
+                slope(z, a.act);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float w = param(a.weight, a.param_bf16, c + i, 1.f), n = (x[i] - mean) * r, dz = dy[i] * z[i];
                     if (part) {
                         const float2 o = t == static_cast<int>(blockIdx.x) ? make_float2(0.f, 0.f) : part[c + i];
                         part[c + i] = make_float2(o.x + dz * n, o.y + dz);
                     }
-                    x[i] = r * (w * dz - s0 - n * s1);
-                } else {
-                    x[i] = activate(z, a.act);
+                    z[i] = r * (w * dz - s0 - n * s1);
                 }
+            } else {
+                activate(z, a.act);
             }
-            store_piece<T, V>(BACK ? a.dx : a.y, to + c, x);
+            store_piece<T, V>(BACK ? a.dx : a.y, to + c, z);
         }
     }
 }
@@ -293,10 +351,10 @@ struct NormPlace {
     {
         block = index % a.blocks;
         const int y = index / a.blocks;
-        b = y / a.slabs;
+        b = fast_div(y, a.div_slabs);
         slab = y - b * a.slabs;
-        n0 = static_cast<int>(static_cast<long long>(a.N) * slab / a.slabs);
-        n1 = static_cast<int>(static_cast<long long>(a.N) * (slab + 1) / a.slabs);
+        n0 = slab * a.slab;
+        n1 = min(n0 + a.slab, a.N);
         const int wide = a.cols * V;
         if (a.parts == 1) {
             c0 = block * wide;
@@ -312,35 +370,68 @@ struct NormPlace {
     }
 };
 
+// A thread's tokens of the slab, U at a time, the next ones' loads in flight while these are worked on: before anything else
+// (`first`), then work(n, pieces of x, of dy) for each token.
+template <typename T, int V, int U, bool DY, bool DOWN>
+struct NormStream {
+    const T *x, *dy;
+    long long xn;
+    int C, rows, n, n1, both;
+    __device__ __forceinline__ int token(int i) const { return DOWN ? both - i : i; }
+    Piece<T, V> px[U], py[DY ? U : 1];
+    __device__ __forceinline__ void fetch(int at)
+    {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int m = token(min(at + u * rows, n1 - 1));
+            px[u] = piece_at<T, V>(x, m * xn);
+            if constexpr (DY) py[u] = piece_at<T, V>(dy, static_cast<long long>(m) * C);
+        }
+    }
+    __device__ __forceinline__ NormStream(const NormArgs& a, const NormPlace& at)
+        : x(static_cast<const T*>(a.x) + (at.b * a.xb + at.col)), xn(a.xn), C(a.C), rows(a.rows), n(at.mine ? at.n0 + at.row : at.n1), n1(at.n1), both(at.n0 + at.n1 - 1)
+    {
+        if constexpr (DY) dy = static_cast<const T*>(a.dy) + (static_cast<long long>(at.b) * a.N * a.C + at.col);
+        if (n < n1) fetch(n);
+    }
+    template <typename Work>
+    __device__ __forceinline__ void run(Work work)
+    {
+        for (; n < n1; n += U * rows) {
+            float fx[U][V], fy[DY ? U : 1][V];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                px[u].unpack(fx[u]);
+                if constexpr (DY) py[u].unpack(fy[u]);
+            }
+            if (n + U * rows < n1) fetch(n + U * rows);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (n + u * rows >= n1) break;
+                work(token(n + u * rows), fx[u], fy[DY ? u : 0]);
+            }
+        }
+    }
+};
+
 // Statistics of a slab: per thread and channel a running mean and sum of squared distances from it; then over the channels and rows of a
 // group through LDS, first the mean, then the distances from that.
 template <typename T, int V>
 __global__ __launch_bounds__(kT) void norm_stats_kernel(NormArgs a)
 {
-    constexpr int U = 4;                                            // tokens whose loads are in flight
     extern __shared__ __align__(16) float2 box[];                   // [rows][entries of a row]: mean, squares
     const NormPlace at(a, xcd_remap(blockIdx.x, gridDim.x), V);
     float mean[V] = {}, sq[V] = {};
     int count = 0;
-    if (at.mine) {
-        const long long from = at.b * a.xb + at.col;
-        for (int n = at.n0 + at.row; n < at.n1; n += U * a.rows) {
-            float x[U][V];
+    NormStream<T, V, 4, false, false>(a, at).run([&](int, const float (&x)[V], const float (&)[V]) {
+        const float inv = fast_rcp(static_cast<float>(++count));
 #pragma unroll
-            for (int u = 0; u < U; ++u) load_piece<T, V>(a.x, from + min(n + u * a.rows, at.n1 - 1) * a.xn, x[u]);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (n + u * a.rows >= at.n1) break;
-                const float inv = fast_rcp(static_cast<float>(++count));
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = x[u][i] - mean[i];
-                    mean[i] += d * inv;
-                    sq[i] += d * (x[u][i] - mean[i]);
-                }
-            }
+        for (int i = 0; i < V; ++i) {
+            const float d = x[i] - mean[i];
+            mean[i] += d * inv;
+            sq[i] += d * (x[i] - mean[i]);
         }
-    }
+    });
     // a thread's channels of one group become one entry
     const bool whole = a.P % V == 0;
     const int each = whole ? 1 : V, wide = a.cols * each, of_group = whole ? min(a.P, at.c1 - at.c0) / V : a.P;
@@ -365,21 +456,35 @@ __global__ __launch_bounds__(kT) void norm_stats_kernel(NormArgs a)
     const float per = static_cast<float>(whole ? V : 1);
     for (int g = threadIdx.x / lanes; g < groups; g += kT / lanes) {
         float m = 0.f, s = 0.f;
-        for (int r = 0; r < a.rows; ++r) {
-            const float n = static_cast<float>((tokens - r + a.rows - 1) / a.rows);
-            for (int e = lane; e < of_group; e += lanes) m += n * box[r * wide + g * of_group + e].x;
-        }
-        m = team_sum(m, lanes) / (static_cast<float>(tokens) * of_group);
-        for (int r = 0; r < a.rows; ++r) {
-            const float n = static_cast<float>((tokens - r + a.rows - 1) / a.rows) * per;
-            for (int e = lane; e < of_group; e += lanes) {
-                const float2 v = box[r * wide + g * of_group + e];
-                s += v.y + n * (v.x - m) * (v.x - m);
+        // (a part of a group is wider than half a workgroup: one row)
+        auto each = [&](auto add) {
+#pragma unroll 4
+            for (int i = lane; i < a.rows * of_group; i += lanes) {
+                const int r = a.rows == 1 ? 0 : fast_div(i, a.div_entry);
+                add(box[r * (wide - of_group) + g * of_group + i], static_cast<float>(fast_div(tokens - r + a.rows - 1, a.div_rows)));
             }
-        }
+        };
+        each([&](float2 v, float n) { m += n * v.x; });
+        m = team_sum(m, lanes) / (static_cast<float>(tokens) * of_group);
+        each([&](float2 v, float n) { s += v.y + n * per * (v.x - m) * (v.x - m); });
         s = team_sum(s, lanes);
         const int entry = a.parts == 1 ? at.c0 / a.P + g : at.block;
         if (lane == 0) reinterpret_cast<float2*>(a.part)[(static_cast<long long>(at.b) * a.slabs + at.slab) * a.entries + entry] = make_float2(m, s);
+    }
+}
+
+// What the slabs (and a group's parts) left for one group, spread over a team's lanes: add(entry, slab, part).
+template <typename Add>
+__device__ __forceinline__ void each_entry(const NormArgs& a, const float2* from, int lane, int lanes, Add add)
+{
+    if (a.parts == 1) {
+#pragma unroll 8
+        for (int s = lane; s < a.slabs; s += lanes) add(from[s * a.entries], s, 0);
+    } else {
+        for (int i = lane; i < a.slabs * a.parts; i += lanes) {
+            const int s = i / a.parts, p = i - s * a.parts;
+            add(from[s * a.entries + p], s, p);
+        }
     }
 }
 
@@ -387,27 +492,27 @@ __global__ __launch_bounds__(kT) void norm_stats_kernel(NormArgs a)
 __device__ __forceinline__ void join_stats(const NormArgs& a, const NormPlace& at, int V, float2* box)
 {
     const int g0 = at.c0 / a.P, groups = a.parts == 1 ? (at.c1 - at.c0) / a.P : 1, lanes = team_lanes(groups);
-    const int lane = threadIdx.x & (lanes - 1), n = a.slabs * a.parts;
+    const int lane = threadIdx.x & (lanes - 1);
     const float2* const part = reinterpret_cast<const float2*>(a.part) + static_cast<long long>(at.b) * a.slabs * a.entries;
     const float inv = 1.f / (static_cast<float>(a.N) * a.P);
-    // values of part p of slab s
-    auto values = [&](int s, int p) {
-        const int tokens = static_cast<int>(static_cast<long long>(a.N) * (s + 1) / a.slabs) - static_cast<int>(static_cast<long long>(a.N) * s / a.slabs);
-        return static_cast<float>(tokens) * (a.parts == 1 ? a.P : min(a.cols * V, a.P - p * a.cols * V));
-    };
     for (int g = threadIdx.x / lanes; g < groups; g += kT / lanes) {
+        const float2* const from = part + (g0 + g) * a.parts;
+        auto values = [&](int slab, int p) {
+            return static_cast<float>(min(a.slab, a.N - slab * a.slab)) * (a.parts == 1 ? a.P : min(a.cols * V, a.P - p * a.cols * V));
+        };
+        // one pass, with distances from the first slab's mean: at most the number of slabs times a rounding's error, relative to
+        // the variance, where that slab alone differs from the others
+        const float base = from[0].x;
         float m = 0.f, s = 0.f;
-        for (int i = lane; i < n; i += lanes) {
-            const int slab = i / a.parts, p = i - slab * a.parts;
-            m += values(slab, p) * part[slab * a.entries + (g0 + g) * a.parts + p].x;
-        }
+        each_entry(a, from, lane, lanes, [&](float2 v, int slab, int p) {
+            const float d = v.x - base, n = values(slab, p);
+            m += n * d;
+            s += v.y + n * d * d;
+        });
         m = team_sum(m, lanes) * inv;
-        for (int i = lane; i < n; i += lanes) {
-            const int slab = i / a.parts, p = i - slab * a.parts;
-            const float2 v = part[slab * a.entries + (g0 + g) * a.parts + p];
-            s += v.y + values(slab, p) * (v.x - m) * (v.x - m);
-        }
-        const float r = 1.f / sqrtf(team_sum(s, lanes) * inv + a.eps);
+        s = fmaxf(team_sum(s, lanes) * inv - m * m, 0.f);
+        m += base;
+        const float r = 1.f / sqrtf(s + a.eps);
         if (lane == 0) {
             box[g] = make_float2(m, r);
             if (a.stats && at.slab == 0 && (a.parts == 1 || at.block % a.parts == 0))
@@ -420,45 +525,45 @@ __device__ __forceinline__ void join_stats(const NormArgs& a, const NormPlace& a
 template <typename T, int V>
 __global__ __launch_bounds__(kT) void norm_apply_kernel(NormArgs a)
 {
-    constexpr int U = 4;
     extern __shared__ __align__(16) float2 box[];
     const NormPlace at(a, xcd_remap(blockIdx.x, gridDim.x), V);
+    NormStream<T, V, 4, false, true> stream(a, at);
+    float f[V], bias[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        f[i] = at.mine ? param(a.weight, a.param_bf16, at.col + i, 1.f) : 0.f;
+        bias[i] = at.mine ? param(a.bias, a.param_bf16, at.col + i, 0.f) : 0.f;
+    }
     join_stats(a, at, V, box);
     if (!at.mine) return;
-    float mean[V], f[V], bias[V];
+    // (x r - mean r: as far off as the mean's own rounding makes x - mean)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const float2 s = box[(at.col + i) / a.P - at.c0 / a.P];
-        mean[i] = s.x;
-        f[i] = s.y * param(a.weight, a.param_bf16, at.col + i, 1.f);
-        bias[i] = param(a.bias, a.param_bf16, at.col + i, 0.f);
+        f[i] *= s.y;
+        bias[i] -= s.x * f[i];
     }
-    const long long from = at.b * a.xb + at.col, to = static_cast<long long>(at.b) * a.N * a.C + at.col;
-    for (int n = at.n0 + at.row; n < at.n1; n += U * a.rows) {
-        float x[U][V];
+    const long long to = static_cast<long long>(at.b) * a.N * a.C + at.col;
+    stream.run([&](int n, const float (&x)[V], const float (&)[V]) {
+        float z[V];
 #pragma unroll
-        for (int u = 0; u < U; ++u) load_piece<T, V>(a.x, from + min(n + u * a.rows, at.n1 - 1) * a.xn, x[u]);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (n + u * a.rows >= at.n1) break;
-#pragma unroll
-            for (int i = 0; i < V; ++i) x[u][i] = activate((x[u][i] - mean[i]) * f[i] + bias[i], a.act);
-            store_piece<T, V>(a.y, to + static_cast<long long>(n + u * a.rows) * a.C, x[u]);
-        }
-    }
+        for (int i = 0; i < V; ++i) z[i] = x[i] * f[i] + bias[i];
+        activate(z, a.act);
+        store_piece<T, V>(a.y, to + static_cast<long long>(n) * a.C, z);
+    });
 }
 
 // A thread's channels in the backward.
 template <int V>
 struct NormChannels {
-    float mean[V], r[V], w[V], bias[V];
+    float r[V], shift[V], w[V], bias[V];        // n = x r + shift
     __device__ __forceinline__ NormChannels(const NormArgs& a, const NormPlace& at)
     {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const float2 s = reinterpret_cast<const float2*>(a.stats)[static_cast<long long>(at.b) * a.groups + (at.mine ? (at.col + i) / a.P : 0)];
-            mean[i] = s.x;
             r[i] = s.y;
+            shift[i] = -s.x * s.y;
             w[i] = param(a.weight, a.param_bf16, at.mine ? at.col + i : 0, 1.f);
             bias[i] = param(a.bias, a.param_bf16, at.mine ? at.col + i : 0, 0.f);
         }
@@ -469,76 +574,100 @@ struct NormChannels {
 template <typename T, int V>
 __global__ __launch_bounds__(kT) void norm_sums_kernel(NormArgs a)
 {
-    constexpr int U = 2;
     extern __shared__ __align__(16) float2 box[];                   // [V][kT]
     const NormPlace at(a, xcd_remap(blockIdx.x, gridDim.x), V);
+    NormStream<T, V, 2, true, false> stream(a, at);
     float s1[V] = {}, s0[V] = {};
-    if (at.mine) {
-        const NormChannels<V> ch(a, at);
-        const long long from = at.b * a.xb + at.col, up = static_cast<long long>(at.b) * a.N * a.C + at.col;
-        for (int n = at.n0 + at.row; n < at.n1; n += U * a.rows) {
-            float x[U][V], dy[U][V];
+    const NormChannels<V> ch(a, at);
+    stream.run([&](int, const float (&x)[V], const float (&dy)[V]) {
+        float n[V], z[V];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int m = min(n + u * a.rows, at.n1 - 1);
-                load_piece<T, V>(a.x, from + m * a.xn, x[u]);
-                load_piece<T, V>(a.dy, up + static_cast<long long>(m) * a.C, dy[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (n + u * a.rows >= at.n1) break;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float v = (x[u][i] - ch.mean[i]) * ch.r[i], dz = dy[u][i] * slope(v * ch.w[i] + ch.bias[i], a.act);
-                    s1[i] += dz * v;
-                    s0[i] += dz;
-                }
-            }
+        for (int i = 0; i < V; ++i) {
+            n[i] = x[i] * ch.r[i] + ch.shift[i];
+            z[i] = n[i] * ch.w[i] + ch.bias[i];
         }
-    }
+        slope(z, a.act);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float dz = dy[i] * z[i];
+            s1[i] += dz * n[i];
+            s0[i] += dz;
+        }
+    });
 #pragma unroll
     for (int i = 0; i < V; ++i) box[i * kT + threadIdx.x] = make_float2(s1[i], s0[i]);
     __syncthreads();
-    float2* const part = reinterpret_cast<float2*>(a.part) + (static_cast<long long>(at.b) * a.slabs + at.slab) * a.C;
-    const int wide = (at.c1 - at.c0);
-    for (int c = threadIdx.x; c < wide; c += kT) {
+    // rows of a channel: a team of lanes each
+    const long long slab = static_cast<long long>(at.b) * a.slabs + at.slab;
+    float2* const part = reinterpret_cast<float2*>(a.part) + slab * a.C;
+    const int wide = at.c1 - at.c0, team = min(team_lanes(wide), a.rows_lanes), of = threadIdx.x & (team - 1);
+    for (int c = threadIdx.x / team; c < wide; c += kT / team) {
         const int col = c / V, i = c - col * V;
-        float2 s = box[i * kT + col];
-        for (int r = 1; r < a.rows; ++r) {
+        float2 s = make_float2(0.f, 0.f);
+#pragma unroll 4
+        for (int r = of; r < a.rows; r += team) {
             const float2 o = box[i * kT + col + r * a.cols];
             s.x += o.x;
             s.y += o.y;
         }
-        part[at.c0 + c] = s;
+        s.x = team_sum(s.x, team);
+        s.y = team_sum(s.y, team);
+        // (a channel's first row is its team's alone to read)
+        if (of == 0) {
+            box[i * kT + col] = s;
+            part[at.c0 + c] = s;
+        }
+    }
+    __syncthreads();
+    const int groups = a.parts == 1 ? wide / a.P : 1, lanes = team_lanes(groups), lane = threadIdx.x & (lanes - 1);
+    const int of_group = a.parts == 1 ? a.P : wide;
+    for (int g = threadIdx.x / lanes; g < groups; g += kT / lanes) {
+        float t1 = 0.f, t0 = 0.f;
+        for (int i = lane; i < of_group; i += lanes) {
+            const int c = g * of_group + i, col = c / V;
+            const float2 o = box[(c - col * V) * kT + col];
+            const float w = param(a.weight, a.param_bf16, at.c0 + c, 1.f);
+            t1 += w * o.x;
+            t0 += w * o.y;
+        }
+        t1 = team_sum(t1, lanes);
+        t0 = team_sum(t0, lanes);
+        const int entry = a.parts == 1 ? at.c0 / a.P + g : at.block;
+        if (lane == 0) reinterpret_cast<float2*>(a.group_part)[slab * a.entries + entry] = make_float2(t1, t0);
     }
 }
 
-// Gradients of the weights: sums of the workgroups' sums, 32 channels a workgroup.
+// Gradients of the weights: sums of the workgroups' sums, 16 channels a workgroup.
 __device__ __forceinline__ void norm_params(const NormArgs& a, int block, int threads, float2* box)
 {
-    const int c = block * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5, slices = threads / 32;
+    const int c = block * 16 + (threadIdx.x & 15), slice = threadIdx.x >> 4, slices = threads / 16;
     const float2* const part = reinterpret_cast<const float2*>(a.part);
     float2 s = make_float2(0.f, 0.f);
     if (c < a.C) {
         const int n0 = static_cast<int>(static_cast<long long>(a.sums) * slice / slices), n1 = static_cast<int>(static_cast<long long>(a.sums) * (slice + 1) / slices);
-        for (int n = n0; n < n1; n += 8) {
-            float2 o[8];
+        for (int n = n0; n < n1; n += 4) {
+            float2 o[4];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) o[u] = part[static_cast<long long>(min(n + u, n1 - 1)) * a.C + c];
+            for (int u = 0; u < 4; ++u) o[u] = part[static_cast<long long>(min(n + u, n1 - 1)) * a.C + c];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < 4; ++u) {
                 if (n + u >= n1) break;
                 s.x += o[u].x;
                 s.y += o[u].y;
             }
         }
     }
-    box[threadIdx.x] = s;
+    s.x += xchg_f32<16>(s.x);
+    s.y += xchg_f32<16>(s.y);
+    s.x += xchg_f32<32>(s.x);
+    s.y += xchg_f32<32>(s.y);
+    if ((threadIdx.x & 63) < 16) box[(threadIdx.x >> 6) * 16 + (threadIdx.x & 15)] = s;
     __syncthreads();
     if (slice == 0 && c < a.C) {
-        for (int i = 1; i < slices; ++i) {
-            s.x += box[i * 32 + threadIdx.x].x;
-            s.y += box[i * 32 + threadIdx.x].y;
+#pragma unroll 4
+        for (int i = 1; i < threads / 64; ++i) {
+            s.x += box[i * 16 + threadIdx.x].x;
+            s.y += box[i * 16 + threadIdx.x].y;
         }
         if (a.dweight) store_param(a.dweight, a.param_bf16, c, s.x);
         if (a.dbias) store_param(a.dbias, a.param_bf16, c, s.y);
@@ -554,32 +683,28 @@ __global__ __launch_bounds__(kT) void norm_params_kernel(NormArgs a)
 template <typename T, int V>
 __global__ __launch_bounds__(kT) void norm_dx_kernel(NormArgs a)
 {
-    constexpr int U = 2;
     extern __shared__ __align__(16) float2 box[];
-    const int own = a.B * a.slabs * a.blocks;
+    const int own = static_cast<int>(a.own);
     if (static_cast<int>(blockIdx.x) >= own) return norm_params(a, blockIdx.x - own, kT, box);
     const NormPlace at(a, xcd_remap(blockIdx.x, own), V);
+    NormStream<T, V, 2, true, true> stream(a, at);
+    const NormChannels<V> ch(a, at);
     const int g0 = at.c0 / a.P, groups = a.parts == 1 ? (at.c1 - at.c0) / a.P : 1, lanes = team_lanes(groups);
     const int lane = threadIdx.x & (lanes - 1);
-    const float2* const part = reinterpret_cast<const float2*>(a.part) + static_cast<long long>(at.b) * a.slabs * a.C;
+    const float2* const part = reinterpret_cast<const float2*>(a.group_part) + static_cast<long long>(at.b) * a.slabs * a.entries;
     const float inv = 1.f / (static_cast<float>(a.N) * a.P);
     for (int g = threadIdx.x / lanes; g < groups; g += kT / lanes) {
         float s1 = 0.f, s0 = 0.f;
-#pragma unroll 4
-        for (int i = lane; i < a.slabs * a.P; i += lanes) {
-            const int slab = fast_div(i, a.div_P), c = (g0 + g) * a.P + i - slab * a.P;
-            const float w = param(a.weight, a.param_bf16, c, 1.f);
-            const float2 o = part[static_cast<long long>(slab) * a.C + c];
-            s1 += w * o.x;
-            s0 += w * o.y;
-        }
+        each_entry(a, part + (g0 + g) * a.parts, lane, lanes, [&](float2 v, int, int) {
+            s1 += v.x;
+            s0 += v.y;
+        });
         s1 = team_sum(s1, lanes) * inv;
         s0 = team_sum(s0, lanes) * inv;
         if (lane == 0) box[g] = make_float2(s1, s0);
     }
     __syncthreads();
     if (!at.mine) return;
-    const NormChannels<V> ch(a, at);
     float s1[V], s0[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -587,26 +712,19 @@ __global__ __launch_bounds__(kT) void norm_dx_kernel(NormArgs a)
         s1[i] = s.x;
         s0[i] = s.y;
     }
-    const long long from = at.b * a.xb + at.col, up = static_cast<long long>(at.b) * a.N * a.C + at.col;
-    for (int n = at.n0 + at.row; n < at.n1; n += U * a.rows) {
-        float x[U][V], dy[U][V];
+    const long long to = static_cast<long long>(at.b) * a.N * a.C + at.col;
+    stream.run([&](int t, const float (&x)[V], const float (&dy)[V]) {
+        float n[V], z[V];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int m = min(n + u * a.rows, at.n1 - 1);
-            load_piece<T, V>(a.x, from + m * a.xn, x[u]);
-            load_piece<T, V>(a.dy, up + static_cast<long long>(m) * a.C, dy[u]);
+        for (int i = 0; i < V; ++i) {
+            n[i] = x[i] * ch.r[i] + ch.shift[i];
+            z[i] = n[i] * ch.w[i] + ch.bias[i];
         }
+        slope(z, a.act);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (n + u * a.rows >= at.n1) break;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float v = (x[u][i] - ch.mean[i]) * ch.r[i], dz = dy[u][i] * slope(v * ch.w[i] + ch.bias[i], a.act);
-                x[u][i] = ch.r[i] * (dz * ch.w[i] - s0[i] - v * s1[i]);
-            }
-            store_piece<T, V>(a.dx, up + static_cast<long long>(n + u * a.rows) * a.C, x[u]);
-        }
-    }
+        for (int i = 0; i < V; ++i) z[i] = ch.r[i] * (dy[i] * z[i] * ch.w[i] - s0[i] - n[i] * s1[i]);
+        store_piece<T, V>(a.dx, to + static_cast<long long>(t) * a.C, z);
+    });
 }
 
 template <typename T, int V, bool BACK>
@@ -625,12 +743,18 @@ hipError_t launch(NormArgs a, const NormPlan& p, bool back, hipStream_t stream)
     a.cols = p.cols;
     a.rows = p.rows;
     a.slabs = p.slabs;
+    a.slab = p.slab;
+    a.div_rows = make_fastdiv(p.rows);
+    a.div_entry = make_fastdiv(a.P % V == 0 ? a.P / V : a.P);
+    a.rows_lanes = 1;
+    while (a.rows_lanes < p.rows && a.rows_lanes < 64) a.rows_lanes *= 2;
+    a.group_part = a.part ? a.part + p.channel_floats : nullptr;
+    a.div_slabs = make_fastdiv(std::max(p.slabs, 1));
     a.blocks = p.blocks;
     a.parts = p.parts;
     a.lanes = p.lanes;
     a.div_N = make_fastdiv(a.N);
-    a.div_P = make_fastdiv(a.P);
-    const unsigned param_blocks = a.dweight || a.dbias ? static_cast<unsigned>((a.C + 31) / 32) : 0;
+    const unsigned param_blocks = a.dweight || a.dbias ? static_cast<unsigned>((a.C + 15) / 16) : 0;
     if (p.tokens) {
         a.sums = p.grid;
         if (!back) launch_tokens<T, V, false>(a, p, stream);
@@ -640,11 +764,11 @@ hipError_t launch(NormArgs a, const NormPlan& p, bool back, hipStream_t stream)
     }
     a.entries = a.groups * p.parts;
     a.sums = a.B * p.slabs;
-    const unsigned grid = static_cast<unsigned>(a.B) * p.slabs * p.blocks;
     const size_t groups_lds = static_cast<size_t>(p.parts == 1 ? std::max(1, std::min(a.groups, p.cols * V / a.P)) : 1) * sizeof(float2);
+    const size_t entries_lds = static_cast<size_t>(p.rows) * p.cols * (a.P % V == 0 ? 1 : V) * sizeof(float2);
+    const unsigned grid = a.own = static_cast<unsigned>(a.B) * p.slabs * p.blocks;
     if (!back) {
-        const int each = a.P % V == 0 ? 1 : V;
-        hipLaunchKernelGGL((norm_stats_kernel<T, V>), dim3(grid), dim3(kT), static_cast<size_t>(p.rows) * p.cols * each * sizeof(float2), stream, a);
+        hipLaunchKernelGGL((norm_stats_kernel<T, V>), dim3(grid), dim3(kT), entries_lds, stream, a);
         hipLaunchKernelGGL((norm_apply_kernel<T, V>), dim3(grid), dim3(kT), groups_lds, stream, a);
     } else {
         hipLaunchKernelGGL((norm_sums_kernel<T, V>), dim3(grid), dim3(kT), static_cast<size_t>(kT) * V * sizeof(float2), stream, a);

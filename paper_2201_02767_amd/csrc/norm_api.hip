@@ -28,9 +28,9 @@ qta_status check_norm(const qta_group_norm_args* a, bool shapes_only)
 }
 
 bool use_bf16(const qta_group_norm_args* a) { return a->dtype == QTA_BF16; }
-NormPlan plan(const qta_group_norm_args* a, int align)
+NormPlan plan(const qta_group_norm_args* a, int align, bool back)
 {
-    return norm_plan(a->B, a->N, a->C, a->groups, a->per_token != 0, use_bf16(a), align);
+    return norm_plan(a->B, a->N, a->C, a->groups, a->per_token != 0, use_bf16(a), align, back);
 }
 // Elements of the widest access that all addresses and strides allow.
 int widest(const qta_group_norm_args* a, const void* p, const void* q, const void* r)
@@ -49,18 +49,18 @@ int widest(const qta_group_norm_args* a, const void* p, const void* q, const voi
 size_t most_bytes(const qta_group_norm_args* a, bool back)
 {
     size_t n = kAlign;
-    for (int v = use_bf16(a) ? 8 : 4; v >= 1; v /= 2) n = std::max(n, back ? plan(a, v).bwd_bytes : plan(a, v).fwd_bytes);
+    for (int v = use_bf16(a) ? 8 : 4; v >= 1; v /= 2) n = std::max(n, plan(a, v, back).bytes);
     return n;
 }
 bool fits(const qta_group_norm_args* a, const NormPlan& p)
 {
     if (p.tokens) return p.blocks <= 65535;
-    return static_cast<long long>(a->B) * p.slabs * p.blocks + a->C / 32 + 1 < (1LL << 32) / kNormThreads;
+    return static_cast<long long>(a->B) * p.slabs * p.blocks + a->C / 16 + 1 < (1LL << 32) / kNormThreads;
 }
-bool all_fit(const qta_group_norm_args* a)
+bool all_fit(const qta_group_norm_args* a, bool back)
 {
     for (int v = use_bf16(a) ? 8 : 4; v >= 1; v /= 2)
-        if (!fits(a, plan(a, v))) return false;
+        if (!fits(a, plan(a, v, back))) return false;
     return true;
 }
 
@@ -89,7 +89,7 @@ extern "C" {
 
 size_t qta_group_norm_workspace_bytes(const qta_group_norm_args* args)
 {
-    return check_norm(args, true) == QTA_OK && all_fit(args) ? most_bytes(args, false) : 0;
+    return check_norm(args, true) == QTA_OK && all_fit(args, false) ? most_bytes(args, false) : 0;
 }
 
 qta_status qta_group_norm(const qta_group_norm_args* args, void* y, float* stats, void* workspace, size_t workspace_bytes, void* stream)
@@ -97,10 +97,10 @@ qta_status qta_group_norm(const qta_group_norm_args* args, void* y, float* stats
     const qta_status st = check_norm(args, false);
     if (st != QTA_OK) return st;
     if (!y || y == args->x || !aligned(y, use_bf16(args) ? 2 : 4) || !aligned(stats, 8)) return QTA_ERR_INVALID;
-    if (!all_fit(args)) return QTA_ERR_UNSUPPORTED;
-    const NormPlan p = plan(args, widest(args, y, nullptr, nullptr));
+    if (!all_fit(args, false)) return QTA_ERR_UNSUPPORTED;
+    const NormPlan p = plan(args, widest(args, y, nullptr, nullptr), false);
     if (!p.tokens) {
-        if (workspace_bytes < p.fwd_bytes) return QTA_ERR_WORKSPACE;
+        if (workspace_bytes < p.bytes) return QTA_ERR_WORKSPACE;
         if (!workspace || !aligned(workspace, kAlign)) return QTA_ERR_INVALID;
     }
     NormArgs a = make_args(args);
@@ -112,7 +112,7 @@ qta_status qta_group_norm(const qta_group_norm_args* args, void* y, float* stats
 
 size_t qta_group_norm_backward_workspace_bytes(const qta_group_norm_args* args)
 {
-    return check_norm(args, true) == QTA_OK && all_fit(args) ? most_bytes(args, true) : 0;
+    return check_norm(args, true) == QTA_OK && all_fit(args, true) ? most_bytes(args, true) : 0;
 }
 
 qta_status qta_group_norm_backward(const qta_group_norm_args* args, const float* stats, const void* dy, void* dx, void* dweight, void* dbias,
@@ -123,11 +123,11 @@ qta_status qta_group_norm_backward(const qta_group_norm_args* args, const float*
     const unsigned size = use_bf16(args) ? 2 : 4, psize = args->param_dtype == QTA_BF16 ? 2 : 4;
     if (!dy || !dx || dx == args->x || dx == dy || !aligned(dy, size) || !aligned(dx, size)) return QTA_ERR_INVALID;
     if (!aligned(dweight, psize) || !aligned(dbias, psize)) return QTA_ERR_INVALID;
-    if (!all_fit(args)) return QTA_ERR_UNSUPPORTED;
-    const NormPlan p = plan(args, widest(args, dy, dx, nullptr));
+    if (!all_fit(args, true)) return QTA_ERR_UNSUPPORTED;
+    const NormPlan p = plan(args, widest(args, dy, dx, nullptr), true);
     if (!args->per_token && (!stats || !aligned(stats, 8))) return QTA_ERR_INVALID;
     if (!p.tokens || dweight || dbias) {
-        if (workspace_bytes < p.bwd_bytes) return QTA_ERR_WORKSPACE;
+        if (workspace_bytes < p.bytes) return QTA_ERR_WORKSPACE;
         if (!workspace || !aligned(workspace, kAlign)) return QTA_ERR_INVALID;
     }
     NormArgs a = make_args(args);
