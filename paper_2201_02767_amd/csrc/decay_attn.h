@@ -38,6 +38,7 @@ struct DecayArgs {
     const float* log_decay;
     const int32_t* lens;
     float scale;
+    bool exact;                 // the states are results themselves
     float* part;                // fp32 [roles][B][heads][segs][DK][DV]: what each segment adds to the state, then the states before them
 };
 
@@ -68,7 +69,21 @@ struct DecayStepArgs {
 constexpr int kDecayStepTokens = 16;
 
 // Tokens of a chunk: as many as LDS holds twice.
-constexpr int decay_chunk(bool bf16_inputs) { return bf16_inputs ? 64 : 32; }
+#ifndef DECAY_C
+#define DECAY_C 32
+#endif
+constexpr int decay_chunk(bool bf16_inputs) { return bf16_inputs ? DECAY_C : 32; }
+#ifndef DECAY_D
+#define DECAY_D 4
+#endif
+// Chunks in LDS at a time: up to four, two where two workgroups a unit would not fit otherwise.
+constexpr int decay_depth(int bytes) { return 4 * bytes <= (76 << 10) && DECAY_D >= 4 ? 4 : 3 * bytes <= (144 << 10) && DECAY_D >= 3 ? 3 : 2; }
+#ifndef DECAY_W
+#define DECAY_W 4LL
+#endif
+#ifndef DECAY_LB
+#define DECAY_LB 2
+#endif
 
 // Segments of a call.
 struct DecaySegments {
@@ -77,7 +92,7 @@ struct DecaySegments {
 inline DecaySegments decay_segments(int B, int heads, int N, int roles, bool bf16_inputs)
 {
     const long long chunk = decay_chunk(bf16_inputs), rows = static_cast<long long>(B) * heads * roles;
-    const long long want = 4LL * device_cu_count();
+    const long long want = DECAY_W * device_cu_count();
     const long long most = (N + 4 * chunk - 1) / (4 * chunk);
     const long long segs = std::max(1LL, std::min(most, (want + rows - 1) / rows));
     const long long seg = ((N + segs - 1) / segs + chunk - 1) / chunk * chunk;

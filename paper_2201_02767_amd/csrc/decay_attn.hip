@@ -58,6 +58,23 @@ __device__ __forceinline__ void unpack_frag(const Frag<bf16>& f, float* x)
     }
 }
 
+// A buffer descriptor of a map from `base` (wave-uniform) on: raw bytes, offsets below 2^31.
+__device__ __forceinline__ u32x4_t map_words(const unsigned char* base)
+{
+    const uint64_t p = reinterpret_cast<uint64_t>(base);
+    const int lo = __builtin_amdgcn_readfirstlane(static_cast<int>(p)), hi = __builtin_amdgcn_readfirstlane(static_cast<int>(p >> 32));
+    return u32x4_t{static_cast<uint32_t>(lo), static_cast<uint32_t>(hi) & 0xFFFFu, 0x7FFFFFFFu, 0x00020000u};
+}
+
+// 16 bytes a lane from the map to LDS, lane i's at byte dst + 16 i. In assembly, which has no register of a lane's to write: of
+// the builtin the compiler waits for every load before the next transposed read from LDS, which here are of chunks that landed long before
+// (that wait in the middle of a chunk: 200 us for 152 below). wait for them with s_waitcnt vmcnt.
+__device__ __forceinline__ void load_lds16_untracked(const u32x4_t& map, uint32_t off, uint32_t dst)
+{
+    // (nothing else here uses m0; five wait states between a lane operation that wrote the descriptor and the load, one behind m0)
+    asm volatile("s_nop 4\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(map), "s"(dst) : "memory");
+}
+
 // log2 of a head's decay, so large at most that products with token counts stay numbers.
 __device__ __forceinline__ float decay_log2(const float* log_decay, int h)
 {
@@ -66,15 +83,17 @@ __device__ __forceinline__ float decay_log2(const float* log_decay, int h)
 }
 __device__ __forceinline__ int decay_length(const int32_t* lens, int b, int N) { return lens ? min(max(lens[b], 0), N) : N; }
 
+// EXACT: what is added to the state keeps 24 bits (bf16: three terms of the weighted values), for a state that the call returns; 16 bits
+// (two) do where the state only makes results of 8.
 // STATES: only what each segment adds to the state, to a.part. Otherwise the results, from the states before each segment.
-template <typename T, int DK, int DV, int C, bool STATES>
-__global__ __launch_bounds__(2 * DV) void decay_chunk_kernel(DecayArgs a)
+template <typename T, int DK, int DV, int C, bool STATES, bool EXACT>
+__global__ __launch_bounds__(2 * DV, DK <= 64 ? DECAY_LB : 2) void decay_chunk_kernel(DecayArgs a)
 {
     using KT = Tile<T, DK>;
     using VT = Tile<T, DV>;
     constexpr int ES = sizeof(T), W = DV / 32, A = DK / 32, TT = C / 32;
     constexpr int kQ = STATES ? 0 : KT::bytes(C), kK = KT::bytes(C), kStage = kQ + kK + VT::bytes(C);
-    constexpr int PT = ES == 2 ? 2 : 1, ST = ES == 2 ? 3 : 1;       // terms of scores and states as operands, of what states get
+    constexpr int PT = ES == 2 ? 2 : 1, ST = ES == 2 ? (EXACT ? 3 : 2) : 1;      // terms of scores and states as operands, of what states get
     static_assert(TT <= 2, "the products of one or two tiles of tokens");
     extern __shared__ __align__(1024) unsigned char lds_raw[];
     lds_byte* const lds = (lds_byte*)lds_raw;
@@ -117,7 +136,7 @@ __global__ __launch_bounds__(2 * DV) void decay_chunk_kernel(DecayArgs a)
 
     // weights: of a score (row acc_row(r) of column tok) on the diagonal tile and on the one before it, of the state in each token,
     // and of rows 16 u + (0 .. 15) of a whole chunk in the state
-    float diag[16], before[TT == 2 ? 16 : 1], after = 0.f, come[TT], into[8], into_step[C / 16];
+    float diag[16], before[TT == 2 ? 16 : 1], after = 0.f, come[TT], into[C / 16][8];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         const int apart = tok - acc_row(r, half);
@@ -127,38 +146,69 @@ __global__ __launch_bounds__(2 * DV) void decay_chunk_kernel(DecayArgs a)
     if constexpr (TT == 2) after = exp2f(g2 * tok) * a.scale;
 #pragma unroll
     for (int t = 0; t < TT; ++t) come[t] = exp2f(g2 * (32 * t + tok + e1)) * role.f;
+    float keep;
+    auto weigh = [&](int tokens) {                                  // of a chunk of so many
+        keep = exp2f(g2 * tokens);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) into[i] = exp2f(g2 * (15 - (8 * (i >> 2) + 4 * half + (i & 3)))) * role.u;
+        for (int u = 0; u < C / 16; ++u)
 #pragma unroll
-    for (int u = 0; u < C / 16; ++u) into_step[u] = exp2f(g2 * (C - 15 - 16 * u - e1));
-    const float keep = exp2f(g2 * C);
+            for (int i = 0; i < 8; ++i) {
+                const int j = 16 * u + 8 * (i >> 2) + 4 * half + (i & 3);
+                into[u][i] = j < tokens ? exp2f(g2 * (tokens - j - e1)) * role.u : 0.f;
+            }
+    };
+    weigh(C);
 
     // Token t of the role's time lies at t, or with time running back at length - 1 - t. Rows behind the last token are read as that.
-    auto stage = [&](int c0, lds_byte* at) {
-        const int last = min(C, t1 - c0) - 1;
-        const int first = role.back ? length - 1 - c0 - last : c0;
-        auto off = [&](long long stride) {
-            return [=](int r) {
-                const int m = min(r, last);
-                return static_cast<uint32_t>(role.back ? last - m : m) * (static_cast<uint32_t>(stride) * ES);
-            };
+    // A lane's places within a chunk are the same for all whole ones: only the last chunk, which is staged last, changes them.
+    constexpr int RK = 64 / KT::kChunks * W, RV = 64 / VT::kChunks * W, NK = (C + RK - 1) / RK, NV = (C + RV - 1) / RV;   // rows and number of instructions
+    uint32_t qoff[STATES ? 1 : NK], koff[NK], voff[NV];
+    auto place = [&](int tokens) {
+        auto rows = [&](auto& off, int n, int per, int chunks, auto swz, long long stride) {
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+                const int r = i * per + wave * (64 / chunks) + lane / chunks, m = min(r, tokens - 1);
+                off[i] = static_cast<uint32_t>(role.back ? tokens - 1 - m : m) * (static_cast<uint32_t>(stride) * ES) + ((lane % chunks) ^ swz(r)) * 16;
+            }
         };
-        if constexpr (!STATES)
-            KT::stage(at, tiles::map_resource(byte_at(role.q, b * role.qb + first * role.qn + h * role.qh, ES)), C, wave, W, lane, off(role.qn));
-        KT::stage(at + kQ, tiles::map_resource(byte_at(role.k, b * role.kb + first * role.kn + h * role.kh, ES)), C, wave, W, lane, off(role.kn));
-        VT::stage(at + kQ + kK, tiles::map_resource(byte_at(role.v, b * role.vb + first * role.vn + h * role.vh, ES)), C, wave, W, lane, off(role.vn));
+        if constexpr (!STATES) rows(qoff, NK, RK, KT::kChunks, KT::swz, role.qn);
+        rows(koff, NK, RK, KT::kChunks, KT::swz, role.kn);
+        rows(voff, NV, RV, VT::kChunks, VT::swz, role.vn);
+    };
+    place(C);
+    auto stage = [&](int c0, lds_byte* at) {
+        const int tokens = min(C, t1 - c0);
+        if (tokens < C) place(tokens);
+        const int first = role.back ? length - c0 - tokens : c0;
+        auto bring = [&](const auto& off, int n, int per, int chunks, int bytes, const void* x, long long elem, lds_byte* to) {
+            const u32x4_t map = map_words(byte_at(x, elem, ES));
+            const uint32_t at0 = __builtin_amdgcn_readfirstlane(lds_address(to) + wave * (64 / chunks) * bytes);
+#pragma unroll
+            for (int i = 0; i < n; ++i)
+                if (i * per + wave * (64 / chunks) < C) load_lds16_untracked(map, off[i], at0 + i * per * bytes);
+        };
+        if constexpr (!STATES) bring(qoff, NK, RK, KT::kChunks, KT::kRow, role.q, b * role.qb + first * role.qn + h * role.qh, at);
+        bring(koff, NK, RK, KT::kChunks, KT::kRow, role.k, b * role.kb + first * role.kn + h * role.kh, at + kQ);
+        bring(voff, NV, RV, VT::kChunks, VT::kRow, role.v, b * role.vb + first * role.vn + h * role.vh, at + kQ + kK);
     };
 
     const uint32_t base = lds_address(lds);
     const uint32_t row = base + KT::row_base(lane), kcol = base + kQ + KT::col_base(lane, true), vcol = base + kQ + kK + VT::col_base(lane);
     uint32_t at = 0;
-    if (t0 < t1) stage(t0, lds);
-    for (int c0 = t0; c0 < t1; c0 += C) {
-        // (the other half of LDS was read before this barrier, and is free behind it)
+    // D chunks in LDS: one worked on, the others on their way. A wave's loads land in order, so that once no more than those of the
+    // D - 2 later chunks are outstanding (kLater: as many as every wave has issued for them at least) the next chunk is there.
+    constexpr int D = decay_depth(kStage), kLater = (D - 2) * ((STATES ? 1 : 2) * (C / RK) + C / RV);
+    if (t0 < t1) {
+        for (int d = 0; d < D - 1 && t0 + d * C < t1; ++d) stage(t0 + d * C, lds + d * kStage);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __syncthreads();
-        if (c0 + C < t1) stage(c0 + C, lds + (at ^ kStage));
+    }
+    for (int c0 = t0; c0 < t1; c0 += C) {
+        // (what lies there was read before the last barrier)
+        const bool more = c0 + (D - 1) * C < t1;
+        if (more) stage(c0 + (D - 1) * C, lds + (at == 0 ? (D - 1) * kStage : at - kStage));
         const int left = t1 - c0;
+        if (left < C) weigh(left);
         f32x16 o[TT];
         Terms<T, PT> p[3][2];                                       // tiles (0, 0), (1, 0), (1, 1) of the scores
         if constexpr (!STATES) {
@@ -201,10 +251,8 @@ __global__ __launch_bounds__(2 * DV) void decay_chunk_kernel(DecayArgs a)
                     p[t][w] = split_terms<T, PT>(z);
                 }
         }
-        // (a chunk that the last token ends has weights of its own: into[] counts from the end of a whole one)
-        const float keep_now = left >= C ? keep : exp2f(g2 * left);
 #pragma unroll
-        for (int t = 0; t < A; ++t) S[t] *= keep_now;
+        for (int t = 0; t < A; ++t) S[t] *= keep;
 #pragma unroll
         for (int u = 0; u < C / 16; ++u) {
             const Frag<T> vf = VT::col_frag(vcol + at, 0, 16 * u, wave);
@@ -215,20 +263,10 @@ __global__ __launch_bounds__(2 * DV) void decay_chunk_kernel(DecayArgs a)
                     if constexpr (TT == 2) o[1] = mma(vf, p[u < 2 ? 1 : 2][u & 1].t[n], o[1]);
                 }
             }
-            float z[8], w[8];
+            float z[8];
             unpack_frag(vf, z);
-            if (left >= C) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = into[i] * into_step[u];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int j = 16 * u + 8 * (i >> 2) + 4 * half + (i & 3);
-                    w[i] = j < left ? exp2f(g2 * (left - j - e1)) * role.u : 0.f;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] *= w[i];
+            for (int i = 0; i < 8; ++i) z[i] *= into[u][i];
             const Terms<T, ST> vt = split_terms<T, ST>(z);
 #pragma unroll
             for (int t = 0; t < A; ++t) {
@@ -237,6 +275,9 @@ __global__ __launch_bounds__(2 * DV) void decay_chunk_kernel(DecayArgs a)
                 for (int n = 0; n < ST; ++n) S[t] = mma(kf, vt.t[n], S[t]);
             }
         }
+        // the next chunk has landed before this one's results go out, so that nobody waits for these
+        if (more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLater) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         if constexpr (!STATES) {
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
@@ -249,7 +290,8 @@ __global__ __launch_bounds__(2 * DV) void decay_chunk_kernel(DecayArgs a)
                 }
             }
         }
-        at ^= kStage;
+        __syncthreads();
+        at = at == (D - 1) * kStage ? 0 : at + kStage;
     }
     float* to = nullptr;
     if constexpr (STATES) to = a.part + static_cast<long long>(which) * a.B * a.heads * a.segs * (DK * DV) + cell;
@@ -355,12 +397,12 @@ __global__ __launch_bounds__(256) void decay_step_kernel(DecayStepArgs a)
     }
 }
 
-template <typename T, int DK, int DV, bool STATES>
-hipError_t launch(const DecayArgs& a, hipStream_t stream)
+template <typename T, int DK, int DV, bool STATES, bool EXACT>
+hipError_t launch_exact(const DecayArgs& a, hipStream_t stream)
 {
     static std::atomic<unsigned long long> configured{0};
-    constexpr int C = decay_chunk(sizeof(T) == 2), lds = 2 * C * ((STATES ? 1 : 2) * DK + DV) * static_cast<int>(sizeof(T));
-    const auto kernel = &decay_chunk_kernel<T, DK, DV, C, STATES>;
+    constexpr int C = decay_chunk(sizeof(T) == 2), stage = C * ((STATES ? 1 : 2) * DK + DV) * static_cast<int>(sizeof(T)), lds = decay_depth(stage) * stage;
+    const auto kernel = &decay_chunk_kernel<T, DK, DV, C, STATES, EXACT>;
     const hipError_t e = set_max_lds_once(reinterpret_cast<const void*>(kernel), configured);
     if (e != hipSuccess) return e;
     DecayArgs p = a;
@@ -369,6 +411,15 @@ hipError_t launch(const DecayArgs& a, hipStream_t stream)
     const long long blocks = static_cast<long long>(a.roles) * a.B * a.heads * a.segs;
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(2 * DV), lds, stream, p);
     return hipGetLastError();
+}
+
+template <typename T, int DK, int DV, bool STATES>
+hipError_t launch(const DecayArgs& a, hipStream_t stream)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (!a.exact) return launch_exact<T, DK, DV, STATES, false>(a, stream);
+    }
+    return launch_exact<T, DK, DV, STATES, true>(a, stream);
 }
 
 template <typename T, int DK, int DV>
