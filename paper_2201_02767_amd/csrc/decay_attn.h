@@ -68,35 +68,27 @@ struct DecayStepArgs {
 // Calls of up to this many tokens go token by token through states that stay in registers.
 constexpr int kDecayStepTokens = 16;
 
-// Tokens of a chunk: as many as LDS holds twice.
-#ifndef DECAY_C
-#define DECAY_C 32
-#endif
-constexpr int decay_chunk(bool bf16_inputs) { return bf16_inputs ? DECAY_C : 32; }
-#ifndef DECAY_D
-#define DECAY_D 4
-#endif
-// Chunks in LDS at a time: up to four, two where two workgroups a unit would not fit otherwise.
-constexpr int decay_depth(int bytes) { return 4 * bytes <= (76 << 10) && DECAY_D >= 4 ? 4 : 3 * bytes <= (144 << 10) && DECAY_D >= 3 ? 3 : 2; }
-#ifndef DECAY_W
-#define DECAY_W 4LL
-#endif
-#ifndef DECAY_LB
-#define DECAY_LB 2
-#endif
+// Tokens of a chunk: a tile of the products.
+constexpr int kDecayChunk = 32;
+constexpr int kDecayTables = 4096 + 2 * kDecayChunk * 4;            // bytes of the weights behind the chunks in LDS
+// Chunks in LDS at a time: as many as leave room for three workgroups of the largest kind (a unit has 160 KB), at most four. (The loads
+// of two are enough: with two, three and four chunks prompts of 65536 tokens take the same 200 us.)
+constexpr int decay_depth(int bytes) { return 4 * bytes <= (48 << 10) ? 4 : 3 * bytes <= (48 << 10) ? 3 : 2; }
 
-// Segments of a call.
+// Segments of a call: enough for two workgroups of four waves a unit, or as many waves in smaller ones (2 x 8192 tokens, 16 heads of 128,
+// bf16, forward and backward: states 31 + 31, scans 11 + 11, results 67 + 175 us; with four a unit 40 + 36, 21 + 21 and 72 + 190: the
+// states' bytes), none below two chunks, or one in fp32, whose products take 16 times as long (2 x 997 tokens, 8 heads of 32, a step's five
+// launches 53 us with two, 44 with one; 3 x 1031 bf16 tokens, 8 heads of 32/64: 20 us with two and with one, 29 with eight).
 struct DecaySegments {
     int segs, seg;
 };
-inline DecaySegments decay_segments(int B, int heads, int N, int roles, bool bf16_inputs)
+inline DecaySegments decay_segments(int B, int heads, int N, int dv, int roles, bool bf16_inputs)
 {
-    const long long chunk = decay_chunk(bf16_inputs), rows = static_cast<long long>(B) * heads * roles;
-    const long long want = DECAY_W * device_cu_count();
-    const long long most = (N + 4 * chunk - 1) / (4 * chunk);
+    const long long rows = static_cast<long long>(B) * heads * roles, want = 2LL * device_cu_count() * 128 / dv;
+    const long long most = std::max(1, N / ((bf16_inputs ? 2 : 1) * kDecayChunk));
     const long long segs = std::max(1LL, std::min(most, (want + rows - 1) / rows));
-    const long long seg = ((N + segs - 1) / segs + chunk - 1) / chunk * chunk;
-    return {static_cast<int>((N + seg - 1) / seg), static_cast<int>(seg)};
+    const int seg = static_cast<int>(((N + segs - 1) / segs + kDecayChunk - 1) / kDecayChunk * kDecayChunk);
+    return {(N + seg - 1) / seg, seg};
 }
 
 constexpr long long kDecayMaxBlocks = (1LL << 32) / 256 - 1;

@@ -83,18 +83,43 @@ __device__ __forceinline__ float decay_log2(const float* log_decay, int h)
 }
 __device__ __forceinline__ int decay_length(const int32_t* lens, int b, int N) { return lens ? min(max(lens[b], 0), N) : N; }
 
+// Column tok of a result, 32 rows, as 32 neighbours from element `at` on. bf16: a lane takes 16 of them, by exchanging what lies between
+// with the other half's.
+template <typename T>
+__device__ __forceinline__ void store_tile(void* base, long long at, const f32x16& o)
+{
+    const int half = (threadIdx.x >> 5) & 1;
+    if constexpr (sizeof(T) == 2) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = pack2(o[2 * i], o[2 * i + 1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const auto x = __builtin_amdgcn_permlane32_swap(w[i], w[i + 4], false, false);
+            w[i] = x[0];
+            w[i + 4] = x[1];
+        }
+        u32x4_t* const to = reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(base) + at + 16 * half);
+        to[0] = u32x4_t{w[0], w[1], w[4], w[5]};
+        to[1] = u32x4_t{w[2], w[3], w[6], w[7]};
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) store4<float>(base, at + 2 * r + 4 * half, o[r], o[r + 1], o[r + 2], o[r + 3]);
+    }
+}
+
 // EXACT: what is added to the state keeps 24 bits (bf16: three terms of the weighted values), for a state that the call returns; 16 bits
 // (two) do where the state only makes results of 8.
 // STATES: only what each segment adds to the state, to a.part. Otherwise the results, from the states before each segment.
-template <typename T, int DK, int DV, int C, bool STATES, bool EXACT>
-__global__ __launch_bounds__(2 * DV, DK <= 64 ? DECAY_LB : 2) void decay_chunk_kernel(DecayArgs a)
+template <typename T, int DK, int DV, bool STATES, bool EXACT>
+__global__ __launch_bounds__(2 * DV, sizeof(T) == 2 ? (DK == 128 && DV == 32 ? 2 : 3) : (DK == 32 ? 3 : 2)) void decay_chunk_kernel(DecayArgs a)
 {
     using KT = Tile<T, DK>;
     using VT = Tile<T, DV>;
-    constexpr int ES = sizeof(T), W = DV / 32, A = DK / 32, TT = C / 32;
+    constexpr int ES = sizeof(T), W = DV / 32, A = DK / 32, C = kDecayChunk;
     constexpr int kQ = STATES ? 0 : KT::bytes(C), kK = KT::bytes(C), kStage = kQ + kK + VT::bytes(C);
     constexpr int PT = ES == 2 ? 2 : 1, ST = ES == 2 ? (EXACT ? 3 : 2) : 1;      // terms of scores and states as operands, of what states get
-    static_assert(TT <= 2, "the products of one or two tiles of tokens");
+    constexpr int D = decay_depth(kStage);
     extern __shared__ __align__(1024) unsigned char lds_raw[];
     lds_byte* const lds = (lds_byte*)lds_raw;
 
@@ -134,33 +159,22 @@ __global__ __launch_bounds__(2 * DV, DK <= 64 ? DECAY_LB : 2) void decay_chunk_k
             for (int r = 0; r < 16; ++r) S[t][r] = from[state_at(t, r)];
     }
 
-    // weights: of a score (row acc_row(r) of column tok) on the diagonal tile and on the one before it, of the state in each token,
-    // and of rows 16 u + (0 .. 15) of a whole chunk in the state
-    float diag[16], before[TT == 2 ? 16 : 1], after = 0.f, come[TT], into[C / 16][8];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int apart = tok - acc_row(r, half);
-        diag[r] = apart >= 0 ? exp2f(g2 * apart) * a.scale : 0.f;
-        if constexpr (TT == 2) before[r] = exp2f(g2 * (32 - acc_row(r, half)));
+    // Weights, in LDS behind the chunks (registers are what keeps waves off the units): of a score on the diagonal tile (row acc_row(r) of
+    // column tok), of token j in the state of a whole chunk and of the last one, which may be shorter; in registers: of the state in each token
+    const int tail = t1 > t0 ? (t1 - t0 - 1) % C + 1 : C;
+    lds_byte* const tables = lds + D * kStage;
+    for (int x = threadIdx.x; x < 64 * 16; x += 2 * DV) {           // [r / 4][lane][r % 4]
+        const int l = (x >> 2) & 63, r = (x >> 8) * 4 + (x & 3), apart = (l & 31) - acc_row(r, l >> 5);
+        *(lds_ptr<float>)(tables + x * 4) = apart >= 0 ? exp2f(g2 * apart) * a.scale : 0.f;
     }
-    if constexpr (TT == 2) after = exp2f(g2 * tok) * a.scale;
-#pragma unroll
-    for (int t = 0; t < TT; ++t) come[t] = exp2f(g2 * (32 * t + tok + e1)) * role.f;
-    float keep;
-    auto weigh = [&](int tokens) {                                  // of a chunk of so many
-        keep = exp2f(g2 * tokens);
-#pragma unroll
-        for (int u = 0; u < C / 16; ++u)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int j = 16 * u + 8 * (i >> 2) + 4 * half + (i & 3);
-                into[u][i] = j < tokens ? exp2f(g2 * (tokens - j - e1)) * role.u : 0.f;
-            }
-    };
-    weigh(C);
+    for (int x = threadIdx.x; x < 2 * C; x += 2 * DV) {             // [whole, last][16 u + 8 (lane / 32) + i], in the order of a column fragment
+        const int y = x & (C - 1), j = (y & ~15) + 8 * ((y >> 2) & 1) + 4 * ((y >> 3) & 1) + (y & 3), n = x < C ? C : tail;
+        *(lds_ptr<float>)(tables + 4096 + x * 4) = j < n ? exp2f(g2 * (n - j - e1)) * role.u : 0.f;
+    }
+    const float come = exp2f(g2 * (tok + e1)) * role.f, keep_whole = exp2f(g2 * C), keep_last = exp2f(g2 * tail);
 
     // Token t of the role's time lies at t, or with time running back at length - 1 - t. Rows behind the last token are read as that.
-    // A lane's places within a chunk are the same for all whole ones: only the last chunk, which is staged last, changes them.
+    // A lane's places within a chunk are the same for all whole ones.
     constexpr int RK = 64 / KT::kChunks * W, RV = 64 / VT::kChunks * W, NK = (C + RK - 1) / RK, NV = (C + RV - 1) / RV;   // rows and number of instructions
     uint32_t qoff[STATES ? 1 : NK], koff[NK], voff[NV];
     auto place = [&](int tokens) {
@@ -175,10 +189,10 @@ __global__ __launch_bounds__(2 * DV, DK <= 64 ? DECAY_LB : 2) void decay_chunk_k
         rows(koff, NK, RK, KT::kChunks, KT::swz, role.kn);
         rows(voff, NV, RV, VT::kChunks, VT::swz, role.vn);
     };
-    place(C);
+    int placed = 0;
     auto stage = [&](int c0, lds_byte* at) {
         const int tokens = min(C, t1 - c0);
-        if (tokens < C) place(tokens);
+        if (tokens != placed) place(placed = tokens);
         const int first = role.back ? length - c0 - tokens : c0;
         auto bring = [&](const auto& off, int n, int per, int chunks, int bytes, const void* x, long long elem, lds_byte* to) {
             const u32x4_t map = map_words(byte_at(x, elem, ES));
@@ -197,76 +211,73 @@ __global__ __launch_bounds__(2 * DV, DK <= 64 ? DECAY_LB : 2) void decay_chunk_k
     uint32_t at = 0;
     // D chunks in LDS: one worked on, the others on their way. A wave's loads land in order, so that once no more than those of the
     // D - 2 later chunks are outstanding (kLater: as many as every wave has issued for them at least) the next chunk is there.
-    constexpr int D = decay_depth(kStage), kLater = (D - 2) * ((STATES ? 1 : 2) * (C / RK) + C / RV);
-    if (t0 < t1) {
-        for (int d = 0; d < D - 1 && t0 + d * C < t1; ++d) stage(t0 + d * C, lds + d * kStage);
+    constexpr int kLater = (D - 2) * ((STATES ? 1 : 2) * (C / RK) + C / RV);
+    // The results' chunks come in the order of time. What a segment adds to the state is summed from its last chunk to its first, with
+    // weights that go to the segment's end: then the results' launch, which starts at the segments' first chunks, finds those in the
+    // memory's cache, where they were read last.
+    const int chunks = t0 < t1 ? (t1 - t0 + C - 1) / C : 0;
+    auto start = [&](int x) { return t0 + (STATES ? chunks - 1 - x : x) * C; };
+    if (chunks > 0) {
+        for (int d = 0; d < D - 1 && d < chunks; ++d) stage(start(d), lds + d * kStage);
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __syncthreads();
     }
-    for (int c0 = t0; c0 < t1; c0 += C) {
+    for (int x = 0; x < chunks; ++x) {
         // (what lies there was read before the last barrier)
-        const bool more = c0 + (D - 1) * C < t1;
-        if (more) stage(c0 + (D - 1) * C, lds + (at == 0 ? (D - 1) * kStage : at - kStage));
+        const int c0 = start(x);
+        const bool more = x + D - 1 < chunks;
+        if (more) stage(start(x + D - 1), lds + (at == 0 ? (D - 1) * kStage : at - kStage));
         const int left = t1 - c0;
-        if (left < C) weigh(left);
-        f32x16 o[TT];
-        Terms<T, PT> p[3][2];                                       // tiles (0, 0), (1, 0), (1, 1) of the scores
+        f32x16 o{};
+        Terms<T, PT> p[2];
         if constexpr (!STATES) {
-            f32x16 s[TT == 2 ? 3 : 1];
-#pragma unroll
-            for (int t = 0; t < TT; ++t) o[t] = f32x16{};
-#pragma unroll
-            for (int t = 0; t < (TT == 2 ? 3 : 1); ++t) s[t] = f32x16{};
+            f32x16 s{};
 #pragma unroll
             for (int c = 0; c < DK / 16; ++c) {
                 float z[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = S[c / 2][8 * (c & 1) + i];
                 const Terms<T, PT> st = split_terms<T, PT>(z);
-                Frag<T> qf[TT], kf[TT];
+                const Frag<T> qf = KT::row_frag(row + at, 0, 0, c);
+                s = mma(KT::row_frag(row + at, kQ, 0, c), qf, s);
 #pragma unroll
-                for (int t = 0; t < TT; ++t) {
-                    qf[t] = KT::row_frag(row + at, 0, 32 * t, c);
-                    kf[t] = KT::row_frag(row + at, kQ, 32 * t, c);
-                }
-                s[0] = mma(kf[0], qf[0], s[0]);
-                if constexpr (TT == 2) {
-                    s[1] = mma(kf[0], qf[1], s[1]);
-                    s[2] = mma(kf[1], qf[1], s[2]);
-                }
-#pragma unroll
-                for (int t = 0; t < TT; ++t)
-#pragma unroll
-                    for (int n = 0; n < PT; ++n) o[t] = mma(st.t[n], qf[t], o[t]);
+                for (int n = 0; n < PT; ++n) o = mma(st.t[n], qf, o);
             }
+            o *= come;
 #pragma unroll
-            for (int t = 0; t < TT; ++t) o[t] *= come[t];
+            for (int w = 0; w < 2; ++w) {
+                float z[8];
 #pragma unroll
-            for (int t = 0; t < (TT == 2 ? 3 : 1); ++t)
+                for (int i = 0; i < 8; i += 4) {
+                    const f32x4 d = *(lds_ptr<f32x4>)(tables + (8 * w + i) / 4 * 1024 + lane * 16);
 #pragma unroll
-                for (int w = 0; w < 2; ++w) {
-                    float z[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) z[i] = s[t][8 * w + i] * (TT == 2 && t == 1 ? before[TT == 2 ? 8 * w + i : 0] * after : diag[8 * w + i]);
-                    p[t][w] = split_terms<T, PT>(z);
+                    for (int e = 0; e < 4; ++e) z[i + e] = s[8 * w + i + e] * d[e];
                 }
+                p[w] = split_terms<T, PT>(z);
+            }
         }
+        const float keep = left >= C ? keep_whole : keep_last;
+        lds_byte* const into = tables + 4096 + (left >= C ? 0 : 4 * C) + half * 32;
+        const float far = STATES ? exp2f(g2 * max(left - C, 0)) : 1.f;
+        if constexpr (!STATES) {
 #pragma unroll
-        for (int t = 0; t < A; ++t) S[t] *= keep;
+            for (int t = 0; t < A; ++t) S[t] *= keep;
+        }
 #pragma unroll
         for (int u = 0; u < C / 16; ++u) {
             const Frag<T> vf = VT::col_frag(vcol + at, 0, 16 * u, wave);
             if constexpr (!STATES) {
 #pragma unroll
-                for (int n = 0; n < PT; ++n) {
-                    if (u < 2) o[0] = mma(vf, p[0][u & 1].t[n], o[0]);
-                    if constexpr (TT == 2) o[1] = mma(vf, p[u < 2 ? 1 : 2][u & 1].t[n], o[1]);
-                }
+                for (int n = 0; n < PT; ++n) o = mma(vf, p[u].t[n], o);
             }
             float z[8];
             unpack_frag(vf, z);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] *= into[u][i];
+            for (int i = 0; i < 8; i += 4) {
+                const f32x4 w = *(lds_ptr<f32x4>)(into + u * 64 + i * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[i + e] *= STATES ? w[e] * far : w[e];
+            }
             const Terms<T, ST> vt = split_terms<T, ST>(z);
 #pragma unroll
             for (int t = 0; t < A; ++t) {
@@ -279,15 +290,9 @@ __global__ __launch_bounds__(2 * DV, DK <= 64 ? DECAY_LB : 2) void decay_chunk_k
         if (more) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLater) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         if constexpr (!STATES) {
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                const int i = 32 * t + tok;
-                if (i < left) {
-                    const int n = role.back ? length - 1 - c0 - i : c0 + i;
-                    const long long to = ((static_cast<long long>(b) * a.N + n) * a.heads + h) * DV + 32 * wave + 4 * half;
-#pragma unroll
-                    for (int r = 0; r < 16; r += 4) store4<T>(role.out, to + 2 * r, o[t][r], o[t][r + 1], o[t][r + 2], o[t][r + 3]);
-                }
+            if (tok < left) {
+                const int n = role.back ? length - 1 - c0 - tok : c0 + tok;
+                store_tile<T>(role.out, ((static_cast<long long>(b) * a.N + n) * a.heads + h) * DV + 32 * wave, o);
             }
         }
         __syncthreads();
@@ -321,18 +326,23 @@ __global__ __launch_bounds__(256) void decay_scan_kernel(DecayScanArgs a)
     const float* const state = role ? a.state[1] : a.state[0];
     float* const last = role ? a.last[1] : a.last[0];
     f32x4 S = state ? reinterpret_cast<const f32x4*>(state)[bh * quads + quad] : f32x4{};
-    constexpr int kAhead = 8;                                       // segments whose loads are in flight
-    for (int s0 = 0; s0 < a.segs; s0 += kAhead) {
-        f32x4 add[kAhead];
+    // the next four segments' loads are in flight while four are added
+    constexpr int kAhead = 4;
+    f32x4 add[kAhead], next[kAhead];
+    auto fetch = [&](f32x4 (&x)[kAhead], int s0) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) add[i] = part[static_cast<long long>(min(s0 + i, a.segs - 1)) * quads];
+        for (int i = 0; i < kAhead; ++i) x[i] = part[static_cast<long long>(min(s0 + i, a.segs - 1)) * quads];
+    };
+    fetch(add, 0);
+    for (int s0 = 0; s0 < a.segs; s0 += kAhead) {
+        fetch(next, s0 + kAhead);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int s = s0 + i;
-            if (s >= a.segs) break;
-            const int left = length - s * a.seg;
-            part[static_cast<long long>(s) * quads] = S;
-            if (left > 0) S = S * (left >= a.seg ? keep : exp2f(g2 * left)) + add[i];
+            const int left = length - (s0 + i) * a.seg;
+            if (s0 + i < a.segs) part[static_cast<long long>(s0 + i) * quads] = S;
+            if (left >= a.seg) S = S * keep + add[i];
+            else if (left > 0) S = S * exp2f(g2 * left) + add[i];
+            add[i] = next[i];
         }
     }
     if (last) reinterpret_cast<f32x4*>(last)[bh * quads + quad] = S;
@@ -401,8 +411,8 @@ template <typename T, int DK, int DV, bool STATES, bool EXACT>
 hipError_t launch_exact(const DecayArgs& a, hipStream_t stream)
 {
     static std::atomic<unsigned long long> configured{0};
-    constexpr int C = decay_chunk(sizeof(T) == 2), stage = C * ((STATES ? 1 : 2) * DK + DV) * static_cast<int>(sizeof(T)), lds = decay_depth(stage) * stage;
-    const auto kernel = &decay_chunk_kernel<T, DK, DV, C, STATES, EXACT>;
+    constexpr int stage = kDecayChunk * ((STATES ? 1 : 2) * DK + DV) * static_cast<int>(sizeof(T)), lds = decay_depth(stage) * stage + kDecayTables;
+    const auto kernel = &decay_chunk_kernel<T, DK, DV, STATES, EXACT>;
     const hipError_t e = set_max_lds_once(reinterpret_cast<const void*>(kernel), configured);
     if (e != hipSuccess) return e;
     DecayArgs p = a;
