@@ -465,7 +465,7 @@ qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const float* m
  *   log_decay   device fp32 [heads], natural logarithms of the decays: <= 0 (-inf: nothing is remembered). A positive one grows;
  *               results are then right as long as they are finite. Beyond +-11356 it counts as that.
  *   state       fp32 [B][heads][dk][dv] contiguous, 16-byte aligned, or NULL for zeros.
- *   dk, dv      32, 64 or 128 each.
+ *   dk, dv      32, 64 or 128 each. N at most 2^29, heads 2^16, B * heads 2^24.
  *   scale       2^-64 .. 2^64; <= 0: 1/sqrt(dk).
  *   lens        device int32 [B] or NULL: element b's tokens are [0, lens[b]) (clamped to [0, N]). What lies behind them is never
  *               used, whatever it holds; its results are zeros.

@@ -21,8 +21,8 @@ qta_status check_decay(const qta_decay_attn_args* a, bool shapes_only)
     if (a->B <= 0 || a->heads <= 0 || a->N <= 0 || a->dk <= 0 || a->dv <= 0) return QTA_ERR_INVALID;
     if (a->dtype != QTA_F32 && a->dtype != QTA_BF16) return QTA_ERR_INVALID;
     if (!size_ok(a->dk) || !size_ok(a->dv)) return QTA_ERR_UNSUPPORTED;
-    // (token counts are int with room for the chunk behind the last)
-    if (a->N > (1 << 30) || a->heads > (1 << 16) || static_cast<long long>(a->B) * a->heads > (1LL << 24)) return QTA_ERR_UNSUPPORTED;
+    // (token counts are int, with room for a segment behind the last)
+    if (a->N > (1 << 29) || a->heads > (1 << 16) || static_cast<long long>(a->B) * a->heads > (1LL << 24)) return QTA_ERR_UNSUPPORTED;
     if (shapes_only) return QTA_OK;
     if (!a->q || !a->k || !a->v || !a->log_decay) return QTA_ERR_INVALID;
     for (const void* p : {a->q, a->k, a->v, static_cast<const void*>(a->state)})

@@ -133,6 +133,13 @@ def decay_attn_backward(q, k, v, log_decay, dout, *, scale=None, lens=None, stat
     return (*_decay_backward(args, q, k, v, dout, dstate_out, dstate), dstate)
 
 
+def _once(backward):
+    """A Function's backward whose results are not to be differentiated again. (The decorator for that takes 7 us a call: only where
+    a graph of the backward is asked for.)"""
+    guarded = torch.autograd.function.once_differentiable(backward)
+    return staticmethod(lambda ctx, *grads: guarded(ctx, *grads) if torch.is_grad_enabled() else backward(ctx, *grads))
+
+
 class _DecayAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, state, log_decay, scale, lens, return_state):
@@ -144,8 +151,7 @@ class _DecayAttention(torch.autograd.Function):
         ctx.save_for_backward(q, k, v, state, log_decay, lens)
         return (out, last) if return_state else out
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dout, dstate_out=None):
         q, k, v, state, log_decay, lens = ctx.saved_tensors
         if dout is None and dstate_out is None:

@@ -5,6 +5,7 @@ import ctypes
 
 import torch
 
+from .decay import _once
 from .dense import _call, _no_tangents, _tokens, _workspace
 from .qta import _DTYPES, _SIGS, _dtype_code
 
@@ -73,8 +74,7 @@ class _GroupNorm(torch.autograd.Function):
         ctx.save_for_backward(x, weight, bias, stats)
         return y
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy):
         x, weight, bias, stats = ctx.saved_tensors
         dy = dy.contiguous()
