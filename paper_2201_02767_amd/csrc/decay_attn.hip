@@ -68,7 +68,7 @@ __device__ __forceinline__ u32x4_t map_words(const unsigned char* base)
 
 // 16 bytes a lane from the map to LDS, lane i's at byte dst + 16 i. In assembly, which has no register of a lane's to write: of
 // the builtin the compiler waits for every load before the next transposed read from LDS, which here are of chunks that landed long before
-// (that wait in the middle of a chunk: 200 us for 152 below). wait for them with s_waitcnt vmcnt.
+// (that wait in the middle of a chunk: 130 us for 105 of the states of 65536 tokens). Wait for them with s_waitcnt vmcnt.
 __device__ __forceinline__ void load_lds16_untracked(const u32x4_t& map, uint32_t off, uint32_t dst)
 {
     // (nothing else here uses m0; five wait states between a lane operation that wrote the descriptor and the load, one behind m0)
