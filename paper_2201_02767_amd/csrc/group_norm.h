@@ -34,7 +34,7 @@ struct NormArgs {
     int lanes, sums;            // (per token) lanes of a group; workgroups' sums in part
     int rows_lanes;             // lanes that share the rows of a channel
     float* group_part;
-    FastDiv div_N, div_slabs, div_rows, div_entry;
+    FastDiv div_N, div_P, div_slabs, div_rows, div_entry;
 };
 
 // Maps take two launches that each go over them (bound by memory: 8 maps of 200 x 336 x 256 bf16, 275 MB each, SiLU: 45 us to read x, 103 to

@@ -54,6 +54,21 @@ __device__ __forceinline__ float param(const void* p, bool is_bf16, int c, float
     if (!p) return otherwise;
     return is_bf16 ? Storage<bf16>::load1(p, c) : Storage<float>::load1(p, c);
 }
+// N weights from channel c on, or `otherwise`. (One choice for all: a branch for each would wait for each load by itself.)
+template <int N>
+__device__ __forceinline__ void params(const void* p, bool is_bf16, int c, float otherwise, float (&x)[N])
+{
+    if (!p) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = otherwise;
+    } else if (is_bf16) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = Storage<bf16>::load1(p, c + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = Storage<float>::load1(p, c + i);
+    }
+}
 __device__ __forceinline__ void store_param(void* p, bool is_bf16, int c, float x)
 {
     if (is_bf16) Storage<bf16>::store1(p, c, x);
@@ -137,10 +152,12 @@ __global__ __launch_bounds__(256) void norm_tokens_kernel(NormArgs a)
         const int c = (lane + k * a.lanes) * V;
         on[k] = mine && c < a.P;
         at[k] = on[k] ? g * a.P + c : 0;
+        params(a.weight, a.param_bf16, at[k], 1.f, w[k]);
+        params(a.bias, a.param_bf16, at[k], 0.f, bias[k]);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            w[k][i] = on[k] ? param(a.weight, a.param_bf16, at[k] + i, 1.f) : 0.f;
-            bias[k][i] = on[k] ? param(a.bias, a.param_bf16, at[k] + i, 0.f) : 0.f;
+            w[k][i] = on[k] ? w[k][i] : 0.f;
+            bias[k][i] = on[k] ? bias[k][i] : 0.f;
         }
     }
     // (the next token's loads are in flight while one is worked on; rows behind the last are read as that)
@@ -529,17 +546,14 @@ __global__ __launch_bounds__(kT) void norm_apply_kernel(NormArgs a)
     const NormPlace at(a, xcd_remap(blockIdx.x, gridDim.x), V);
     NormStream<T, V, 4, false, true> stream(a, at);
     float f[V], bias[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        f[i] = at.mine ? param(a.weight, a.param_bf16, at.col + i, 1.f) : 0.f;
-        bias[i] = at.mine ? param(a.bias, a.param_bf16, at.col + i, 0.f) : 0.f;
-    }
+    params(a.weight, a.param_bf16, at.mine ? at.col : 0, 1.f, f);
+    params(a.bias, a.param_bf16, at.mine ? at.col : 0, 0.f, bias);
     join_stats(a, at, V, box);
     if (!at.mine) return;
     // (x r - mean r: as far off as the mean's own rounding makes x - mean)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const float2 s = box[(at.col + i) / a.P - at.c0 / a.P];
+        const float2 s = box[fast_div(at.col + i, a.div_P) - at.c0 / a.P];
         f[i] *= s.y;
         bias[i] -= s.x * f[i];
     }
@@ -559,13 +573,13 @@ struct NormChannels {
     float r[V], shift[V], w[V], bias[V];        // n = x r + shift
     __device__ __forceinline__ NormChannels(const NormArgs& a, const NormPlace& at)
     {
+        params(a.weight, a.param_bf16, at.mine ? at.col : 0, 1.f, w);
+        params(a.bias, a.param_bf16, at.mine ? at.col : 0, 0.f, bias);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float2 s = reinterpret_cast<const float2*>(a.stats)[static_cast<long long>(at.b) * a.groups + (at.mine ? (at.col + i) / a.P : 0)];
+            const float2 s = reinterpret_cast<const float2*>(a.stats)[static_cast<long long>(at.b) * a.groups + (at.mine ? fast_div(at.col + i, a.div_P) : 0)];
             r[i] = s.y;
             shift[i] = -s.x * s.y;
-            w[i] = param(a.weight, a.param_bf16, at.mine ? at.col + i : 0, 1.f);
-            bias[i] = param(a.bias, a.param_bf16, at.mine ? at.col + i : 0, 0.f);
         }
     }
 };
@@ -708,7 +722,7 @@ __global__ __launch_bounds__(kT) void norm_dx_kernel(NormArgs a)
     float s1[V], s0[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const float2 s = box[(at.col + i) / a.P - g0];
+        const float2 s = box[fast_div(at.col + i, a.div_P) - g0];
         s1[i] = s.x;
         s0[i] = s.y;
     }
@@ -754,6 +768,7 @@ hipError_t launch(NormArgs a, const NormPlan& p, bool back, hipStream_t stream)
     a.parts = p.parts;
     a.lanes = p.lanes;
     a.div_N = make_fastdiv(a.N);
+    a.div_P = make_fastdiv(a.P);
     const unsigned param_blocks = a.dweight || a.dbias ? static_cast<unsigned>((a.C + 15) / 16) : 0;
     if (p.tokens) {
         a.sums = p.grid;
