@@ -50,7 +50,7 @@ DecaySegments fwd_segments(const qta_decay_attn_args* a)
 {
     return a->N <= kDecayStepTokens ? DecaySegments{1, a->N} : decay_segments(a->B, a->heads, a->N, a->dv, 1, use_bf16(a));
 }
-DecaySegments bwd_segments(const qta_decay_attn_args* a) { return decay_segments(a->B, a->heads, a->N, std::max(a->dk, a->dv), 2, use_bf16(a)); }
+DecaySegments bwd_segments(const qta_decay_attn_args* a) { return decay_segments(a->B, a->heads, a->N, std::min(a->dk, a->dv), 2, use_bf16(a)); }
 size_t fwd_bytes(const qta_decay_attn_args* a)
 {
     const int segs = fwd_segments(a).segs;

@@ -112,7 +112,7 @@ __device__ __forceinline__ void store_tile(void* base, long long at, const f32x1
 // (two) do where the state only makes results of 8.
 // STATES: only what each segment adds to the state, to a.part. Otherwise the results, from the states before each segment.
 template <typename T, int DK, int DV, bool STATES, bool EXACT>
-__global__ __launch_bounds__(2 * DV, sizeof(T) == 2 ? (DK == 128 && DV == 32 ? 2 : 3) : (DK == 32 ? 3 : 2)) void decay_chunk_kernel(DecayArgs a)
+__global__ __launch_bounds__(2 * DV, decay_waves(sizeof(T) == 2, DK, DV)) void decay_chunk_kernel(DecayArgs a)
 {
     using KT = Tile<T, DK>;
     using VT = Tile<T, DV>;
