@@ -84,8 +84,8 @@ inline NormPlan norm_plan(int B, int N, int C, int groups, bool per_token, bool 
         p.cols = p.wide ? 1 : std::min(groups, slots);              // groups of a workgroup
         p.rows = p.wide ? 1 : slots / p.cols;                       // tokens of a workgroup at a time
         p.blocks = (groups + p.cols - 1) / p.cols;
-        // four workgroups a unit, each with its own sums for the weights (16384 tokens of 16 x 128, bf16: forward and backward 29 and
-        // 42 us and 6 for the sums; with two 35, 49 and 4, with eight 30, 51 and 11)
+        // four workgroups a unit, each with its own sums for the weights (16384 tokens of 16 x 128, bf16: forward and backward 26 and 40 us,
+        // 5.1 TB/s, and 6 for the sums; when these took 29 and 42, two a unit took 35, 49 and 4, eight 30, 51 and 11)
         const long long tokens = (static_cast<long long>(B) * N + p.rows - 1) / p.rows;
         p.grid = static_cast<int>(std::min<long long>(tokens, std::max(1LL, 4LL * device_cu_count() / p.blocks)));
         p.bytes = back ? static_cast<size_t>(p.grid) * C * 2 * sizeof(float) : 0;
@@ -113,7 +113,7 @@ inline NormPlan norm_plan(int B, int N, int C, int groups, bool per_token, bool 
     }
     p.rows = kNormThreads / p.cols;
     // one workgroup a unit: half as many threads in twice as many, or two a unit, read more of the slabs' sums in all (2 x 19200 tokens
-    // of 256 channels, bf16: the second launch 16 us, 22 and 30). Where batch elements and blocks leave slabs uneven over
+    // of 256 channels, bf16: the second launch takes 10.7 us; when it took 16 they took 22 and 30). Where batch elements and blocks leave slabs uneven over
     // the units, four times as many.
     const long long want = device_cu_count(), wide = static_cast<long long>(B) * p.blocks;
     const long long many = want / wide >= 8 ? want / wide : (4 * want + wide - 1) / wide;
