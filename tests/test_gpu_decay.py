@@ -347,3 +347,51 @@ def test_a_layer_of_them(dev):
         o, state = layer(*[t[:, n:n + 1] for t in qkv], start=n, state=state)
         rows.append(o)
     assert float((torch.cat(rows, 1).double() - ref).detach().abs().max()) <= 2000 * R.F * float(ref.detach().abs().max())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(128, 32), (64, 128), (32, 64)])
+def test_other_widths(dev, dk, dv, dtype):
+    """The pairs of widths that the sizes leave out, in one and in several segments."""
+    for N in (5, 75, 500):
+        check(*make(dev, 2, N, 2, dk, dv, dtype, seed=N + dk))
+        args, ups = make(dev, 2, N, 2, dk, dv, dtype, seed=N)
+        check(args, ups, lens=[N - 3, N // 2])
+
+
+@pytest.mark.parametrize("N", [6, 200])
+def test_broadcast_batches_and_tokens(dev, N):
+    """Zero strides along the batch and along the tokens."""
+    r = gen(21, dev)
+    q, k, v = r(1, N, 2, 32).expand(3, N, 2, 32), r(3, 1, 2, 32).expand(3, N, 2, 32), r(1, 1, 2, 64).expand(3, N, 2, 64)
+    (_, _, _, g, s), _ = make(dev, 3, 1, 2, 32, 64, "f32", seed=N)
+    check((q, k, v, g, s), (r(3, N, 2, 64), r(3, 2, 32, 64)), label="broadcast")
+
+
+def test_a_captured_training_step(dev):
+    """Forward and backward captured together, replayed on new inputs, against eager steps."""
+    (q, k, v, g, _), (dout, _) = make(dev, 1, 150, 2, 32, 32, "f32", seed=3, state=False)
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+
+    def step(xs):
+        y = P.decay_attention(*xs, g)
+        y = P.group_norm(y.flatten(-2), 2, per_token=True).unflatten(-1, (2, 32))
+        return torch.autograd.grad(y, xs, dout)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step(leaves)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        grads = step(leaves)
+    r = gen(5, dev)
+    for _ in range(3):
+        with torch.no_grad():
+            for t in leaves:
+                t.copy_(r(*t.shape))
+        graph.replay()
+        eager = step([t.detach().clone().requires_grad_() for t in leaves])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(grads, eager))

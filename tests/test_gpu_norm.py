@@ -209,3 +209,14 @@ def test_refusals(dev):
         P.group_norm(x.to(torch.bfloat16), 2, w, z(8, t=torch.bfloat16))
     with pytest.raises(TypeError):
         P.group_norm([1.0], 2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("per_token", [False, True])
+@pytest.mark.parametrize("shape,groups", [((2, 3, 600), 300), ((1, 2, 1200), 1200), ((1, 6, 8200), 1), ((1, 5, 2501), 1), ((2, 40, 9), 9),
+                                          ((1, 70, 4400), 1100), ((3, 1, 2048), 16)],
+                         ids=lambda s: "x".join(map(str, s)) if isinstance(s, tuple) else str(s))
+def test_many_and_wide_groups(dev, shape, groups, per_token, dtype):
+    """More groups than a workgroup has lanes for, and groups wider than a workgroup."""
+    x, w, b, dy = make(dev, shape, dtype, seed=sum(shape))
+    check(x, groups, w, b, dy, per_token=per_token, act="gelu")
