@@ -65,7 +65,7 @@ def _decay_args(q, k, v, log_decay, scale, lens, state):
 
 
 def _decay_forward(args, shape, q, state, state_out):
-    out = torch.empty(shape, dtype=q.dtype, device=q.device)
+    out = q.new_empty(shape)
     if out.numel() == 0 or args.dk == 0:
         out.zero_()
         if state_out is not None and state_out is not state:

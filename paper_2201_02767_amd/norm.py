@@ -6,7 +6,7 @@ import ctypes
 import torch
 
 from .decay import _once
-from .dense import _call, _no_tangents, _tokens, _workspace
+from .dense import _call, _new, _no_tangents, _tokens, _workspace
 from .qta import _DTYPES, _SIGS, _dtype_code
 
 _P, _I, _F, _L = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_int64
@@ -54,7 +54,7 @@ def _norm_args(x, groups, weight, bias, eps, act, per_token):
 
 
 def _norm_forward(args, x, keep):
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    y = _new(x)
     stats = torch.empty((args.B, args.groups, 2), dtype=torch.float32, device=x.device) if keep and not args.per_token else None
     if y.numel():
         ws, nbytes = (None, 0) if args.per_token else _workspace("qta_group_norm_workspace_bytes", args, x)
@@ -87,19 +87,18 @@ class _GroupNorm(torch.autograd.Function):
             args.bias = None if bias is None else bias.data_ptr()
         else:
             args = _norm_args(x, groups, weight, bias, eps, act, per_token)
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dx = torch.empty_like(dy)
         dw = torch.empty_like(weight) if weight is not None and ctx.needs_input_grad[1] else None
         db = torch.empty_like(bias) if bias is not None and ctx.needs_input_grad[2] else None
         if dx.numel():
-            n = 256
+            ws, n = None, 0
             if not per_token or dw is not None or db is not None:
                 ws, n = _workspace("qta_group_norm_backward_workspace_bytes", args, x)
-            else:
-                ws = None
-            if ws is None:
-                ws, n = torch.empty(256, dtype=torch.uint8, device=x.device), 256
+                if ws is None:
+                    ws, n = torch.empty(256, dtype=torch.uint8, device=x.device), 256
             _call("qta_group_norm_backward", x, ctypes.byref(args), None if stats is None else stats.data_ptr(), dy.data_ptr(),
-                  dx.data_ptr(), None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(), ws.data_ptr(), n)
+                  dx.data_ptr(), None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+                  None if ws is None else ws.data_ptr(), n)
         else:
             for t in (dw, db):
                 if t is not None:
