@@ -471,8 +471,8 @@ qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const float* m
  *               used, whatever it holds; its results are zeros.
  * Tokens before the lengths are finite: a tile computes the places that the order of time masks and leaves them out by a weight
  * of zero. Sums and states are fp32. With bf16 inputs the state and the weighted scores are taken into products as two bf16
- * terms (16 bits), what is added to the state as three (24 bits) where the call returns a state and as two otherwise, and results are
- * rounded once.
+ * terms (16 bits), what is added to the state as three (24 bits), and results are rounded once. They are the same bits whether or not
+ * the call returns a state.
  */
 typedef struct {
     const void* q;

@@ -150,7 +150,6 @@ qta_status qta_decay_attn(const qta_decay_attn_args* args, void* out, float* sta
     }
     DecayArgs a = make_args(args, seg);
     a.roles = 1;
-    a.exact = state_out != nullptr;
     a.part = static_cast<float*>(workspace);
     DecayRole& r = a.role[0];
     r = make_role({args->q, args->q_batch, args->q_token, args->q_head}, {args->k, args->k_batch, args->k_token, args->k_head},
@@ -166,7 +165,6 @@ qta_status qta_decay_attn(const qta_decay_attn_args* args, void* out, float* sta
         scan.last[0] = state_out;
         if (launch_decay_scan(scan, 1, s) != hipSuccess) return QTA_ERR_HIP;
         r.state = a.part;
-        a.exact = false;
     } else {
         r.state = args->state;
         r.last = state_out;
@@ -201,7 +199,6 @@ qta_status qta_decay_attn_backward(const qta_decay_attn_args* args, const void* 
         v{args->v, args->v_batch, args->v_token, args->v_head},
         d{dout, static_cast<long long>(args->N) * args->heads * DV, static_cast<long long>(args->heads) * DV, DV};
     DecayArgs a = make_args(args, seg);
-    a.exact = dstate != nullptr;
     const float* before = args->state;          // S and R, dk x dv each
     const float* behind = dstate_out;
     if (seg.segs > 1) {
@@ -220,7 +217,6 @@ qta_status qta_decay_attn_backward(const qta_decay_attn_args* args, const void* 
         scan.state[1] = behind;
         scan.last[1] = dstate;
         if (launch_decay_scan(scan, 2, s) != hipSuccess) return QTA_ERR_HIP;
-        a.exact = false;
         before = a.part;
         behind = a.part + static_cast<size_t>(args->B) * args->heads * seg.segs * DK * DV;
     }

@@ -38,7 +38,6 @@ struct DecayArgs {
     const float* log_decay;
     const int32_t* lens;
     float scale;
-    bool exact;                 // the states are results themselves
     float* part;                // fp32 [roles][B][heads][segs][DK][DV]: what each segment adds to the state, then the states before them
 };
 

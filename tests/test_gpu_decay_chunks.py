@@ -1,0 +1,25 @@
+"""Linear attention with a decay on the GPU: its bits, and its chunks and segments where they are many."""
+import pytest
+import torch
+
+import paper_2201_02767_amd as P
+from tests.test_gpu_decay import make
+from tests.test_gpu_dense import announce, dev       # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dk,dv", [(32, 64), (128, 128)])
+@pytest.mark.parametrize("N", [5, 40, 130, 600, 3000])
+def test_results_are_the_same_with_and_without_a_state(dev, N, dk, dv, dtype):
+    """The bits of a result do not depend on whether the state, or its gradient, is asked for."""
+    (q, k, v, g, s), (dout, dlast) = make(dev, 2, N, 2, dk, dv, dtype, seed=N)
+    announce(f"decay_attn with and without the state {N} {dk} {dv} {dtype}")
+    assert torch.equal(P.decay_attn(q, k, v, g, state=s), P.decay_attn(q, k, v, g, state=s, return_state=True)[0])
+    zero = torch.zeros_like(s)
+    assert torch.equal(P.decay_attn(q, k, v, g), P.decay_attn(q, k, v, g, state=zero, return_state=True)[0])
+    without = P.decay_attn_backward(q, k, v, g, dout, dstate_out=dlast)
+    assert without[3] is None
+    given = P.decay_attn_backward(q, k, v, g, dout, state=zero, dstate_out=dlast)
+    assert all(torch.equal(a, b) for a, b in zip(without[:3], given[:3]))
