@@ -114,6 +114,10 @@ __device__ __forceinline__ void slope(float (&z)[N], int act)
     }
 }
 
+// The variance, from the mean square of the distances from a rounded mean and their mean, which is what that rounding left. Added to the mean, that
+// makes the mean of equal values their value, so that they are nothing but the bias, however large r is.
+__device__ __forceinline__ float variance(float square, float left) { return fmaxf(square - left * left, 0.f); }
+
 // Sum over `lanes` (a power of two up to 64) neighbouring lanes, in all of them.
 __device__ __forceinline__ float team_sum(float x, int lanes)
 {
@@ -191,16 +195,23 @@ __global__ __launch_bounds__(256) void norm_tokens_kernel(NormArgs a)
         }
         if (r0 + step < rows) fetch(r0 + step);
         const float mean = team_sum(sum, a.lanes) * inv;
-        float sq = 0.f;
+        float sq = 0.f, left = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 x[k][i] = on[k] ? x[k][i] - mean : 0.f;
                 sq += x[k][i] * x[k][i];
+                left += x[k][i];
             }
+        // what the mean's rounding left (places that hold no channel have weights of zero)
+        left = team_sum(left, a.lanes) * inv;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[k][i] -= left;
         // (rows behind the last add nothing to the weights' gradients, also where eps is 0)
-        const float r = here ? 1.f / sqrtf(team_sum(sq, a.lanes) * inv + a.eps) : 0.f;
+        const float r = here ? 1.f / sqrtf(variance(team_sum(sq, a.lanes) * inv, left) + a.eps) : 0.f;
         if constexpr (!BACK) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -301,14 +312,20 @@ __global__ __launch_bounds__(256) void norm_wide_kernel(NormArgs a)
 #pragma unroll
             for (int i = 0; i < V; ++i) sum += x[i];
         }
-        const float mean = group_total(sum, box) * inv;
+        float mean = group_total(sum, box) * inv, left = 0.f;
         sum = 0.f;
         for (int c = c0; c < c1; c += 256 * V) {
             load_piece<T, V>(a.x, from + c, x);
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum += (x[i] - mean) * (x[i] - mean);
+            for (int i = 0; i < V; ++i) {
+                const float d = x[i] - mean;
+                sum += d * d;
+                left += d;
+            }
         }
-        const float r = 1.f / sqrtf(group_total(sum, box) * inv + a.eps);
+        left = group_total(left, box) * inv;
+        const float r = 1.f / sqrtf(variance(group_total(sum, box) * inv, left) + a.eps);
+        mean += left;
         float s0 = 0.f, s1 = 0.f;
         if constexpr (BACK) {
             for (int c = c0; c < c1; c += 256 * V) {
@@ -455,10 +472,13 @@ __global__ __launch_bounds__(kT) void norm_stats_kernel(NormArgs a)
     if (at.mine) {
         float2* const to = box + at.row * wide + (at.col - at.c0) / V * each;
         if (whole) {
-            float m = 0.f, s = 0.f;
+            float m = 0.f, left = 0.f, s = 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) m += mean[i];
             m *= 1.f / V;
+#pragma unroll
+            for (int i = 0; i < V; ++i) left += mean[i] - m;
+            m += left * (1.f / V);
 #pragma unroll
             for (int i = 0; i < V; ++i) s += sq[i] + count * (mean[i] - m) * (mean[i] - m);
             to[0] = make_float2(m, s);
@@ -472,7 +492,8 @@ __global__ __launch_bounds__(kT) void norm_stats_kernel(NormArgs a)
     const int lane = threadIdx.x & (lanes - 1);
     const float per = static_cast<float>(whole ? V : 1);
     for (int g = threadIdx.x / lanes; g < groups; g += kT / lanes) {
-        float m = 0.f, s = 0.f;
+        float m = 0.f, left = 0.f, s = 0.f;
+        const float entries = static_cast<float>(tokens) * of_group;
         // (a part of a group is wider than half a workgroup: one row)
         auto each = [&](auto add) {
 #pragma unroll 4
@@ -482,9 +503,15 @@ __global__ __launch_bounds__(kT) void norm_stats_kernel(NormArgs a)
             }
         };
         each([&](float2 v, float n) { m += n * v.x; });
-        m = team_sum(m, lanes) / (static_cast<float>(tokens) * of_group);
-        each([&](float2 v, float n) { s += v.y + n * per * (v.x - m) * (v.x - m); });
-        s = team_sum(s, lanes);
+        m = team_sum(m, lanes) / entries;
+        each([&](float2 v, float n) {
+            const float d = v.x - m;
+            left += n * d;
+            s += v.y + n * per * d * d;
+        });
+        left = team_sum(left, lanes) / entries;
+        s = entries * per * variance(team_sum(s, lanes) / (entries * per), left);
+        m += left;
         const int entry = a.parts == 1 ? at.c0 / a.P + g : at.block;
         if (lane == 0) reinterpret_cast<float2*>(a.part)[(static_cast<long long>(at.b) * a.slabs + at.slab) * a.entries + entry] = make_float2(m, s);
     }
@@ -514,8 +541,7 @@ __device__ __forceinline__ void join_stats(const NormArgs& a, const NormPlace& a
     const float inv = 1.f / (static_cast<float>(a.N) * a.P);
     for (int g = threadIdx.x / lanes; g < groups; g += kT / lanes) {
         const float2* const from = part + (g0 + g) * a.parts;
-        // the mean, then the distances from it; what the mean's own rounding left of their sum corrects both. A lane's first entries stay in
-        // registers between the two (2 x 19200 tokens of 256 channels, bf16: a pass takes 17.4 us, with them read again 18.9)
+        // the mean, then the distances from it, as in a slab. A lane's first entries stay in registers between the two (2 x 19200 tokens of 256 channels, bf16: a pass takes 17.4 us, with them read again 18.9, before the means were corrected)
         constexpr int kHeld = 8;
         const int total = a.slabs * a.parts;
         auto fetch = [&](int i, float2& v, float& n) {
@@ -541,18 +567,17 @@ __device__ __forceinline__ void join_stats(const NormArgs& a, const NormPlace& a
                 add(v, n);
             }
         };
-        float m = 0.f, c = 0.f, s = 0.f;
+        float m = 0.f, left = 0.f, s = 0.f;
         each([&](float2 v, float n) { m += n * v.x; });
         m = team_sum(m, lanes) * inv;
         each([&](float2 v, float n) {
             const float d = v.x - m;
-            c += n * d;
+            left += n * d;
             s += v.y + n * d * d;
         });
-        c = team_sum(c, lanes) * inv;
-        s = fmaxf(team_sum(s, lanes) * inv - c * c, 0.f);
-        m += c;
-        const float r = 1.f / sqrtf(s + a.eps);
+        left = team_sum(left, lanes) * inv;
+        const float r = 1.f / sqrtf(variance(team_sum(s, lanes) * inv, left) + a.eps);
+        m += left;
         if (lane == 0) {
             box[g] = make_float2(m, r);
             if (a.stats && at.slab == 0 && (a.parts == 1 || at.block % a.parts == 0))
@@ -573,18 +598,18 @@ __global__ __launch_bounds__(kT) void norm_apply_kernel(NormArgs a)
     params(a.bias, a.param_bf16, at.mine ? at.col : 0, 0.f, bias);
     join_stats(a, at, V, box);
     if (!at.mine) return;
-    // (x r - mean r: as far off as the mean's own rounding makes x - mean)
+    float mean[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const float2 s = box[fast_div(at.col + i, a.div_P) - at.c0 / a.P];
+        mean[i] = s.x;
         f[i] *= s.y;
-        bias[i] -= s.x * f[i];
     }
     const long long to = static_cast<long long>(at.b) * a.N * a.C + at.col;
     stream.run([&](int n, const float (&x)[V], const float (&)[V]) {
         float z[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) z[i] = x[i] * f[i] + bias[i];
+        for (int i = 0; i < V; ++i) z[i] = (x[i] - mean[i]) * f[i] + bias[i];
         activate(z, a.act);
         store_piece<T, V>(a.y, to + static_cast<long long>(n) * a.C, z);
     });
@@ -593,7 +618,7 @@ __global__ __launch_bounds__(kT) void norm_apply_kernel(NormArgs a)
 // A thread's channels in the backward.
 template <int V>
 struct NormChannels {
-    float r[V], shift[V], w[V], bias[V];        // n = x r + shift
+    float mean[V], r[V], w[V], bias[V];
     __device__ __forceinline__ NormChannels(const NormArgs& a, const NormPlace& at)
     {
         params(a.weight, a.param_bf16, at.mine ? at.col : 0, 1.f, w);
@@ -601,8 +626,8 @@ struct NormChannels {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const float2 s = reinterpret_cast<const float2*>(a.stats)[static_cast<long long>(at.b) * a.groups + (at.mine ? fast_div(at.col + i, a.div_P) : 0)];
+            mean[i] = s.x;
             r[i] = s.y;
-            shift[i] = -s.x * s.y;
         }
     }
 };
@@ -620,7 +645,7 @@ __global__ __launch_bounds__(kT) void norm_sums_kernel(NormArgs a)
         float n[V], z[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            n[i] = x[i] * ch.r[i] + ch.shift[i];
+            n[i] = (x[i] - ch.mean[i]) * ch.r[i];
             z[i] = n[i] * ch.w[i] + ch.bias[i];
         }
         slope(z, a.act);
@@ -754,7 +779,7 @@ __global__ __launch_bounds__(kT) void norm_dx_kernel(NormArgs a)
         float n[V], z[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            n[i] = x[i] * ch.r[i] + ch.shift[i];
+            n[i] = (x[i] - ch.mean[i]) * ch.r[i];
             z[i] = n[i] * ch.w[i] + ch.bias[i];
         }
         slope(z, a.act);

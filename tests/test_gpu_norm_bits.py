@@ -20,3 +20,48 @@ def test_a_slab_unlike_the_others(dev, C, groups, apart):
         x = r(1, N, C)
         x[:, at * N // 256:(at + 1) * N // 256] += apart
         within("y", P.group_norm(x, groups), R.group_norm(x, groups, N * C // 256 // 4096, N // 256))
+
+
+EQUAL = [((1, 5000, 90), 6), ((2, 700, 64), 8), ((1, 9, 4104), 1), ((1, 6, 20000), 1), ((3, 40, 96), 1), ((1, 30000, 5), 5)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("per_token", [False, True])
+@pytest.mark.parametrize("shape,groups", EQUAL, ids=lambda s: "x".join(map(str, s)) if isinstance(s, tuple) else str(s))
+def test_equal_values_are_the_bias(dev, shape, groups, per_token, dtype):
+    """A group of equal values far from zero, which 1 / sqrt(eps) makes of any rounding of its mean: over maps the mean is exact. Per token
+    distances from the first mean, 100 f of it at most (as many values at most follow each other in a sum), are corrected by their mean, 100 f
+    of them off: (100 f)^2 |x| r. Their mean square, less that of their mean, is 200 f (100 f x)^2 off nothing."""
+    r = gen(43, dev)
+    C = shape[-1]
+    b = r(C).to(dtype)
+    announce(f"group_norm of equal values {shape} {groups} {per_token} {dtype}")
+    for value in (1000.1, -1e4 / 3, 2.0 ** -10 / 3):
+        x = torch.full(shape, value, device=dev, dtype=dtype)
+        w, value = (1 + 0.3 * r(C)).to(dtype), float(x[0, 0, 0])
+        y = P.group_norm(x, groups, w, b, per_token=per_token)
+        if per_token:
+            off = (100 * R.F) ** 2 * abs(value) / 1e-5 ** 0.5 * w.double().abs()
+            u = torch.finfo(dtype).eps / 2
+            assert bool(((y.double() - b.double()).abs() <= off + u * (b.double().abs() + off)).all()), value
+        else:
+            assert torch.equal(y, b.expand(shape)), value
+        # and dx is r (dn - mean dn): the group's gradients without their mean
+        x.requires_grad_()
+        dy = r(*shape).to(dtype)
+        dx, = torch.autograd.grad(P.group_norm(x, groups, w, b, per_token=per_token), x, dy)
+        dn = (dy.double() * w.double()).unflatten(-1, (groups, -1))
+        over = (3,) if per_token else (1, 3)
+        want = ((dn - dn.mean(over, keepdim=True)) / 1e-5 ** 0.5).flatten(-2)
+        # (r by 4 f and eps as a float; the sum of dn by a step for each of its terms in a row, at most 100 here)
+        dr = 8 * R.F + per_token * 100 * R.F * (100 * R.F * value) ** 2 / 1e-5
+        bound = (torch.finfo(dtype).eps / 2 + dr) * want.abs() + 108 * R.F * (dn.abs() + dn.abs().mean(over, keepdim=True)).flatten(-2) / 1e-5 ** 0.5
+        within("dx", dx, (want, bound))
+
+
+@pytest.mark.parametrize("shift", [0.0, 300.0, -5000.0])
+def test_means_far_from_zero(dev, shift):
+    r = gen(44, dev)
+    announce(f"group_norm, means of {shift}")
+    x = r(1, 262144, 16) + shift
+    within("y", P.group_norm(x, 2), R.group_norm(x, 2, 4, 1024))
