@@ -544,8 +544,8 @@ typedef struct {
  *   y           [B][N][C] dtype, contiguous, aligned as x. Not x itself.
  *   stats       for qta_group_norm_backward: fp32 [B][groups][2], mean and 1 / sqrt(var + eps), 8-byte aligned. NULL for inference, and
  *               not used with per_token.
- *   workspace   qta_group_norm_workspace_bytes bytes (at least 256 for valid shapes, 0 otherwise), 256-byte aligned; may be NULL where 256
- *               are asked for. Need not be preserved or cleared; calls that may run at the same time need one each.
+ *   workspace   qta_group_norm_workspace_bytes bytes (256 with per_token, more without, 0 for invalid shapes), 256-byte aligned; may be NULL
+ *               where 256 are asked for. Need not be preserved or cleared; calls that may run at the same time need one each.
  */
 size_t qta_group_norm_workspace_bytes(const qta_group_norm_args* args);
 qta_status qta_group_norm(const qta_group_norm_args* args, void* y, float* stats, void* workspace, size_t workspace_bytes,
@@ -555,6 +555,8 @@ qta_status qta_group_norm(const qta_group_norm_args* args, void* y, float* stats
  * qta_group_norm_backward - gradients for dy = dLoss/dy, contiguous, aligned as x; stats are the forward's (not used with per_token).
  *   dx          [B][N][C] dtype, contiguous, overwritten.
  *   dweight, dbias  [C] param_dtype, overwritten; each may be NULL. (With weight NULL they are those of weights of 1 and 0.)
+ *   workspace   qta_group_norm_backward_workspace_bytes bytes (more than 256 for valid shapes), as above; may be NULL with per_token where
+ *               neither dweight nor dbias is asked for.
  */
 size_t qta_group_norm_backward_workspace_bytes(const qta_group_norm_args* args);
 qta_status qta_group_norm_backward(const qta_group_norm_args* args, const float* stats, const void* dy, void* dx, void* dweight,

@@ -45,10 +45,10 @@ int widest(const qta_group_norm_args* a, const void* p, const void* q, const voi
     while (V > 1 && !ok(V)) V /= 2;
     return V;
 }
-// The most that a call asks for, whatever its alignment.
+// The most that a call asks for, whatever its alignment: above kAlign, which says that a call takes none, unless it does.
 size_t most_bytes(const qta_group_norm_args* a, bool back)
 {
-    size_t n = kAlign;
+    size_t n = a->per_token && !back ? kAlign : 2 * kAlign;
     for (int v = use_bf16(a) ? 8 : 4; v >= 1; v /= 2) n = std::max(n, plan(a, v, back).bytes);
     return n;
 }

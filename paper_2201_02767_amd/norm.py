@@ -58,8 +58,6 @@ def _norm_forward(args, x, keep):
     stats = torch.empty((args.B, args.groups, 2), dtype=torch.float32, device=x.device) if keep and not args.per_token else None
     if y.numel():
         ws, nbytes = (None, 0) if args.per_token else _workspace("qta_group_norm_workspace_bytes", args, x)
-        if ws is None and not args.per_token:
-            ws, nbytes = torch.empty(256, dtype=torch.uint8, device=x.device), 256
         _call("qta_group_norm", x, ctypes.byref(args), y.data_ptr(), None if stats is None else stats.data_ptr(),
               None if ws is None else ws.data_ptr(), nbytes)
     return y, stats
@@ -94,8 +92,6 @@ class _GroupNorm(torch.autograd.Function):
             ws, n = None, 0
             if not per_token or dw is not None or db is not None:
                 ws, n = _workspace("qta_group_norm_backward_workspace_bytes", args, x)
-                if ws is None:
-                    ws, n = torch.empty(256, dtype=torch.uint8, device=x.device), 256
             _call("qta_group_norm_backward", x, ctypes.byref(args), None if stats is None else stats.data_ptr(), dy.data_ptr(),
                   dx.data_ptr(), None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
                   None if ws is None else ws.data_ptr(), n)
