@@ -465,7 +465,7 @@ qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const float* m
  *   log_decay   device fp32 [heads], natural logarithms of the decays: <= 0 (-inf: nothing is remembered). A positive one grows;
  *               results are then right as long as they are finite. Beyond +-11356 it counts as that.
  *   state       fp32 [B][heads][dk][dv] contiguous, 16-byte aligned, or NULL for zeros.
- *   dk, dv      32, 64 or 128 each. N at most 2^29, heads 2^16, B * heads 2^24.
+ *   dk, dv      32, 64 or 128 each. N at most 2^29, heads 2^16, B * heads 2^22 (more is unsupported where a launch does not take it).
  *   scale       2^-64 .. 2^64; <= 0: 1/sqrt(dk).
  *   lens        device int32 [B] or NULL: element b's tokens are [0, lens[b]) (clamped to [0, N]). What lies behind them is never
  *               used, whatever it holds; its results are zeros.
@@ -522,7 +522,8 @@ qta_status qta_decay_attn_backward(const qta_decay_attn_args* args, const void* 
  *   x           [B][N][C] dtype by strides in elements, channels contiguous, aligned to its type (16-byte aligned tensors whose strides
  *               and C are multiples of 16 bytes take 16-byte accesses, others narrower ones).
  *   weight, bias  [C] contiguous, fp32 or (with bf16 x) bf16, aligned to their type; each may be NULL (1 and 0).
- *   groups      divides C; B * N and C at most 2^30 and 2^20, B * C at most 2^30.
+ *   groups      divides C; B * N and C at most 2^30 and 2^20, B * C at most 2^30, and B but with per_token at most 2^21 (more is
+ *               unsupported where a launch does not take it).
  *   eps         at least 0 (a group of equal values is then 0 times infinity).
  * Statistics and sums are fp32, differences from the mean, in a fixed order: runs are identical. Results are rounded once.
  */

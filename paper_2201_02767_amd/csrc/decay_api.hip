@@ -61,11 +61,15 @@ size_t bwd_bytes(const qta_decay_attn_args* a)
     const int segs = bwd_segments(a).segs;
     return segs > 1 ? 2 * part_bytes(a, segs) : 0;
 }
-// Whether every launch of a call is one that HIP takes.
-bool fits(const qta_decay_attn_args* a, int roles, int segs)
+// Whether every launch of a call is one that HIP takes, in workgroups of at most 256 threads.
+bool fits(const qta_decay_attn_args* a, int roles, int segs, bool step)
 {
-    return static_cast<long long>(roles) * a->B * a->heads * std::max(segs, (a->dk * a->dv + 1023) / 1024) <= kDecayMaxBlocks;
+    const long long rows = static_cast<long long>(a->B) * a->heads;
+    const long long scan = segs > 1 ? rows * (a->dk * a->dv / 1024) : 0;
+    return std::max(step ? rows * decay_step_slices(a->dv) : roles * rows * segs, scan) <= kDecayMaxBlocks;
 }
+bool fwd_fits(const qta_decay_attn_args* a) { return fits(a, 1, fwd_segments(a).segs, a->N <= kDecayStepTokens); }
+bool bwd_fits(const qta_decay_attn_args* a) { return fits(a, 3, bwd_segments(a).segs, false); }
 
 struct Operand {
     const void* x;
@@ -114,7 +118,7 @@ extern "C" {
 
 size_t qta_decay_attn_workspace_bytes(const qta_decay_attn_args* args)
 {
-    if (check_decay(args, true) != QTA_OK || !fits(args, 1, fwd_segments(args).segs)) return 0;
+    if (check_decay(args, true) != QTA_OK || !fwd_fits(args)) return 0;
     return std::max(fwd_bytes(args), kAlign);
 }
 
@@ -125,7 +129,7 @@ qta_status qta_decay_attn(const qta_decay_attn_args* args, void* out, float* sta
     if (st != QTA_OK) return st;
     if (!out || !aligned(out, 16) || !aligned(state_out, 16)) return QTA_ERR_INVALID;
     const DecaySegments seg = fwd_segments(args);
-    if (!fits(args, 1, seg.segs)) return QTA_ERR_UNSUPPORTED;
+    if (!fwd_fits(args)) return QTA_ERR_UNSUPPORTED;
     if (seg.segs > 1) {
         if (workspace_bytes < fwd_bytes(args)) return QTA_ERR_WORKSPACE;
         if (!workspace || !aligned(workspace, kAlign)) return QTA_ERR_INVALID;
@@ -174,7 +178,7 @@ qta_status qta_decay_attn(const qta_decay_attn_args* args, void* out, float* sta
 
 size_t qta_decay_attn_backward_workspace_bytes(const qta_decay_attn_args* args)
 {
-    if (check_decay(args, true) != QTA_OK || !fits(args, 3, bwd_segments(args).segs)) return 0;
+    if (check_decay(args, true) != QTA_OK || !bwd_fits(args)) return 0;
     return std::max(bwd_bytes(args), kAlign);
 }
 
@@ -187,7 +191,7 @@ qta_status qta_decay_attn_backward(const qta_decay_attn_args* args, const void* 
         if (!p || !aligned(p, 16)) return QTA_ERR_INVALID;
     if (!aligned(dstate_out, 16) || !aligned(dstate, 16) || (dstate && dstate == dstate_out)) return QTA_ERR_INVALID;
     const DecaySegments seg = bwd_segments(args);
-    if (!fits(args, 3, seg.segs)) return QTA_ERR_UNSUPPORTED;
+    if (!bwd_fits(args)) return QTA_ERR_UNSUPPORTED;
     if (seg.segs > 1) {
         if (workspace_bytes < bwd_bytes(args)) return QTA_ERR_WORKSPACE;
         if (!workspace || !aligned(workspace, kAlign)) return QTA_ERR_INVALID;

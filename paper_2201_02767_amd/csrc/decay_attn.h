@@ -66,6 +66,8 @@ struct DecayStepArgs {
 
 // Calls of up to this many tokens go token by token through states that stay in registers.
 constexpr int kDecayStepTokens = 16;
+// Workgroups that share the columns of a head's state in them, 64 each.
+constexpr int decay_step_slices(int dv) { return dv < 64 ? 1 : dv / 64; }
 
 // Tokens of a chunk: a tile of the products.
 constexpr int kDecayChunk = 32;

@@ -439,6 +439,7 @@ hipError_t launch_step(const DecayStepArgs& a, hipStream_t stream)
     DecayStepArgs p = a;
     p.div_heads = make_fastdiv(a.heads);
     constexpr int SV = DV < 64 ? DV : 64;
+    static_assert(DV / SV == decay_step_slices(DV), "as the launches are checked");
     const long long blocks = static_cast<long long>(a.B) * a.heads * (DV / SV);
     hipLaunchKernelGGL((decay_step_kernel<T, DK, DV, SV>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, p);
     return hipGetLastError();

@@ -3,8 +3,9 @@ import pytest
 import torch
 
 import paper_2201_02767_amd as P
+from tests import decay_ref as R
 from tests.test_gpu_decay import make
-from tests.test_gpu_dense import announce, dev       # noqa: F401
+from tests.test_gpu_dense import announce, dev, gen, within       # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +24,20 @@ def test_results_are_the_same_with_and_without_a_state(dev, N, dk, dv, dtype):
     assert without[3] is None
     given = P.decay_attn_backward(q, k, v, g, dout, state=zero, dstate_out=dlast)
     assert all(torch.equal(a, b) for a, b in zip(without[:3], given[:3]))
+
+
+@pytest.mark.parametrize("N,d", [(1, 128), (17, 32)])
+def test_as_many_heads_as_the_header_names(dev, N, d):
+    """2^22 (batch, head) pairs, forward and backward, on a sample of the batch elements."""
+    B, heads = 1 << 18, 16
+    announce(f"decay_attn {B} x {heads} heads of {d}, {N} tokens")
+    q, k, v, dout = (torch.empty(B, N, heads, d, device=dev, dtype=torch.bfloat16).normal_() for _ in range(4))
+    g = -torch.logspace(-0.3, -3.0, heads, device=dev)
+    out = P.decay_attn(q, k, v, g)
+    grads = P.decay_attn_backward(q, k, v, g, dout)
+    torch.cuda.synchronize()
+    for b in (0, 99_999, B - 1):
+        some = [t[b:b + 1] for t in (q, k, v)]
+        want = R.decay_attention(*some, g, dout=dout[b:b + 1])
+        for n, t in zip(("out", "dq", "dk", "dv"), (out, *grads)):
+            within(n, t[b:b + 1], want[n])
