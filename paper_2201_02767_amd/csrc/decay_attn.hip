@@ -78,8 +78,11 @@ __device__ __forceinline__ u32x4_t map_words(const unsigned char* base)
 // (that wait in the middle of a chunk: 130 us for 105 of the states of 65536 tokens). Wait for them with s_waitcnt vmcnt.
 __device__ __forceinline__ void load_lds16_untracked(const u32x4_t& map, uint32_t off, uint32_t dst)
 {
-    // (nothing else here uses m0; five wait states between a lane operation that wrote the descriptor and the load, one behind m0)
-    asm volatile("s_nop 4\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(map), "s"(dst) : "memory");
+    // (five wait states between a lane operation that wrote the descriptor and the load, one behind m0. The compiler takes no m0 on a list of what
+    // is overwritten, so it is put back)
+    uint32_t kept;
+    asm volatile("s_mov_b32 %0, m0\n\ts_nop 3\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(kept) : "v"(off), "s"(map), "s"(dst) : "memory");
 }
 
 // log2 of a head's decay, so large at most that products with token counts stay numbers.
