@@ -463,14 +463,17 @@ qta_status qta_diff_attn_backward(const qta_diff_attn_args* args, const float* m
  *   q, k        [B][N][heads][dk], v [B][N][heads][dv] dtype, by strides in elements; channels contiguous, pointers 16-byte
  *               aligned, strides multiples of 16 bytes (0: broadcast).
  *   log_decay   device fp32 [heads], natural logarithms of the decays: <= 0 (-inf: nothing is remembered). A positive one grows;
- *               results are then right as long as they are finite. Beyond +-11356 it counts as that.
+ *               results are then right as long as exp(g N) is an fp32 number, and what it is multiplied with too (g N below 80, values of
+ *               some hundreds). Beyond +-11356 it counts as that.
  *   state       fp32 [B][heads][dk][dv] contiguous, 16-byte aligned, or NULL for zeros.
  *   dk, dv      32, 64 or 128 each. N at most 2^29, heads 2^16, B * heads 2^22 (more is unsupported where a launch does not take it).
  *   scale       2^-64 .. 2^64; <= 0: 1/sqrt(dk).
  *   lens        device int32 [B] or NULL: element b's tokens are [0, lens[b]) (clamped to [0, N]). What lies behind them is never
  *               used, whatever it holds; its results are zeros.
- * Tokens before the lengths are finite: a tile computes the places that the order of time masks and leaves them out by a weight
- * of zero. Sums and states are fp32. With bf16 inputs the state and the weighted scores are taken into products as two bf16
+ * Tokens before the lengths, states and upstream gradients are finite: in calls of more than 16 tokens, and in gradients, a tile computes the
+ * places that the order of time masks and leaves them out by a weight of zero, so that a NaN or an infinity (of a product of two tokens
+ * too) also reaches up to 31 neighbours that do not depend on its token; other heads and batch elements it never does.
+ * Sums and states are fp32. With bf16 inputs the state and the weighted scores are taken into products as two bf16
  * terms (16 bits), what is added to the state as three (24 bits), and results are rounded once. They are the same bits whether or not
  * the call returns a state.
  */

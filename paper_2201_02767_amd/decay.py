@@ -96,13 +96,17 @@ def decay_attn(q, k, v, log_decay, *, scale=None, lens=None, state=None, return_
         S_t = exp(g) S_{t-1} + k_t v_t^T,    out_t = scale * S_t^T q_t.
 
     q, k ``[B, N, heads, dk]``, v ``[B, N, heads, dv]`` (or maps ``[B, H, W, ..]``, row by row), dk and dv 32, 64 or 128;
-    ``log_decay`` fp32 ``[heads]``, at most 0. Returns ``[B, N, heads, dv]``; with ``return_state`` or ``state_out`` a pair of
+    ``log_decay`` fp32 ``[heads]``, at most 0 (a positive one grows, and is right while exp(g N) stays far from fp32's largest: g N below
+    80). Returns ``[B, N, heads, dv]``; with ``return_state`` or ``state_out`` a pair of
     it and the state behind the last token, fp32 ``[B, heads, dk, dv]``.
 
     ``state``: the state before the first token (None: zeros), so that a call goes on where another one ended: prompts
     in pieces, then single tokens, which are read and written through the state alone. ``state_out``: where the new state goes;
     may be ``state`` itself. ``lens`` (int32 ``[B]``): tokens of each batch element; what lies behind them is never used, and gives
-    zeros. ``scale``: positive, or None for 1/sqrt(dk)."""
+    zeros. ``scale``: positive, or None for 1/sqrt(dk).
+
+    Tokens before the lengths and the state have to be finite: in calls of more than 16 tokens a NaN or an infinity makes NaNs of up to 31
+    *earlier* results of its head as well."""
     _no_tangents(q, k, v, log_decay, state)
     args, shape, sshape = _decay_args(q, k, v, log_decay, scale, lens, state)
     given = state_out is not None
@@ -175,7 +179,8 @@ class _DecayAttention(torch.autograd.Function):
 
 def decay_attention(q, k, v, log_decay, *, scale=None, lens=None, state=None, return_state=False):
     """Differentiable ``decay_attn`` (reverse mode): gradients of q, k, v and state, from those of the output and of the returned
-    state. ``log_decay`` that requires gradients is refused."""
+    state. ``log_decay`` that requires gradients is refused. Upstream gradients have to be finite like the tokens: what is not reaches
+    up to 31 gradients on the other side of its token too."""
     _no_tangents(q, k, v, log_decay, state)
     if not (torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in (q, k, v, log_decay, state))):
         return decay_attn(q, k, v, log_decay, scale=scale, lens=lens, state=state, return_state=return_state)
