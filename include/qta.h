@@ -528,7 +528,9 @@ qta_status qta_decay_attn_backward(const qta_decay_attn_args* args, const void* 
  *   groups      divides C; B * N and C at most 2^30 and 2^20, B * C at most 2^30, and B but with per_token at most 2^21 (more is
  *               unsupported where a launch does not take it).
  *   eps         at least 0 (a group of equal values is then 0 times infinity).
- * Statistics and sums are fp32, differences from the mean, in a fixed order: runs are identical. Results are rounded once.
+ * Statistics and sums are fp32, differences from the mean, in a fixed order: runs are identical. Results are rounded once. A NaN or an
+ * infinity in x makes NaNs of its group's results (with per_token of its token's group) and of the gradients that these enter, and reaches
+ * nothing else. Squares of differences from the mean that overflow in sum make the variance infinite, and results the bias's.
  */
 typedef enum { QTA_ACT_NONE = 0, QTA_ACT_RELU = 1, QTA_ACT_SILU = 2, QTA_ACT_GELU = 3 } qta_act;    /* GELU by the error function */
 typedef struct {

@@ -107,7 +107,9 @@ def group_norm(x, groups, weight=None, bias=None, *, eps=1e-5, act="none", per_t
     ``[B, H, W, C]``, fp32 or bf16; mean and variance are those of each of the ``groups`` groups of C / groups neighbouring channels
     over the tokens of a batch element, or with ``per_token`` over one token (which causal models need, and the heads of an
     attention's output ``out.flatten(-2)`` with a group for each). ``weight``, ``bias``: ``[C]``, fp32 or x's type, or None.
-    ``act``: "none", "relu", "silu" or "gelu" (by the error function). Differentiable in x, weight and bias (reverse mode)."""
+    ``act``: "none", "relu", "silu" or "gelu" (by the error function). Differentiable in x, weight and bias (reverse mode).
+
+    A NaN or an infinity makes NaNs of its group's results (with ``per_token`` of its token's group), and reaches no other group."""
     _no_tangents(x, weight, bias)
     if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in (x, weight, bias)):
         return _GroupNorm.apply(x, weight, bias, groups, eps, act, per_token)

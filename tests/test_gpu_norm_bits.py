@@ -1,4 +1,6 @@
 """Group norm over maps on the GPU where statistics lose bits, against tests/norm_bits.py's bounds."""
+import math
+
 import pytest
 import torch
 
@@ -65,3 +67,40 @@ def test_means_far_from_zero(dev, shift):
     announce(f"group_norm, means of {shift}")
     x = r(1, 262144, 16) + shift
     within("y", P.group_norm(x, 2), R.group_norm(x, 2, 4, 1024))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("per_token", [False, True])
+@pytest.mark.parametrize("shape,groups", [((2, 900, 32), 4), ((2, 50, 90), 6), ((2, 7, 9000), 2)],
+                         ids=lambda s: "x".join(map(str, s)) if isinstance(s, tuple) else str(s))
+def test_what_is_not_finite_stays_in_its_group(dev, shape, groups, per_token, value, dtype):
+    r = gen(45, dev)
+    C = shape[-1]
+    x, w, b, dy = r(*shape).to(dtype), r(C).to(dtype), r(C).to(dtype), r(*shape).to(dtype)
+    announce(f"group_norm with {value} in a group {shape} {groups} {per_token} {dtype}")
+    split = lambda t: t.detach().unflatten(-1, (groups, -1))
+    for act in ("none", "relu", "silu", "gelu"):
+        both = []
+        for bad in (False, True):
+            leaves = [t.clone() for t in (x, w, b)]
+            if bad:
+                leaves[0][1, 3, C // groups + 1] = value
+            leaves = [t.requires_grad_() for t in leaves]
+            y = P.group_norm(leaves[0], groups, *leaves[1:], act=act, per_token=per_token)
+            both.append([split(t) for t in (y, *torch.autograd.grad(y, leaves, dy))])
+        clean, got = both
+        hit = torch.zeros(*shape[:-1], groups, dtype=torch.bool, device=dev)
+        hit[1, 3 if per_token else slice(None), 1] = True
+        for n in (0, 1):
+            assert bool(got[n][hit].isnan().all()) and torch.equal(got[n][~hit], clean[n][~hit]), (act, n)
+        group = torch.arange(groups, device=dev) == 1
+        assert bool(got[2][group].isnan().all()) and all(torch.equal(got[n][~group], clean[n][~group]) for n in (2, 3)), act
+
+
+def test_squares_that_overflow(dev):
+    """Distances of 2^70: an infinite variance, and the bias."""
+    x = torch.tensor([1.0, -1.0], device=dev).repeat(1, 300, 8) * 2.0 ** 70
+    b = torch.arange(16, device=dev, dtype=torch.float32)
+    for per_token in (False, True):
+        assert torch.equal(P.group_norm(x, 2, None, b, per_token=per_token), b.expand(x.shape))
