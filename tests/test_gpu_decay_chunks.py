@@ -1,13 +1,17 @@
 """Linear attention with a decay on the GPU: its bits, and its chunks and segments where they are many."""
+import ctypes
 import math
+import sys
 
 import pytest
 import torch
 
 import paper_2201_02767_amd as P
+from paper_2201_02767_amd.decay import _decay_args
+from tests import decay_bits as Bits
 from tests import decay_ref as R
 from tests.test_gpu_decay import check, make
-from tests.test_gpu_dense import announce, dev, gen, within       # noqa: F401
+from tests.test_gpu_dense import DT, announce, dev, gen, i32, within       # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +85,72 @@ def test_growth(dev, N, dtype):
     for t in (k, v):
         t[:, :3 * N // 4] = 0
     check((q, k, v, g, None), (dout, None), label="growth of zeros")
+
+
+def chunks(args, back):
+    """(segments, chunks of 32 tokens in a segment) of a call, from the states that its workspace has room for."""
+    q, k, v, g, _ = args
+    a, _, (B, heads, dk, dv) = _decay_args(q, k, v, g, None, None, None)
+    name = "qta_decay_attn_backward_workspace_bytes" if back else "qta_decay_attn_workspace_bytes"
+    one = B * heads * dk * dv * 4 * (2 if back else 1)
+    segs = max(1, getattr(P.lib(), name)(ctypes.byref(a)) // one)
+    tokens = -(-q.shape[1] // segs)
+    return segs, -(-tokens // 32)
+
+
+# widths, and batch elements, heads and tokens, that give segments of many chunks, with four, three and two chunks in LDS at a time
+MANY = [("bf16", 32, 32, 4, 16, 32, 1171), ("bf16", 64, 64, 4, 16, 16, 1171), ("bf16", 64, 128, 3, 8, 16, 900), ("bf16", 32, 128, 4, 16, 16, 1171),
+        ("bf16", 128, 32, 2, 16, 32, 700), ("bf16", 128, 128, 2, 8, 16, 777), ("f32", 32, 32, 4, 16, 32, 1171), ("f32", 32, 64, 3, 16, 16, 900),
+        ("f32", 64, 64, 2, 16, 16, 777), ("f32", 128, 128, 2, 8, 16, 777)]
+
+
+@pytest.mark.parametrize("dtype,dk,dv,depth,B,heads,N", MANY, ids=lambda x: str(x))
+def test_segments_of_many_chunks(dev, dtype, dk, dv, depth, B, heads, N):
+    """Every place in LDS is used again and again, in several segments, forward and backward, with decays that remember whole segments (e^-1.6 over
+    1171 tokens and up), and lengths within and on the borders of segments and chunks."""
+    assert depth == (4 if 4 * (2 * dk + dv) * 32 * (2 if dtype == "bf16" else 4) <= 49152 else
+                     3 if 3 * (2 * dk + dv) * 32 * (2 if dtype == "bf16" else 4) <= 49152 else 2)
+    (q, k, v, _, s), ups = make(dev, B, N, heads, dk, dv, dtype, seed=N + dk)
+    g = -torch.logspace(-4.0, -2.9, heads, device=dev)
+    args = (q, k, v, g, s)
+    for back in (False, True):
+        segs, each = chunks(args, back)
+        assert segs >= (1 if back else 2) and each >= 2 * depth + 1, (back, segs, each)
+    check(args, ups, label="many chunks")
+    lens = [N, 0, N - 1, 1, 33, N // 2, N // 2 // 32 * 32, 321, 320][:B]
+    check(args, ups, label="many chunks", lens=lens + [N - 5] * (B - len(lens)))
+
+
+@pytest.mark.parametrize("dk,dv", [(32, 32), (64, 128), (128, 128)])
+@pytest.mark.parametrize("B,N", [(2, 60), (1, 300), (2, 5000)])
+def test_returned_states_keep_24_bits(dev, B, N, dk, dv):
+    """States and their gradients from bf16 tokens, whose weighted values are taken as three bf16 terms, and not as two."""
+    (q, k, v, _, s), (dout, dlast) = make(dev, B, N, 4, dk, dv, "bf16", seed=N)
+    g = torch.tensor(Bits.DECAYS, device=dev)
+    announce(f"decay_attn, bits of the states {B} {N} {dk} {dv}")
+    want = R.decay_attention(q, k, v, g, state=s, dout=dout, dstate_out=dlast)
+    _, last = P.decay_attn(q, k, v, g, state=s, return_state=True)
+    dstate = P.decay_attn_backward(q, k, v, g, dout, state=s, dstate_out=dlast)[3]
+    for n, t in (("state", last), ("dstate", dstate)):
+        off = Bits.rms(t.double(), want[n][0])
+        print(f"{n}: {[round(x, 2) for x in off]} f", file=sys.stderr)
+        assert max(off) <= Bits.STATE, (n, off)
+
+
+@pytest.mark.parametrize("dk,dv", [(32, 32), (64, 128), (128, 64), (128, 128)])
+@pytest.mark.parametrize("B,N", [(2, 12), (2, 60), (1, 300), (2, 3000)])
+def test_fp32_keeps_its_bits(dev, B, N, dk, dv):
+    """The root mean square of the errors, where the bounds element by element are worst cases that leave room for products of far fewer bits. f = 2^-24,
+    independent roundings of 0.4 f: a score and a row of the state's product sum up to 128 terms, 4.5 f each; a weight, a product of two to
+    four powers and a rounded exponent, is off by 2 f; a state is rounded with every chunk that it remembers, and in the scan, 2.2 f each as in
+    tests/decay_bits.py. Together 7.5 f, and twice that is the limit. Products of 16 bits are off by 2^-17 = 128 f, and of bf16 terms by
+    2^-16."""
+    (q, k, v, _, s), (dout, dlast) = make(dev, B, N, 4, dk, dv, "f32", seed=N + 1)
+    g = torch.tensor(Bits.DECAYS, device=dev)
+    announce(f"decay_attn, fp32 bits {B} {N} {dk} {dv}")
+    want = R.decay_attention(q, k, v, g, state=s, dout=dout, dstate_out=dlast)
+    got = (*P.decay_attn(q, k, v, g, state=s, return_state=True), *P.decay_attn_backward(q, k, v, g, dout, state=s, dstate_out=dlast))
+    for n, t in zip(("out", "state", "dq", "dk", "dv", "dstate"), got):
+        off = Bits.rms(t.double(), want[n][0], 2 if n in ("out", "dq", "dk", "dv") else 1)
+        print(f"{n}: {[round(x, 1) for x in off]} f", file=sys.stderr)
+        assert max(off) <= 15.0, (n, off)
