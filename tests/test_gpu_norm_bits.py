@@ -1,11 +1,13 @@
 """Group norm over maps on the GPU where statistics lose bits, against tests/norm_bits.py's bounds."""
 import math
+import sys
 
 import pytest
 import torch
 
 import paper_2201_02767_amd as P
 from tests import norm_bits as R
+from tests import norm_ref as Ref
 from tests.test_gpu_dense import announce, dev, gen, within                # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -104,3 +106,25 @@ def test_squares_that_overflow(dev):
     b = torch.arange(16, device=dev, dtype=torch.float32)
     for per_token in (False, True):
         assert torch.equal(P.group_norm(x, 2, None, b, per_token=per_token), b.expand(x.shape))
+
+
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+@pytest.mark.parametrize("per_token", [False, True])
+@pytest.mark.parametrize("shape,groups", [((3, 5063, 90), 6), ((2, 40, 2048), 2), ((1, 60, 5000), 1), ((1, 40000, 32), 4)],
+                         ids=lambda s: "x".join(map(str, s)) if isinstance(s, tuple) else str(s))
+def test_fp32_keeps_its_bits(dev, shape, groups, per_token, act):
+    """The root mean square of the errors, relative to the values'. f = 2^-24, independent roundings of 0.4 f: x - mean and what the mean is off,
+    0.7 f; r, 1 f; n, z and the products around them five roundings, 0.9 f; an activation or its slope, 2 f. So y within 2.5 f; dz and dn, and the sums that
+    dx takes from them (whose terms' errors differ in sign), 3 f; the weights' gradients, with the 40 additions at most that a value passes,
+    4 f. Twice that are the limits. Statistics of 16 bits, or a mean that keeps 2^-20 of a group's width, are off by more than 16."""
+    r = gen(46, dev)
+    C = shape[-1]
+    x, w, b, dy = r(*shape) * (0.5 + r(C).abs()) + r(C), 1 + 0.2 * r(C), 0.2 * r(C), r(*shape)
+    announce(f"group_norm, fp32 bits {shape} {groups} {per_token} {act}")
+    want = Ref.group_norm(x, groups, w, b, act=act, per_token=per_token, dy=dy)
+    leaves = [t.requires_grad_() for t in (x, w, b)]
+    y = P.group_norm(x, groups, w, b, act=act, per_token=per_token)
+    for (n, t), limit in zip(zip(("y", "dx", "dweight", "dbias"), (y.detach(), *torch.autograd.grad(y, leaves, dy))), (5.0, 6.0, 8.0, 8.0)):
+        off = float((t.double() - want[n][0]).square().mean().sqrt() / want[n][0].square().mean().sqrt()) / R.F
+        print(f"{n}: {off:.2f} f", file=sys.stderr)
+        assert off <= limit, (n, off)
