@@ -204,20 +204,17 @@ __global__ __launch_bounds__(256) void norm_tokens_kernel(NormArgs a)
                 sq += x[k][i] * x[k][i];
                 left += x[k][i];
             }
-        // what the mean's rounding left (places that hold no channel have weights of zero)
         left = team_sum(left, a.lanes) * inv;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int i = 0; i < V; ++i) x[k][i] -= left;
         // (rows behind the last add nothing to the weights' gradients, also where eps is 0)
         const float r = here ? 1.f / sqrtf(variance(team_sum(sq, a.lanes) * inv, left) + a.eps) : 0.f;
+        // n = (x - left) r, in one instruction each (places that hold no channel have weights of zero)
+        const float shift = -left * r;
         if constexpr (!BACK) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 if (!on[k] || !here) continue;
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[k][i] = x[k][i] * r * w[k][i] + bias[k][i];
+                for (int i = 0; i < V; ++i) x[k][i] = fmaf(x[k][i], r, shift) * w[k][i] + bias[k][i];
                 activate(x[k], a.act);
                 store_piece<T, V>(a.y, to + at[k], x[k]);
             }
@@ -228,7 +225,7 @@ __global__ __launch_bounds__(256) void norm_tokens_kernel(NormArgs a)
                 float z[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    x[k][i] *= r;
+                    x[k][i] = fmaf(x[k][i], r, shift);
                     z[i] = x[k][i] * w[k][i] + bias[k][i];
                 }
                 slope(z, a.act);
@@ -639,23 +636,27 @@ __global__ __launch_bounds__(kT) void norm_sums_kernel(NormArgs a)
     extern __shared__ __align__(16) float2 box[];                   // [V][kT]
     const NormPlace at(a, xcd_remap(blockIdx.x, gridDim.x), V);
     NormStream<T, V, 2, true, false> stream(a, at);
-    float s1[V] = {}, s0[V] = {};
+    float s1[V] = {}, s0[V] = {}, f[V];
     const NormChannels<V> ch(a, at);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = ch.r[i] * ch.w[i];
     stream.run([&](int, const float (&x)[V], const float (&dy)[V]) {
-        float n[V], z[V];
+        float d[V], z[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            n[i] = (x[i] - ch.mean[i]) * ch.r[i];
-            z[i] = n[i] * ch.w[i] + ch.bias[i];
+            d[i] = x[i] - ch.mean[i];
+            z[i] = d[i] * f[i] + ch.bias[i];
         }
         slope(z, a.act);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const float dz = dy[i] * z[i];
-            s1[i] += dz * n[i];
+            s1[i] += dz * d[i];
             s0[i] += dz;
         }
     });
+#pragma unroll
+    for (int i = 0; i < V; ++i) s1[i] *= ch.r[i];
 #pragma unroll
     for (int i = 0; i < V; ++i) box[i * kT + threadIdx.x] = make_float2(s1[i], s0[i]);
     __syncthreads();
