@@ -77,7 +77,7 @@ constexpr int kDecayTables = 4096 + 2 * kDecayChunk * 4;            // bytes of 
 constexpr int decay_depth(int bytes) { return 4 * bytes <= (48 << 10) ? 4 : 3 * bytes <= (48 << 10) ? 3 : 2; }
 
 // Waves a SIMD that the kernels' registers are held to: as many as they fit without going to memory inside the chunks' loop, or nearly so (2 x
-// 8192 bf16 tokens, 16 heads of 128/64: 58 us with two, 72 with three and 18 registers in memory; 2 x 4096 fp32 tokens, 16 heads of
+// 8192 bf16 tokens, 16 heads of 128/64: 64 us with two, 81 with three and 18 registers in memory; 2 x 4096 fp32 tokens, 16 heads of
 // 128/32: 93 us with one, 131 with two and 163 in memory; of 128/64 142 with two and 18, 144 with one).
 constexpr int decay_waves(bool bf16_inputs, int dk, int dv)
 {
@@ -86,14 +86,14 @@ constexpr int decay_waves(bool bf16_inputs, int dk, int dv)
 }
 
 // Segments of a call: enough for two workgroups of four waves a unit, or as many waves in smaller ones (2 x 8192 tokens, 16 heads of 128,
-// bf16, forward and backward: states 31 + 31, scans 11 + 11, results 67 + 175 us; with four a unit 40 + 36, 21 + 21 and 72 + 190: the
+// bf16, forward and backward: states 57 + 57, scans 12 + 12, results 88 + 230 us; with four a unit 60 + 60, 23 + 23 and 88 + 239: the
 // states' bytes), none below two chunks, or one in fp32, whose products take 16 times as long (2 x 997 tokens, 8 heads of 32, a step's five
-// launches 53 us with two, 44 with one; 3 x 1031 bf16 tokens, 8 heads of 32/64: 20 us with two and with one, 29 with eight).
+// launches 53 us with two, 44 with one; 3 x 1031 bf16 tokens, 8 heads of 32/64: as long with two as with one, 1.4 times with eight).
 struct DecaySegments {
     int segs, seg;
 };
 // `dv`: the width that makes the workgroups' waves; in a backward, whose launches have either width, the smaller (a backward of 2 x 4096
-// fp32 tokens, 16 heads of 128/32: 298 us by the larger, 245 by the smaller; bf16 2 x 8192 of 128/64: 233 and 215).
+// fp32 tokens, 16 heads of 128/32: 298 us by the larger, 245 by the smaller).
 inline DecaySegments decay_segments(int B, int heads, int N, int dv, int roles, bool bf16_inputs)
 {
     const long long rows = static_cast<long long>(B) * heads * roles, want = 2LL * device_cu_count() * 128 / dv;

@@ -4,12 +4,13 @@
 // chunk to chunk. Scores come transposed, K Q^T, and the state with its rows in the order of a fragment, so that both are operands
 // of the products that make the results, V^T P^T and S^T Q^T, where they lie.
 //
-// What bounds them. 65536 tokens, 16 heads of 64/128, bf16: states 93 to 104 us (403 MB, 3.9 to 4.3 TB/s), results 179 to 220 (820 MB; without
+// What bounds them. 65536 tokens, 16 heads of 64/128, bf16: states 89 to 104 us (403 MB, 3.9 to 4.5 TB/s), results 185 to 231 (820 MB; without
 // any product 197, without stores 120), both at the clock that their power leaves, which a run of passes lowers. 2 x 8192 tokens, 16 heads of
-// 128, bf16, backward: results 176 to 214 us, vector units at work in 57% of the cycles and matrix units in 38%: what is split into two terms.
+// 128, bf16, backward: results 195 to 226 us, vector units at work in 56% of the cycles and matrix units in 41%: what is split into terms.
 // Few or short sequences wait for a chunk's chain of products, 0.5 us in bf16 and 1.1 in fp32 with 32 channels, and for three launches.
-// Tried: a state brought to the present every eight chunks instead of every one (a branch in the chunk: 233 us for 214), results through
-// LDS for whole lines (registers go to memory at 128 x 128: 239), stores past the caches (240 for 220 of the prompts).
+// Tried, with two terms in what states get: a state brought to the present every eight chunks instead of every one (a branch in the chunk:
+// 233 us for 214), results through LDS for whole lines (registers go to memory at 128 x 128: 239), stores past the caches (240 for 220 of the
+// prompts).
 #include <atomic>
 
 #include "decay_attn.h"

@@ -37,8 +37,8 @@ struct NormArgs {
     FastDiv div_N, div_P, div_slabs, div_rows, div_entry;
 };
 
-// Maps take two launches that each go over them (bound by memory: 8 maps of 200 x 336 x 256 bf16, 275 MB each, SiLU: 45 us to read x, 103 to
-// read it and write y, 101 to read x and dy, 157 to read them and write dx, 5.2 to 6.1 TB/s, where a large copy makes 5.1). The second
+// Maps take two launches that each go over them (bound by memory: 8 maps of 200 x 336 x 256 bf16, 275 MB each, SiLU: 46 us to read x, 105 to
+// read it and write y, 100 to read x and dy, 155 to read them and write dx, 5.2 to 6.0 TB/s, where a large copy makes 5.1). The second
 // goes through every slab from its end, where the memory's cache still holds what the first read last, and stores go past the caches (with
 // ordinary stores, whose lines the next kernel's reads push out, and upwards: 71, 95, 150 and 164 us).
 // Batch elements one after the other, which would fit the caches, fill the card too badly: 467 us for these 407.
@@ -84,8 +84,8 @@ inline NormPlan norm_plan(int B, int N, int C, int groups, bool per_token, bool 
         p.cols = p.wide ? 1 : std::min(groups, slots);              // groups of a workgroup
         p.rows = p.wide ? 1 : slots / p.cols;                       // tokens of a workgroup at a time
         p.blocks = (groups + p.cols - 1) / p.cols;
-        // four workgroups a unit, each with its own sums for the weights (16384 tokens of 16 x 128, bf16: forward and backward 26 and 40 us,
-        // 5.1 TB/s, and 6 for the sums; when these took 29 and 42, two a unit took 35, 49 and 4, eight 30, 51 and 11)
+        // four workgroups a unit, each with its own sums for the weights (16384 tokens of 16 x 128, bf16: forward and backward 29 and 43 us,
+        // 4.7 TB/s, and 6 for the sums; two a unit take 1.2 times as long and 4, eight as long forward, 1.2 times as long backward, and 11)
         const long long tokens = (static_cast<long long>(B) * N + p.rows - 1) / p.rows;
         p.grid = static_cast<int>(std::min<long long>(tokens, std::max(1LL, 4LL * device_cu_count() / p.blocks)));
         p.bytes = back ? static_cast<size_t>(p.grid) * C * 2 * sizeof(float) : 0;
@@ -113,7 +113,7 @@ inline NormPlan norm_plan(int B, int N, int C, int groups, bool per_token, bool 
     }
     p.rows = kNormThreads / p.cols;
     // one workgroup a unit: half as many threads in twice as many, or two a unit, read more of the slabs' sums in all (2 x 19200 tokens
-    // of 256 channels, bf16: the second launch takes 10.7 us; when it took 16 they took 22 and 30). Where batch elements and blocks leave slabs uneven over
+    // of 256 channels, bf16: the second launch takes 11.8 us; when it took 16 they took 22 and 30). Where batch elements and blocks leave slabs uneven over
     // the units, four times as many.
     const long long want = device_cu_count(), wide = static_cast<long long>(B) * p.blocks;
     const long long many = want / wide >= 8 ? want / wide : (4 * want + wide - 1) / wide;

@@ -291,7 +291,8 @@ __device__ __forceinline__ float group_total(float x, float* box)
 }
 
 // Tokens whose groups no wave holds: a workgroup goes over a group three times (four in the backward), from the second on mostly in
-// the caches. Its threads keep the sums of their channels in its row of `part`.
+// the caches. Its threads keep the sums of their channels in its row of `part`. Bound by those readings, and in the backward by that row: one group of
+// 4096 channels, 16384 tokens in bf16 153 us forward (268 MB) and 677 backward (403 MB), 8192 in fp32 88 and 300.
 template <typename T, int V, bool BACK>
 __global__ __launch_bounds__(256) void norm_wide_kernel(NormArgs a)
 {
