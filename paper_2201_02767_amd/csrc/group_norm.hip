@@ -115,8 +115,9 @@ __device__ __forceinline__ void slope(float (&z)[N], int act)
 }
 
 // The variance, from the mean square of the distances from a rounded mean and their mean, which is what that rounding left. Added to the mean, that
-// makes the mean of equal values their value, so that they are nothing but the bias, however large r is.
-__device__ __forceinline__ float variance(float square, float left) { return fmaxf(square - left * left, 0.f); }
+// makes the mean of equal values their value, so that they are nothing but the bias, however large r is. (In one instruction: left * left by itself may
+// overflow, and an infinite square less that be no number.)
+__device__ __forceinline__ float variance(float square, float left) { return fmaxf(fmaf(-left, left, square), 0.f); }
 
 // Sum over `lanes` (a power of two up to 64) neighbouring lanes, in all of them.
 __device__ __forceinline__ float team_sum(float x, int lanes)

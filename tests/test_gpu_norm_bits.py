@@ -100,12 +100,18 @@ def test_what_is_not_finite_stays_in_its_group(dev, shape, groups, per_token, va
         assert bool(got[2][group].isnan().all()) and all(torch.equal(got[n][~group], clean[n][~group]) for n in (2, 3)), act
 
 
-def test_squares_that_overflow(dev):
-    """Distances of 2^70: an infinite variance, and the bias."""
-    x = torch.tensor([1.0, -1.0], device=dev).repeat(1, 300, 8) * 2.0 ** 70
-    b = torch.arange(16, device=dev, dtype=torch.float32)
+@pytest.mark.parametrize("shape", [(1, 300, 16), (1, 9000, 6), (2, 3, 5000)], ids=str)
+@pytest.mark.parametrize("power,mean", [(70, 0.0), (70, 3.0), (100, 3.0), (100, -1.7)])
+def test_squares_that_overflow(dev, power, mean, shape):
+    """Distances of 2^70 and 2^100: an infinite variance, the bias, and no gradient of x."""
+    r = gen(47, dev)
+    announce(f"group_norm, values of 2^{power}, {mean} {shape}")
+    x = ((r(*shape) + mean) * 2.0 ** power).requires_grad_()
+    b = r(shape[-1])
     for per_token in (False, True):
-        assert torch.equal(P.group_norm(x, 2, None, b, per_token=per_token), b.expand(x.shape))
+        y = P.group_norm(x, 2 if shape[-1] < 5000 else 1, None, b, per_token=per_token)
+        assert torch.equal(y, b.expand(shape))
+        assert not bool(torch.autograd.grad(y, x, r(*shape))[0].any())
 
 
 @pytest.mark.parametrize("act", ["none", "silu", "gelu"])
